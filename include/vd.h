@@ -328,6 +328,98 @@ vd_status vd_running_sum_init(const vd_cache* c, double* running_sum, vd_stream_
 vd_status vd_running_sum_init_ex(const vd_cache* c, int32_t of_keys, double* running_sum,
                                  vd_stream_t stream);
 
+/* ------------------------------------------------------------------------
+ * A cache held in 4 bits (not in the paper: a storage form of its cache, for
+ * what a budget N leaves to be kept), the attention that reads it, and the pass
+ * that makes the rows.  head_dim is a multiple of 32, at most 256; capacity a
+ * multiple of 8.
+ *
+ * Format: 16 neighbouring values of a row share a scale s, the group's largest
+ * magnitude / 6 rounded to nearest (ties to even) to an unsigned 8-bit float
+ * with 5 exponent bits (bias 15, subnormals) and 3 mantissa bits, at most 10240
+ * (larger groups saturate).  A value is stored as the nearest of
+ * +-{0, .5, 1, 1.5, 2, 3, 4, 6} * s (ties to the even code; code = sign << 3 |
+ * index): 4.5 bits a value.  What a code stands for is exact in bf16, and
+ * storing it again gives the same code (for scales of 2^-14 and more).  A group with
+ * a NaN or an infinity reads as NaN (scale byte 255), recorded as VD_ERR_NONFINITE.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  void* k;          /* device, [n_seq][n_layer][n_kv_head][capacity][head_dim / 2] bytes:
+                       byte i of a row holds values 2 i (low half) and 2 i + 1 */
+  void* v;          /* same layout as k */
+  void* k_scale;    /* device, [n_seq][n_layer][n_kv_head][capacity][head_dim / 16] bytes */
+  void* v_scale;    /* same layout; all four 16-byte aligned */
+  int32_t* len;     /* device int32 [n_seq], as in vd_cache */
+  int32_t n_seq, n_layer, n_kv_head;
+  int32_t head_dim; /* multiple of 32, at most 256 */
+  int32_t capacity; /* slots per unit, a multiple of 8 */
+} vd_q4_cache;
+
+/* vd_append into a 4-bit cache: B new bf16 rows per unit at slots
+ * [len, len + B), len += B.  Arguments and errors as vd_append. */
+vd_status vd_q4_append(const vd_q4_cache* c, const void* k_new, const void* v_new, int32_t B,
+                       vd_stream_t stream);
+
+/* Rows [0, src->len) of a bf16 cache (an evicted one, say) into layers
+ * [layer0, layer0 + src->n_layer) of dst.  n_seq, n_kv_head and head_dim have to
+ * agree (VD_ERR_INVALID_ARG); capacities may differ, and a sequence longer than
+ * dst's is left untouched (VD_ERR_DEVICE_LEN).  The call that writes dst's last
+ * layer also sets dst->len to src->len; layer by layer, call it in layer order. */
+vd_status vd_q4_pack(const vd_q4_cache* dst, int32_t layer0, const vd_cache* src,
+                     vd_stream_t stream);
+
+/* The way back: rows [0, src->len) of layers [layer0, layer0 + dst->n_layer) of
+ * src to bf16 (exact) in dst, and dst->len = src->len; so that every vd_evict_*
+ * call can run on them before they are packed again.  Errors as vd_q4_pack. */
+vd_status vd_q4_unpack(const vd_q4_cache* src, int32_t layer0, const vd_cache* dst,
+                       vd_stream_t stream);
+
+/* Attention of B new tokens per sequence over one layer of a 4-bit cache and
+ * over the new tokens' own rows (Sec. 2.2, Eq. block_processing: a block attends
+ * to C_{i-1} and, causally, to itself):
+ *   s_j = scale * q . k_j,  out = sum_j softmax(s)_j v_j
+ * over j in the len[s] cached slots and new rows 0 .. i for token i.
+ *   q, out        bf16 device [n_seq][B][n_q_head][head_dim], 16-byte aligned; query head h
+ *                 reads KV head h / (n_q_head / n_kv_head).
+ *   n_q_head      a multiple of n_kv_head.
+ *   k_new, v_new  bf16 device [n_seq][n_layer][n_kv_head][B][head_dim], the buffers of
+ *                 vd_q4_append (layer `layer` is read), or both NULL: the tokens see
+ *                 the cached rows alone, all of them.
+ *   lse_out       nullable fp32 device [n_seq][B][n_q_head]: log sum_j exp(s_j).
+ * A token that sees no row (len 0, no new rows) gets out = 0 and lse = -inf.
+ * A sequence with len out of [0, capacity] gets no output (VD_ERR_DEVICE_LEN).
+ * The cache is not modified.  Scores, softmax statistics and sums are fp32; a weight
+ * is rounded to fp16 (bf16 for the new rows) before it multiplies its value.  out must
+ * not overlap the inputs.  VD_ERR_TIMEOUT: the outputs are unspecified. */
+vd_status vd_q4_attend(const vd_q4_cache* c, int32_t layer, const void* q, int32_t n_q_head,
+                       const void* k_new, const void* v_new, int32_t B, float scale, void* out,
+                       float* lse_out, vd_stream_t stream);
+
+/* The rows of new tokens from their projections, in one pass: per head of the
+ * queries and keys an RMS norm x * w / sqrt(mean(x^2) + eps), then the position
+ * rotation of its first rotary_dim values; values are copied.
+ *   qkv           bf16 device [n_seq][B][n_q_head + 2 * n_kv_head][head_dim]: query,
+ *                 key, value heads.  head_dim a multiple of 8, at most 256.
+ *   q_weight, k_weight  nullable bf16 device [head_dim]: norm weights; NULL: no norm.
+ *   eps           in [0, 1].
+ *   rotary_dim    a multiple of 16, at most head_dim; 0: no rotation.
+ *   inv_freq      fp32 device [rotary_dim / 2]; pair i turns by
+ *                 (pos_first_new[s] + b) * inv_freq[i] (the angle in fp64).
+ *   interleaved   0: pair i is (x[i], x[i + rotary_dim / 2]); 1: (x[2 i], x[2 i + 1]).
+ *   pos_first_new int32 device [n_seq]: the position of the first new token, as in
+ *                 the hole-fill calls.
+ *   q_out         bf16 device [n_seq][B][n_q_head][head_dim] (vd_q4_attend's q).
+ *   k_new, v_new  bf16 device [n_seq][n_layer][n_kv_head][B][head_dim], the buffers of
+ *                 the vd_append* calls; layer `layer` is written.
+ * Norms, angles' sines and rotation are fp32, rounded once.  Outputs must not overlap
+ * the input.  All bf16 buffers 16-byte aligned. */
+vd_status vd_qkv_norm_rope(const void* qkv, int32_t n_seq, int32_t B, int32_t n_q_head,
+                           int32_t n_kv_head, int32_t head_dim, const void* q_weight,
+                           const void* k_weight, float eps, const float* inv_freq,
+                           int32_t rotary_dim, int32_t interleaved, const int32_t* pos_first_new,
+                           void* q_out, void* k_new, void* v_new, int32_t layer, int32_t n_layer,
+                           vd_stream_t stream);
+
 /* Device scratch the calls need beyond their arguments: always 0 (the fused
  * kernels keep every intermediate on chip). */
 size_t vd_workspace_size(const vd_cache* c);

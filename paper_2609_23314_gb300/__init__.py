@@ -26,6 +26,7 @@ __all__ = [
     "vd_evict_block_holefill", "vd_evict_decode_holefill", "vd_append",
     "vd_running_sum_init", "vd_running_sum_init_ex", "vd_workspace_size", "vd_status_string",
     "vd_get_device_status",
+    "Q4Cache", "vd_q4_append", "vd_q4_pack", "vd_q4_unpack", "vd_q4_attend", "vd_qkv_norm_rope",
     "library_path", "load_library",
 ]
 
@@ -50,6 +51,13 @@ class _VdCache(ctypes.Structure):
                 ("n_seq", ctypes.c_int32), ("n_layer", ctypes.c_int32),
                 ("n_kv_head", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("capacity", ctypes.c_int32)]
+
+
+class _VdQ4Cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("len", ctypes.c_void_p), ("n_seq", ctypes.c_int32),
+                ("n_layer", ctypes.c_int32), ("n_kv_head", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("capacity", ctypes.c_int32)]
 
 
 def library_path() -> str:
@@ -83,6 +91,13 @@ def load_library() -> ctypes.CDLL:
             lib.vd_append.argtypes = [cp, P, P, I32, P]
             lib.vd_running_sum_init.argtypes = [cp, P, P]
             lib.vd_running_sum_init_ex.argtypes = [cp, I32, P, P]
+            qp, F = ctypes.POINTER(_VdQ4Cache), ctypes.c_float
+            lib.vd_q4_append.argtypes = [qp, P, P, I32, P]
+            lib.vd_q4_pack.argtypes = [qp, I32, cp, P]
+            lib.vd_q4_unpack.argtypes = [qp, I32, cp, P]
+            lib.vd_q4_attend.argtypes = [qp, I32, P, I32, P, P, I32, F, P, P, P]
+            lib.vd_qkv_norm_rope.argtypes = [P, I32, I32, I32, I32, I32, P, P, F, P, I32, I32, P,
+                                             P, P, P, I32, I32, P]
             lib.vd_workspace_size.argtypes = [cp]
             lib.vd_workspace_size.restype = ctypes.c_size_t
             lib.vd_status_string.argtypes = [S]
@@ -92,7 +107,8 @@ def load_library() -> ctypes.CDLL:
                       "vd_append_evict_block", "vd_append_evict_block_ex", "vd_append_evict_decode",
                       "vd_evict_decode", "vd_evict_block_holefill",
                       "vd_evict_decode_holefill", "vd_append", "vd_running_sum_init",
-                      "vd_running_sum_init_ex",
+                      "vd_running_sum_init_ex", "vd_q4_append", "vd_q4_pack", "vd_q4_unpack",
+                      "vd_q4_attend", "vd_qkv_norm_rope",
                       "vd_get_device_status"):
                 getattr(lib, f).restype = S
             _lib = lib
@@ -182,6 +198,52 @@ class Cache:
         shape = (n_seq, n_layer, n_kv_head, capacity, head_dim)
         return cls(torch.zeros(shape, dtype=torch.bfloat16, device=device),
                    torch.zeros(shape, dtype=torch.bfloat16, device=device),
+                   torch.zeros(n_seq, dtype=torch.int32, device=device))
+
+    @property
+    def units(self) -> int:
+        return self.n_seq * self.n_layer * self.n_kv_head
+
+    def unit_shape(self):
+        return self._unit_shape
+
+    def ref(self):
+        return self._ref
+
+
+class Q4Cache:
+    """A KV cache in 4 bits (format: vd_q4_cache in ``include/vd.h``): codes uint8
+    [n_seq, n_layer, n_kv_head, capacity, head_dim / 2], scales uint8 [..., head_dim / 16]
+    and len int32 [n_seq], all on one CUDA device.  head_dim is a multiple of 32 (at most
+    256), capacity a multiple of 8.  Holds references to the tensors only."""
+
+    def __init__(self, k, v, k_scale, v_scale, len):
+        torch = _torch()
+        if k.dim() != 5:
+            raise ValueError("k must be [n_seq, n_layer, n_kv_head, capacity, head_dim / 2]")
+        self.k, self.v, self.k_scale, self.v_scale, self.len = k, v, k_scale, v_scale, len
+        self.n_seq, self.n_layer, self.n_kv_head, self.capacity = (int(x) for x in k.shape[:4])
+        self.head_dim = 2 * int(k.shape[4])
+        self.device = k.device
+        scales = tuple(k.shape[:4]) + (self.head_dim // 16,)
+        _ptr(k, torch.uint8, k.shape, "k", self.device)
+        _ptr(v, torch.uint8, k.shape, "v", self.device)
+        _ptr(k_scale, torch.uint8, scales, "k_scale", self.device)
+        _ptr(v_scale, torch.uint8, scales, "v_scale", self.device)
+        _ptr(len, torch.int32, (self.n_seq,), "len", self.device)
+        self._s = _VdQ4Cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+                             len.data_ptr(), self.n_seq, self.n_layer, self.n_kv_head,
+                             self.head_dim, self.capacity)
+        self._ref = ctypes.byref(self._s)
+        self._unit_shape = (self.n_seq, self.n_layer, self.n_kv_head)
+
+    @classmethod
+    def empty(cls, n_seq, n_layer, n_kv_head, capacity, head_dim, device="cuda"):
+        torch = _torch()
+        shape = (n_seq, n_layer, n_kv_head, capacity)
+        codes, scales = ([torch.zeros(shape + (head_dim // k,), dtype=torch.uint8, device=device)
+                          for _ in range(2)] for k in (2, 16))
+        return cls(codes[0], codes[1], scales[0], scales[1],
                    torch.zeros(n_seq, dtype=torch.int32, device=device))
 
     @property
@@ -427,6 +489,114 @@ def vd_running_sum_init(cache: Cache, running_sum, stream=None) -> None:
     rp = _ptr(running_sum, torch.float64, cache.unit_shape() + (cache.head_dim,), "running_sum",
               cache.device)
     _check(load_library().vd_running_sum_init(cache.ref(), rp, _stream(stream)), "vd_running_sum_init")
+
+
+def _on_current(device):
+    """Kernels launch on the current device: refuse tensors of another one."""
+    if device.type == "cuda" and device.index != _torch().cuda.current_device():
+        raise ValueError(f"the tensors live on {device}, the current device is "
+                         f"cuda:{_torch().cuda.current_device()}")
+
+
+def vd_q4_append(cache: Q4Cache, k_new, v_new, B: int, stream=None) -> None:
+    """vd_append into a 4-bit cache; k_new, v_new: bf16
+    [n_seq, n_layer, n_kv_head, B, head_dim]."""
+    torch = _torch()
+    _on_current(cache.device)
+    shape = cache.unit_shape() + (int(B), cache.head_dim)
+    kp = _ptr(k_new, torch.bfloat16, shape, "k_new", cache.device)
+    vp = _ptr(v_new, torch.bfloat16, shape, "v_new", cache.device)
+    _check(load_library().vd_q4_append(cache.ref(), kp, vp, int(B), _stream(stream)),
+           "vd_q4_append")
+
+
+def _same_device(q4: Q4Cache, cache: Cache):
+    if q4.device != cache.device:
+        raise ValueError(f"cache must live on {q4.device}, got {cache.device}")
+    _on_current(q4.device)
+
+
+def vd_q4_pack(dst: Q4Cache, src: Cache, layer0: int = 0, stream=None) -> None:
+    """Rows [0, src.len) of a bf16 cache into layers [layer0, layer0 + src.n_layer)
+    of a 4-bit one; the call that writes the last layer also sets dst.len."""
+    _same_device(dst, src)
+    _check(load_library().vd_q4_pack(dst.ref(), int(layer0), src.ref(), _stream(stream)),
+           "vd_q4_pack")
+
+
+def vd_q4_unpack(src: Q4Cache, dst: Cache, layer0: int = 0, stream=None) -> None:
+    """Rows [0, src.len) of layers [layer0, layer0 + dst.n_layer) of a 4-bit cache to
+    bf16 (exact) in dst, and dst.len = src.len."""
+    _same_device(src, dst)
+    _check(load_library().vd_q4_unpack(src.ref(), int(layer0), dst.ref(), _stream(stream)),
+           "vd_q4_unpack")
+
+
+def vd_q4_attend(cache: Q4Cache, q, out, k_new=None, v_new=None, layer: int = 0, scale=None,
+                 lse_out=None, stream=None) -> None:
+    """Attention of new tokens over one layer of a 4-bit cache and, causally, over their
+    own rows.  q, out: bf16 [n_seq, B, n_q_head, head_dim]; k_new, v_new: bf16
+    [n_seq, n_layer, n_kv_head, B, head_dim], the buffers of vd_q4_append, or both None
+    (every token sees the cached rows alone); scale: 1 / sqrt(head_dim) unless given;
+    lse_out: fp32 [n_seq, B, n_q_head]."""
+    torch = _torch()
+    _on_current(cache.device)
+    if q.dim() != 4:
+        raise ValueError("q must be [n_seq, B, n_q_head, head_dim]")
+    B, n_q = int(q.shape[1]), int(q.shape[2])
+    shape = (cache.n_seq, B, n_q, cache.head_dim)
+    new = cache.unit_shape() + (B, cache.head_dim)
+    args = (
+        _ptr(q, torch.bfloat16, shape, "q", cache.device),
+        _ptr(k_new, torch.bfloat16, new, "k_new", cache.device),
+        _ptr(v_new, torch.bfloat16, new, "v_new", cache.device),
+        _ptr(out, torch.bfloat16, shape, "out", cache.device),
+        _ptr(lse_out, torch.float32, shape[:3], "lse_out", cache.device),
+    )
+    scale = cache.head_dim ** -0.5 if scale is None else float(scale)
+    _check(load_library().vd_q4_attend(cache.ref(), int(layer), args[0], n_q, args[1], args[2], B,
+                                       scale, args[3], args[4], _stream(stream)),
+           "vd_q4_attend")
+
+
+def vd_qkv_norm_rope(qkv, q_out, k_new, v_new, layer: int = 0, q_weight=None, k_weight=None,
+                     eps: float = 1e-6, inv_freq=None, pos_first_new=None,
+                     interleaved: bool = False, stream=None) -> None:
+    """Queries and one layer's new rows from projections, in one pass: per-head RMS norm
+    of queries and keys (weights bf16 [head_dim], or None: no norm), rotation of their
+    first 2 * len(inv_freq) values by position (inv_freq fp32, or None: no rotation;
+    pos_first_new int32 [n_seq]), values copied.  qkv: bf16
+    [n_seq, B, n_q_head + 2 * n_kv_head, head_dim]; q_out: bf16
+    [n_seq, B, n_q_head, head_dim]; k_new, v_new: bf16
+    [n_seq, n_layer, n_kv_head, B, head_dim], of which `layer` is written."""
+    torch = _torch()
+    if qkv.dim() != 4 or q_out.dim() != 4 or k_new.dim() != 5:
+        raise ValueError("qkv and q_out must have 4 dimensions, k_new 5")
+    dev = qkv.device
+    _on_current(dev)
+    n_seq, B, heads, d = (int(x) for x in qkv.shape)
+    n_q, n_layer = int(q_out.shape[2]), int(k_new.shape[1])
+    n_kv = (heads - n_q) // 2
+    new = (n_seq, n_layer, n_kv, B, d)
+    pairs = 0 if inv_freq is None else int(inv_freq.numel())
+    if heads != n_q + 2 * n_kv:
+        raise ValueError(f"qkv has {heads} heads, which are not {n_q} query heads and as many "
+                         "key as value heads")
+    args = (
+        _ptr(qkv, torch.bfloat16, (n_seq, B, heads, d), "qkv", dev),
+        _ptr(q_weight, torch.bfloat16, (d,), "q_weight", dev),
+        _ptr(k_weight, torch.bfloat16, (d,), "k_weight", dev),
+        _ptr(inv_freq, torch.float32, (pairs,), "inv_freq", dev),
+        _ptr(pos_first_new, torch.int32, (n_seq,), "pos_first_new", dev),
+        _ptr(q_out, torch.bfloat16, (n_seq, B, n_q, d), "q_out", dev),
+        _ptr(k_new, torch.bfloat16, new, "k_new", dev),
+        _ptr(v_new, torch.bfloat16, new, "v_new", dev),
+    )
+    _check(load_library().vd_qkv_norm_rope(args[0], n_seq, B, n_q, n_kv, d, args[1], args[2],
+                                           float(eps), args[3], 2 * pairs, int(bool(interleaved)),
+                                           args[4], args[5], args[6], args[7], int(layer), n_layer,
+                                           _stream(stream)),
+           "vd_qkv_norm_rope")
 
 
 def vd_workspace_size(cache: Cache) -> int:

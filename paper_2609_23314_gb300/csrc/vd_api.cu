@@ -15,6 +15,7 @@
 
 #include "vd.h"
 #include "vd_evict.cuh"
+#include "vd_host.h"
 #include "vd_resident.cuh"
 #include "vd_small.cuh"
 
@@ -34,6 +35,7 @@ const void* score_kernel_norm(bool general);
 }  // namespace vd
 
 using vd::kThreads;
+using vd::launch_dependent;
 
 // First device-side anomaly since the last vd_get_device_status (0 = none).
 static __device__ unsigned g_vd_status;
@@ -588,27 +590,6 @@ bool cached_fits(const void* kern, long long groups, int c, size_t smem, DeviceS
   return p.cluster != 0;
 }
 
-// A plain kernel of kThreads-thread blocks as a programmatic dependent launch
-// (it waits in griddepcontrol.wait before its first access to memory).
-template <class... Params, class... Args>
-vd_status launch_dependent(unsigned blocks, cudaStream_t s, void (*kern)(Params...),
-                           Args... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(blocks);
-  cfg.blockDim = dim3(kThreads);
-  cfg.stream = s;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, kern, static_cast<Params>(args)...) != cudaSuccess) {
-    cudaGetLastError();
-    return VD_ERR_CUDA;
-  }
-  return VD_OK;
-}
-
 // groups clusters of c CTAs: the streaming and resident kernels' grids are units x
 // c CTAs (a cluster per unit), the short-cache kernel's n_seq x units_per_seq (a
 // cluster per sequence, a CTA per unit) or units x 1.
@@ -881,6 +862,28 @@ vd_status run(const vd_cache* c, int32_t N, const int32_t* N_dev, int32_t B, vd_
 
 }  // namespace
 
+namespace vd {
+
+vd_status device_info(DeviceInfo* out) {
+  DeviceState* st = nullptr;
+  const vd_status r = device_state(&st);
+  if (r == VD_OK) *out = {(int)(st - g_dev), st->sms, st->smem_optin, st->status};
+  return r;
+}
+
+uint32_t wait_limit() {
+  uint32_t scored, other;
+  wait_limits(&scored, &other);
+  return scored;
+}
+
+vd_status launch_len_add(int32_t* len, int n_seq, int cap, int B, cudaStream_t s) {
+  return launch_dependent((unsigned)((n_seq + kThreads - 1) / kThreads), s, vd_len_add_kernel, len,
+                          n_seq, cap, B);
+}
+
+}  // namespace vd
+
 // ---------------------------------------------------------------------------
 // C ABI
 // ---------------------------------------------------------------------------
@@ -994,8 +997,7 @@ vd_status vd_append(const vd_cache* c, const void* k_new, const void* v_new, int
                        static_cast<const uint16_t*>(v_new), c->len, c->n_layer * c->n_kv_head,
                        units, c->capacity, c->head_dim, B, st->status);
   if (r != VD_OK) return r;
-  return launch_dependent((unsigned)((c->n_seq + kThreads - 1) / kThreads), s, vd_len_add_kernel,
-                          c->len, c->n_seq, c->capacity, B);
+  return vd::launch_len_add(c->len, c->n_seq, c->capacity, B, s);
 }
 
 vd_status vd_running_sum_init(const vd_cache* c, double* running_sum, vd_stream_t stream) {

@@ -1,0 +1,150 @@
+// vd_q4_attend.cu -- host side of vd_q4_attend (include/vd.h): argument checks, the
+// choice of tile and cluster, the launch.
+#include <cuda_runtime.h>
+
+#include <climits>
+#include <mutex>
+
+#include "vd_host.h"
+#include "vd_q4_attend.cuh"
+
+namespace vd {
+
+namespace {
+
+using AttendKernel = void (*)(AttendArgs);
+
+struct Stream {
+  AttendKernel kern;
+  int smem, rows;
+};
+
+template <int M, int NT>
+constexpr Stream stream_of() {
+  return {q4_attend_kernel<M, NT>, AttendShape<M, NT>::kTotal, AttendShape<M, NT>::kRows};
+}
+
+// [head_dim / 32 - 1][two row tiles]; two only where their sums fit the registers
+const Stream kStream[8][2] = {
+    {stream_of<1, 1>(), stream_of<1, 2>()}, {stream_of<2, 1>(), stream_of<2, 2>()},
+    {stream_of<3, 1>(), stream_of<3, 2>()}, {stream_of<4, 1>(), stream_of<4, 2>()},
+    {stream_of<5, 1>(), stream_of<5, 1>()}, {stream_of<6, 1>(), stream_of<6, 1>()},
+    {stream_of<7, 1>(), stream_of<7, 1>()}, {stream_of<8, 1>(), stream_of<8, 1>()}};
+
+// CTAs of each kernel that run at once on the device, in clusters of 1, 2, 4, 8, 16
+// (0: such a cluster does not fit); asked for once.
+struct Slots {
+  bool ready;
+  int at[8][2][5];
+};
+std::mutex g_slots_mu;
+Slots g_slots[64];
+
+vd_status slots_of(const DeviceInfo& dev, const Slots** out) {
+  std::lock_guard<std::mutex> lk(g_slots_mu);
+  Slots& s = g_slots[dev.id];
+  if (!s.ready) {
+    for (int m = 0; m < 8; ++m)
+      for (int t = 0; t < 2; ++t) {
+        const Stream& k = kStream[m][t];
+        if (cudaFuncSetAttribute(k.kern, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem) !=
+                cudaSuccess ||
+            cudaFuncSetAttribute(k.kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) !=
+                cudaSuccess) {
+          cudaGetLastError();
+          return VD_ERR_CUDA;
+        }
+        for (int e = 0; e < 5; ++e) {
+          cudaLaunchConfig_t cfg = {};
+          cfg.gridDim = dim3(16 * dev.sms);
+          cfg.blockDim = dim3(kThreads);
+          cfg.dynamicSmemBytes = k.smem;
+          cudaLaunchAttribute attr;
+          attr.id = cudaLaunchAttributeClusterDimension;
+          attr.val.clusterDim.x = 1u << e;
+          attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+          cfg.attrs = &attr;
+          cfg.numAttrs = 1;
+          int n = 0;
+          if (cudaOccupancyMaxActiveClusters(&n, k.kern, &cfg) != cudaSuccess) {
+            cudaGetLastError();
+            n = 0;
+          }
+          s.at[m][t][e] = n << e;
+        }
+        if (s.at[m][t][0] < 1) return VD_ERR_CUDA;
+      }
+    s.ready = true;
+  }
+  *out = &s;
+  return VD_OK;
+}
+
+bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+
+}  // namespace
+
+}  // namespace vd
+
+extern "C" vd_status vd_q4_attend(const vd_q4_cache* c, int32_t layer, const void* q,
+                                  int32_t n_q_head, const void* k_new, const void* v_new,
+                                  int32_t B, float scale, void* out, float* lse_out,
+                                  vd_stream_t stream) {
+  using namespace vd;
+  vd_status r = validate_q4(c);
+  if (r != VD_OK) return r;
+  if (!q || !out || (k_new == nullptr) != (v_new == nullptr)) return VD_ERR_INVALID_ARG;
+  if (layer < 0 || layer >= c->n_layer || B < 1 || n_q_head < 1 || n_q_head % c->n_kv_head != 0)
+    return VD_ERR_INVALID_ARG;
+  if (!(scale > 0.f) || scale > 3.4e38f) return VD_ERR_INVALID_ARG;
+  if (misaligned(q) || misaligned(out) || misaligned(k_new) || misaligned(v_new))
+    return VD_ERR_ALIGNMENT;
+  const int group = n_q_head / c->n_kv_head;
+  const long long rows = (long long)B * group;
+  const long long units = (long long)c->n_seq * c->n_kv_head;
+  if (rows > (1 << 24) || units * rows > INT_MAX / 16) return VD_ERR_UNSUPPORTED;
+  DeviceInfo dev;
+  r = device_info(&dev);
+  if (r != VD_OK) return r;
+  const Slots* slots = nullptr;
+  r = slots_of(dev, &slots);
+  if (r != VD_OK) return r;
+
+  const int m = c->head_dim / 32 - 1;
+  const int two = rows > 8;
+  const Stream& k = kStream[m][two];
+  AttendArgs a;
+  const size_t unit0 = (size_t)layer * c->n_kv_head * c->capacity;
+  const size_t new0 = (size_t)layer * c->n_kv_head * B;
+  a.k = static_cast<const uint8_t*>(c->k) + unit0 * (c->head_dim / 2);
+  a.v = static_cast<const uint8_t*>(c->v) + unit0 * (c->head_dim / 2);
+  a.ks = static_cast<const uint8_t*>(c->k_scale) + unit0 * (c->head_dim / 16);
+  a.vs = static_cast<const uint8_t*>(c->v_scale) + unit0 * (c->head_dim / 16);
+  a.q = static_cast<const uint16_t*>(q);
+  a.k_new = k_new ? static_cast<const uint16_t*>(k_new) + new0 * c->head_dim : nullptr;
+  a.v_new = v_new ? static_cast<const uint16_t*>(v_new) + new0 * c->head_dim : nullptr;
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse_out;
+  a.len = c->len;
+  a.status = dev.status;
+  a.seq_rows = (size_t)c->n_layer * c->n_kv_head * c->capacity;
+  a.seq_new_rows = (size_t)c->n_layer * c->n_kv_head * B;
+  a.n_seq = c->n_seq;
+  a.heads = c->n_kv_head;
+  a.group = group;
+  a.B = B;
+  a.cap = c->capacity;
+  a.rows = (int)rows;
+  a.tiles = (int)((rows + k.rows - 1) / k.rows);
+  a.scale = scale;
+  a.wait_limit = wait_limit();
+  const long long base = units * a.tiles;
+  int e = 0;
+  while (e < 4 && slots->at[m][two][e + 1] > 0 && (base << (e + 1)) <= slots->at[m][two][e + 1] &&
+         c->capacity >= (kStageKeys * kWarps) << (e + 1))
+    ++e;
+  a.cluster = 1 << e;
+  if (base << e > INT_MAX) return VD_ERR_UNSUPPORTED;
+  return launch_clusters((unsigned)(base << e), kThreads, (unsigned)a.cluster, k.smem,
+                         reinterpret_cast<cudaStream_t>(stream), k.kern, a);
+}
