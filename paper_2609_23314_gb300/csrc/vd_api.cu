@@ -15,7 +15,7 @@
 
 #include "vd.h"
 #include "vd_evict.cuh"
-#include "vd_host.h"
+#include "vd_host.cuh"
 #include "vd_resident.cuh"
 #include "vd_small.cuh"
 
@@ -34,6 +34,7 @@ const void* score_kernel_dir();
 const void* score_kernel_norm(bool general);
 }  // namespace vd
 
+using vd::env_int;
 using vd::kThreads;
 using vd::launch_dependent;
 
@@ -685,11 +686,6 @@ int resident_plan(const void* kern, const PlanKey& k, bool decode, bool holefill
   return c;
 }
 
-int env_int(const char* name, int unset) {
-  const char* s = std::getenv(name);
-  return s ? std::atoi(s) : unset;
-}
-
 // Polls after which a device wait gives up.  VD_WAIT_LIMIT=a or a:b lowers them,
 // for tests (a for the scored rows' copies, b for the other tensor's; 0: at once).
 void wait_limits(uint32_t* scored, uint32_t* other) {
@@ -869,6 +865,11 @@ vd_status device_info(DeviceInfo* out) {
   const vd_status r = device_state(&st);
   if (r == VD_OK) *out = {(int)(st - g_dev), st->sms, st->smem_optin, st->status};
   return r;
+}
+
+int env_int(const char* name, int unset) {
+  const char* s = std::getenv(name);
+  return s ? std::atoi(s) : unset;
 }
 
 uint32_t wait_limit() {

@@ -1,4 +1,4 @@
-// vd_host.h -- what the host sides of libvd.so share: the per-device state that
+// vd_host.cuh -- what the host sides of libvd.so share: the per-device state that
 // vd_api.cu owns and the launch of a programmatic dependent kernel.
 #pragma once
 
@@ -25,6 +25,9 @@ vd_status validate_q4(const vd_q4_cache* c);
 
 // Polls after which a device wait gives up (VD_WAIT_LIMIT lowers it, for tests).
 uint32_t wait_limit();
+
+// The environment variable's number, or `unset`.
+int env_int(const char* name, int unset);
 
 // A plain kernel of `threads`-thread blocks, in clusters of c, as a programmatic
 // dependent launch (it waits in griddepcontrol.wait before its first access to memory).

@@ -5,75 +5,80 @@
 #include <climits>
 #include <mutex>
 
-#include "vd_host.h"
+#include "vd_host.cuh"
 #include "vd_q4_attend.cuh"
+#include "vd_q4_tile.cuh"
 
 namespace vd {
 
 namespace {
 
-using AttendKernel = void (*)(AttendArgs);
-
-struct Stream {
-  AttendKernel kern;
-  int smem, rows;
+struct Kernel {
+  void (*kern)(AttendArgs);
+  int smem, rows, threads;
 };
 
 template <int M, int NT>
-constexpr Stream stream_of() {
-  return {q4_attend_kernel<M, NT>, AttendShape<M, NT>::kTotal, AttendShape<M, NT>::kRows};
+constexpr Kernel stream() {
+  return {q4_attend_kernel<M, NT>, AttendShape<M, NT>::kTotal, AttendShape<M, NT>::kRows, kThreads};
 }
 
-// [head_dim / 32 - 1][two row tiles]; two only where their sums fit the registers
-const Stream kStream[8][2] = {
-    {stream_of<1, 1>(), stream_of<1, 2>()}, {stream_of<2, 1>(), stream_of<2, 2>()},
-    {stream_of<3, 1>(), stream_of<3, 2>()}, {stream_of<4, 1>(), stream_of<4, 2>()},
-    {stream_of<5, 1>(), stream_of<5, 1>()}, {stream_of<6, 1>(), stream_of<6, 1>()},
-    {stream_of<7, 1>(), stream_of<7, 1>()}, {stream_of<8, 1>(), stream_of<8, 1>()}};
+template <int M>
+constexpr Kernel block() {
+  return {q4_tile_kernel<M>, TileShape<M>::kTotal, kTileRows, kTileThreads};
+}
+
+// [head_dim / 32 - 1][kind]: the streaming kernel with tiles of 8 and 16 rows (16 only where
+// their sums fit the registers), the block kernel
+constexpr int kKinds = 3;
+const Kernel kKernel[8][kKinds] = {
+    {stream<1, 1>(), stream<1, 2>(), block<1>()}, {stream<2, 1>(), stream<2, 2>(), block<2>()},
+    {stream<3, 1>(), stream<3, 2>(), block<3>()}, {stream<4, 1>(), stream<4, 2>(), block<4>()},
+    {stream<5, 1>(), stream<5, 1>(), block<5>()}, {stream<6, 1>(), stream<6, 1>(), block<6>()},
+    {stream<7, 1>(), stream<7, 1>(), block<7>()}, {stream<8, 1>(), stream<8, 1>(), block<8>()}};
 
 // CTAs of each kernel that run at once on the device, in clusters of 1, 2, 4, 8, 16
-// (0: such a cluster does not fit); asked for once.
+// (0: such a cluster does not fit); asked for once per device and head dim.
 struct Slots {
   bool ready;
-  int at[8][2][5];
+  int at[kKinds][5];
 };
 std::mutex g_slots_mu;
-Slots g_slots[64];
+Slots g_slots[64][8];
 
-vd_status slots_of(const DeviceInfo& dev, const Slots** out) {
+vd_status slots_of(const DeviceInfo& dev, int m, const Slots** out) {
   std::lock_guard<std::mutex> lk(g_slots_mu);
-  Slots& s = g_slots[dev.id];
+  Slots& s = g_slots[dev.id][m];
   if (!s.ready) {
-    for (int m = 0; m < 8; ++m)
-      for (int t = 0; t < 2; ++t) {
-        const Stream& k = kStream[m][t];
-        if (cudaFuncSetAttribute(k.kern, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem) !=
-                cudaSuccess ||
-            cudaFuncSetAttribute(k.kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) !=
-                cudaSuccess) {
-          cudaGetLastError();
-          return VD_ERR_CUDA;
-        }
-        for (int e = 0; e < 5; ++e) {
-          cudaLaunchConfig_t cfg = {};
-          cfg.gridDim = dim3(16 * dev.sms);
-          cfg.blockDim = dim3(kThreads);
-          cfg.dynamicSmemBytes = k.smem;
-          cudaLaunchAttribute attr;
-          attr.id = cudaLaunchAttributeClusterDimension;
-          attr.val.clusterDim.x = 1u << e;
-          attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-          cfg.attrs = &attr;
-          cfg.numAttrs = 1;
-          int n = 0;
-          if (cudaOccupancyMaxActiveClusters(&n, k.kern, &cfg) != cudaSuccess) {
-            cudaGetLastError();
-            n = 0;
-          }
-          s.at[m][t][e] = n << e;
-        }
-        if (s.at[m][t][0] < 1) return VD_ERR_CUDA;
+    for (int t = 0; t < kKinds; ++t) {
+      const Kernel& k = kKernel[m][t];
+      if (cudaFuncSetAttribute(k.kern, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem) !=
+              cudaSuccess ||
+          cudaFuncSetAttribute(k.kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) !=
+              cudaSuccess) {
+        cudaGetLastError();
+        return VD_ERR_CUDA;
       }
+      for (int e = 0; e < 5; ++e) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(16 * dev.sms);
+        cfg.blockDim = dim3(k.threads);
+        cfg.dynamicSmemBytes = k.smem;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = 1u << e;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        int n = 0;
+        if (cudaOccupancyMaxActiveClusters(&n, k.kern, &cfg) != cudaSuccess) {
+          cudaGetLastError();
+          n = 0;
+        }
+        s.at[t][e] = n << e;
+      }
+      if (s.at[t][0] < 1) return VD_ERR_CUDA;
+    }
     s.ready = true;
   }
   *out = &s;
@@ -106,13 +111,14 @@ extern "C" vd_status vd_q4_attend(const vd_q4_cache* c, int32_t layer, const voi
   DeviceInfo dev;
   r = device_info(&dev);
   if (r != VD_OK) return r;
+  const int m = c->head_dim / 32 - 1;
   const Slots* slots = nullptr;
-  r = slots_of(dev, &slots);
+  r = slots_of(dev, m, &slots);
   if (r != VD_OK) return r;
 
-  const int m = c->head_dim / 32 - 1;
-  const int two = rows > 8;
-  const Stream& k = kStream[m][two];
+  const int want = env_int("VD_Q4_KERNEL", -1);
+  const int kind = want >= 0 && want < kKinds ? want : rows > 24 ? 2 : rows > 8 ? 1 : 0;
+  const Kernel& k = kKernel[m][kind];
   AttendArgs a;
   const size_t unit0 = (size_t)layer * c->n_kv_head * c->capacity;
   const size_t new0 = (size_t)layer * c->n_kv_head * B;
@@ -140,11 +146,14 @@ extern "C" vd_status vd_q4_attend(const vd_q4_cache* c, int32_t layer, const voi
   a.wait_limit = wait_limit();
   const long long base = units * a.tiles;
   int e = 0;
-  while (e < 4 && slots->at[m][two][e + 1] > 0 && (base << (e + 1)) <= slots->at[m][two][e + 1] &&
-         c->capacity >= (kStageKeys * kWarps) << (e + 1))
+  const int least = kind == 2 ? 128 : kStageKeys * kWarps;  // tokens that a CTA is worth
+  while (e < 4 && (base << (e + 1)) <= slots->at[kind][e + 1] && c->capacity >= least << (e + 1))
     ++e;
+  const int want_cluster = env_int("VD_Q4_CLUSTER", 0);
+  for (int i = 0; i < 5; ++i)
+    if (want_cluster == 1 << i && slots->at[kind][i] > 0) e = i;
   a.cluster = 1 << e;
   if (base << e > INT_MAX) return VD_ERR_UNSUPPORTED;
-  return launch_clusters((unsigned)(base << e), kThreads, (unsigned)a.cluster, k.smem,
+  return launch_clusters((unsigned)(base << e), (unsigned)k.threads, (unsigned)a.cluster, k.smem,
                          reinterpret_cast<cudaStream_t>(stream), k.kern, a);
 }

@@ -5,7 +5,7 @@
 #include <climits>
 #include <cstdint>
 
-#include "vd_host.h"
+#include "vd_host.cuh"
 #include "vd_q4.cuh"
 
 namespace vd {

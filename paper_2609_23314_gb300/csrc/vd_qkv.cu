@@ -10,7 +10,7 @@
 #include <climits>
 #include <cstdint>
 
-#include "vd_host.h"
+#include "vd_host.cuh"
 
 namespace vd {
 

@@ -24,6 +24,13 @@ def _lib():
     assert vd.vd_get_device_status() == 0
 
 
+@pytest.fixture(params=["automatic", "streaming", "block"])
+def route(request, monkeypatch):
+    """Runs a test with the kernel that the library picks, and with each of the two."""
+    if request.param != "automatic":
+        monkeypatch.setenv("VD_Q4_KERNEL", "0" if request.param == "streaming" else "2")
+
+
 def state(lens, n_layer, n_kv, group, d, B, cap, seed=0, spread=1.0):
     """A cache whose slots behind the lengths hold random codes with NaN scales, and
     new rows and queries."""
@@ -88,18 +95,21 @@ def check(c, q, k_new, v_new, layer=0, scale=None):
 LENS = [0, 1, 7, 8, 15, 16, 17, 31, 32, 33, 64, 100]
 
 
+@pytest.mark.usefixtures("route")
 @pytest.mark.parametrize("d", [32, 64, 96, 128, 160, 192, 224, 256])
 @pytest.mark.parametrize("group,B", [(1, 1), (4, 1), (8, 1), (3, 2), (5, 3), (16, 1)])
 def test_head_dims_and_groups(d, group, B):
     check(*state(LENS, 2, 2, group, d, B, 104), layer=1)
 
 
+@pytest.mark.usefixtures("route")
 @pytest.mark.parametrize("d", [64, 96, 128, 256])
 @pytest.mark.parametrize("group,B", [(1, 17), (4, 16), (4, 40), (2, 128), (7, 31), (1, 200)])
 def test_many_new_tokens(d, group, B):
     check(*state([0, 1, 90, 300], 1, 2, group, d, B, 304))
 
 
+@pytest.mark.usefixtures("route")
 @pytest.mark.parametrize("d,group,B", [(128, 4, 1), (96, 3, 1), (64, 8, 2), (256, 2, 1),
                                        (128, 4, 32), (192, 1, 1)])
 def test_long_caches(d, group, B):
@@ -113,6 +123,7 @@ def test_many_units(n_seq, n_kv, B):
     check(*state([(37 * s) % 257 for s in range(n_seq)], 1, n_kv, 4, 64, B, 264))
 
 
+@pytest.mark.usefixtures("route")
 @pytest.mark.parametrize("d", [64, 96, 128, 256])
 @pytest.mark.parametrize("B", [1, 5, 33])
 def test_without_new_rows(d, B):
@@ -121,12 +132,14 @@ def test_without_new_rows(d, B):
     check(c, q, None, None)
 
 
+@pytest.mark.usefixtures("route")
 @pytest.mark.parametrize("spread,scale", [(30.0, 1.0), (1e-3, 1.0), (1.0, 5.0), (200.0, 0.5)])
 @pytest.mark.parametrize("B", [1, 40])
 def test_large_and_small_scores(spread, scale, B):
     check(*state([70, 130], 1, 2, 4, 128, B, 136, spread=spread), scale=scale)
 
 
+@pytest.mark.usefixtures("route")
 @pytest.mark.parametrize("factor", [1e-30, 1e-36, 1e30])
 @pytest.mark.parametrize("B", [1, 40])
 def test_queries_of_any_size(factor, B):
@@ -135,6 +148,7 @@ def test_queries_of_any_size(factor, B):
     check(c, (q.double() * factor).to(torch.bfloat16), k_new, v_new, scale=0.08 / factor)
 
 
+@pytest.mark.usefixtures("route")
 @pytest.mark.parametrize("B", [3, 40])
 @pytest.mark.parametrize("d", [96, 128])
 @pytest.mark.parametrize("value", [float("nan"), float("inf")])
@@ -187,6 +201,7 @@ def test_lengths_out_of_range_give_no_output():
             assert bool((out[1] == 9.0).all())
 
 
+@pytest.mark.usefixtures("route")
 @pytest.mark.parametrize("B,group", [(1, 4), (40, 4)])
 def test_same_call_same_bytes(B, group):
     """On the current stream, on another one, from two streams at once, captured and
@@ -210,6 +225,7 @@ def test_same_call_same_bytes(B, group):
         assert torch.equal(o, first)
 
 
+@pytest.mark.usefixtures("route")
 @pytest.mark.parametrize("B", [1, 40])
 def test_a_wait_that_gives_up(B, monkeypatch):
     """With no polls left every copy counts as late: the call returns, the status says
