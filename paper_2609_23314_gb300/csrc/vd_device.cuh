@@ -365,6 +365,14 @@ __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
   return __uint_as_float(ld_cluster_u32(addr));
 }
 
+__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(addr));
+  return v;
+}
+
 // ---------------------------------------------------------------------------
 // Block-wide helpers for a kThreads-thread CTA.  `sh` is kWarps ints of shared
 // scratch; every helper ends with a barrier so `sh` can be reused at once.

@@ -2,27 +2,24 @@
 // include/vd.h): the block kernel, for many query rows per KV head (blocks of block
 // prompt processing, prompts).
 //
-// The formula is vd_q4_attend.cuh's.  128 query rows of a KV head are one CTA's tile (a
-// row per thread of four warps and per lane of tensor memory), the tokens come in tiles
-// of KT, and the two products run on tcgen05 with Q, the weights P and both results in
-// tensor memory, so that shared memory carries K and V only:
-//   S = Q K^T   (128 x KT, K's rows along the depth)
+// The formula is vd_q4_attend.cuh's.  128 query rows of a KV head are one CTA's (a row per
+// thread of four warps and per lane of tensor memory), the tokens come in tiles of kKeys,
+// and the two products run on tcgen05 with Q, the weights P and both results in tensor
+// memory, so that shared memory carries K and V only:
+//   S = Q K^T   (128 x kKeys, K's rows along the depth)
 //   O += P V    (128 x head_dim, V's rows along the columns)
-// Roles of the ten warps, which meet only at mbarriers:
-//   0-3  a row each: maximum, weights, their sum; rescale O where the maximum has risen
-//        by more than 2^8 (a smaller rise only makes the weights exceed 1);
-//   4-7  cached codes to fp16 in the swizzled layout of the products (exact), or copies of
-//        the new tokens' bf16 rows; two buffers each for K and V;
-//   8    issues the products: S of tile i + 1 before O of tile i, so that the softmax of
-//        one tile runs beside the products of its neighbours;
-//   9    bulk copies of codes and scales into a ring.
+// Roles of the four warpgroups, which meet only at mbarriers:
+//   0  a row per thread: maximum, weights, their sum; O is rescaled where the maximum has
+//      risen by more than 2^8 (a smaller rise only makes the weights exceed 1);
+//   1  K's tiles: cached codes to fp16 in the swizzled layout of the products (exact), or
+//      copies of the new tokens' bf16 rows.  The next tile's codes are loaded from memory
+//      before this one's are unpacked;
+//   2  V's tiles, the same;
+//   3  one thread issues the products: S of tile i + 1 before O takes tile i, so that the
+//      softmax of one tile runs beside the products of its neighbours.
 // The new tokens' tiles come first, in bf16, then Q is rewritten in fp16 (rows scaled by
 // powers of two, as in the streaming kernel) for the cached ones.  A cluster splits the
 // tiles of a unit and joins the results through distributed shared memory.
-//
-// Bounds per tile of 128 tokens at head_dim 128: 2 x 2.1 M multiply-adds, 1024 cycles at
-// 4096 a cycle; 128 exponentials per thread, 512 cycles; codes to fp16 about 350 issue
-// slots per scheduler.
 #pragma once
 
 #include <cstdint>
@@ -35,33 +32,34 @@
 
 namespace vd {
 
-constexpr int kTileRows = 128;
-constexpr int kTileThreads = 320;
+constexpr int kTileRows = 128;  // rows of a block
+
+constexpr int kTileThreads = 512;
+// registers of the warpgroups' threads: 512 x 128 are launched
+constexpr int kSoftRegs = 208, kTileRegs = 104, kProductRegs = 96;
+static_assert(kSoftRegs + 2 * kTileRegs + kProductRegs <= 4 * 128, "registers");
 
 template <int M>
 struct TileShape {
   static constexpr int kD = 32 * M;
-  static constexpr int kKeys = M <= 4 ? 128 : M <= 7 ? 64 : 32;  // tensor memory: see below
-  static constexpr int kBlocks = (kD + 63) / 64;                 // 64-column blocks of a row
+  static constexpr int kKeys = M <= 4 ? 128 : 64;   // tokens of a tile
+  static constexpr int kBlocks = (kD + 63) / 64;    // 64-column blocks of a row
   static constexpr int kTileBytes = kBlocks * kKeys * 128;
-  static constexpr int kCodeBytes = kKeys * 16 * M;
-  static constexpr int kScaleBytes = kKeys * 2 * M;
-  static constexpr int kRawBytes = 2 * (kCodeBytes + kScaleBytes);
-  static constexpr int kRaw = M == 8 ? 4 : 3;  // stages of the ring
-  static constexpr int kRing = 4 * kTileBytes;
-  static constexpr int kUsed = kRing + kRaw * kRawBytes;
+  static constexpr int kBufs = 3;                   // of K and of V
+  static constexpr int kUsed = 2 * kBufs * kTileBytes;
   static constexpr int kPartBytes = kTileRows * kD * 4;
-  static constexpr int kStats = kUsed > kPartBytes ? kUsed : kPartBytes;
-  static constexpr int kBars = kStats + 2 * kTileRows * 4;
-  static constexpr int kNumBars = 2 * kRaw + 14;
+  static constexpr int kStats = kUsed > kPartBytes ? kUsed : kPartBytes;  // row maxima, sums
+  static constexpr int kFactors = kStats + 2 * kTileRows * 4;
+  static constexpr int kBars = kFactors + kTileRows * 4;
+  static constexpr int kNumBars = 4 * kBufs + 8;
   static constexpr int kMisc = kBars + kNumBars * 8;  // tensor memory address, flags
   // The base is rounded up to 1024.  Never two CTAs on an SM: the second would wait for
   // tensor memory, and the first, in one cluster with it, for the second.
   static constexpr int kNeed = kMisc + 16 + 1024;
   static constexpr int kTotal = kNeed > 120 * 1024 ? kNeed : 120 * 1024;
-  // columns of tensor memory: two S, P (16-bit pairs), O, Q (16-bit pairs)
-  static constexpr int kColP = 2 * kKeys;
-  static constexpr int kColO = (kColP + kKeys / 2 + 31) / 32 * 32;
+  // columns of tensor memory: two S, O, Q (16-bit pairs).  P (16-bit pairs) takes the lower
+  // half of its S, which has been read by then
+  static constexpr int kColO = 2 * kKeys;
   static constexpr int kColQ = kColO + kD;
   static_assert(kColQ + kD / 2 <= 512, "tensor memory");
 };
@@ -93,54 +91,151 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, unsigne
   return ok;
 }
 
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+// One arrival for a warp: 128 single ones would take the barrier's word in turn.
+__device__ __forceinline__ void warp_arrive(uint32_t bar) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0)
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+  __syncwarp();
+}
+
+// A warpgroup's part of a tile of K or V: cached codes.  32 values, 16 bytes of codes, are a
+// unit.
+template <int M>
+struct CodeTile {
+  static constexpr int kKeys = TileShape<M>::kKeys;
+  static constexpr int kUnits = (kKeys * M + 127) / 128;
+  uint4 x[kUnits];
+  uint32_t sb[kUnits];
+
+  // codes, scales: of the tile's first token; left: tokens that are there
+  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int left,
+                                       int t) {
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int j = t + 128 * u;
+      x[u] = make_uint4(0, 0, 0, 0);
+      sb[u] = 0;
+      if (j / M < min(left, kKeys)) {
+        x[u] = ld_cg16(codes + (size_t)j * 16);
+        sb[u] = __ldcg(reinterpret_cast<const uint16_t*>(scales + 2 * j));
+      }
+    }
+  }
+
+  __device__ __forceinline__ void unpack(uint32_t dst, int t) const {
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int j = t + 128 * u;
+      if (kKeys * M % 128 != 0 && j >= kKeys * M) break;
+      const int key = j / M, blk = j % M;
+      // the order of the four 16-byte stores, so that 8 neighbouring lanes meet 8 chunk
+      // positions
+      const int turn = M == 4 ? (blk & 2) : M == 8 ? (blk >> 1) & 3 : 0;
+      uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+      if (M == 8 && (turn & 1)) {
+        uint32_t y = w[0];
+        w[0] = w[1], w[1] = y;
+        y = w[2], w[2] = w[3], w[3] = y;
+      }
+      if (M % 4 == 0 && (turn & 2)) {
+        uint32_t y = w[0];
+        w[0] = w[2], w[2] = y;
+        y = w[1], w[1] = w[3], w[3] = y;
+      }
+      const uint32_t s_lo = (sb[u] & 255u) * 0x00800080u, s_hi = (sb[u] >> 8) * 0x00800080u;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int at = e ^ turn;  // 8-value chunk of the 32
+        const uint32_t sc = at < 2 ? s_lo : s_hi;
+        uint32_t h[4];
+        q4_unpack4(w[e], h);
+        const int chunk = 4 * blk + at;
+        st_shared16(dst + (chunk >> 3) * (kKeys * 128) + key * 128 +
+                        (((chunk & 7) ^ (key & 7)) << 4),
+                    make_uint4(h2_mul(h[0], sc), h2_mul(h[1], sc), h2_mul(h[2], sc),
+                               h2_mul(h[3], sc)));
+      }
+    }
+  }
+};
+
+// The same for new tokens: bf16 rows as they are, zeros behind the last one (left: rows that
+// are there).  FINITE: what is not finite becomes zero too; returns whether there was any.
+template <int M, bool FINITE>
+__device__ __forceinline__ bool copy_rows(const uint16_t* src, int left, uint32_t dst, int t) {
+  constexpr int kD = 32 * M, kKeys = TileShape<M>::kKeys;
+  constexpr int kChunks = kKeys * (kD / 8) / 128;  // 16 bytes each, of a thread
+  bool found = false;
+#pragma unroll 1
+  for (int u0 = 0; u0 < kChunks; u0 += 4) {
+    uint4 x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int j = t + 128 * (u0 + u), key = j / (kD / 8), chunk = j % (kD / 8);
+      x[u] = make_uint4(0, 0, 0, 0);
+      if (u0 + u < kChunks && key < left) x[u] = ld_cg16(src + (size_t)key * kD + 8 * chunk);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (u0 + u >= kChunks) break;
+      const int j = t + 128 * (u0 + u), key = j / (kD / 8), chunk = j % (kD / 8);
+      if (FINITE) {
+        uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if ((w[e] & 0x7f80u) == 0x7f80u) w[e] &= 0xffff0000u, found = true;
+          if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] &= 0xffffu, found = true;
+        }
+        x[u] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+      st_shared16(dst + (chunk >> 3) * (kKeys * 128) + key * 128 +
+                      (((chunk & 7) ^ (key & 7)) << 4), x[u]);
+    }
+  }
+  return found;
 }
 
 template <int M>
 __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) {
   using Sh = TileShape<M>;
-  constexpr int kD = Sh::kD, kKeys = Sh::kKeys;
+  constexpr int kD = Sh::kD, kKeys = Sh::kKeys, kBufs = Sh::kBufs;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw_base = smem_addr(smem_raw);
   const uint32_t base = (raw_base + 1023u) & ~1023u;
   unsigned char* smem = smem_raw + (base - raw_base);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5, role = threadIdx.x >> 7;
   const unsigned rank = blockIdx.x % a.cluster;
   const unsigned item = blockIdx.x / a.cluster;
   const int tile = item % a.tiles;
   const unsigned unit = item / a.tiles;
   const int seq = unit / a.heads, head = unit % a.heads;
 
+  // of the buffers of K and V: filled, and free again; of the two S: scores there, weights
+  // there, added to O; Q written; all products complete
   const uint32_t bars = base + Sh::kBars;
-  const uint32_t raw_full = bars, raw_empty = bars + 8 * Sh::kRaw;
-  const uint32_t k_full = raw_empty + 8 * Sh::kRaw, k_empty = k_full + 16;
-  const uint32_t v_full = k_empty + 16, v_empty = v_full + 16, s_full = v_empty + 16;
-  const uint32_t p_full = s_full + 16, pv_done = p_full + 8, q_full = pv_done + 8;
-  const uint32_t drain = q_full + 8;
+  const uint32_t full = bars, freed = full + 16 * kBufs;  // K's, then V's
+  const uint32_t s_done = freed + 16 * kBufs, p_full = s_done + 16, o_done = p_full + 16;
+  const uint32_t q_full = o_done + 16, drain = q_full + 8;
   volatile int* dead = reinterpret_cast<volatile int*>(smem + Sh::kMisc + 4);
   volatile int* odd = dead + 1;  // a new row of V holds a value that is not finite
   if (threadIdx.x == 0) {
-    for (int i = 0; i < Sh::kRaw; ++i) {
-      mbar_init(raw_full + 8 * i, 1);
-      mbar_init(raw_empty + 8 * i, 128);
+    for (int i = 0; i < 2 * kBufs; ++i) {
+      mbar_init(full + 8 * i, 4);
+      mbar_init(freed + 8 * i, 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(k_full + 8 * i, 128);
-      mbar_init(k_empty + 8 * i, 1);
-      mbar_init(v_full + 8 * i, 128);
-      mbar_init(v_empty + 8 * i, 1);
-      mbar_init(s_full + 8 * i, 1);
+      mbar_init(s_done + 8 * i, 1);
+      mbar_init(p_full + 8 * i, 4);
+      mbar_init(o_done + 8 * i, 1);
     }
-    mbar_init(p_full, 128);
-    mbar_init(pv_done, 1);
-    mbar_init(q_full, 128);
+    mbar_init(q_full, 4);
     mbar_init(drain, 1);
     fence_mbar_init();
     *dead = 0;
     *odd = 0;
   }
-  if (warp == 8) tmem_alloc(base + Sh::kMisc);
+  if (warp == 12) tmem_alloc(base + Sh::kMisc);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -163,315 +258,226 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
   const int cached0 = t0 + fresh - tiles_new;  // its first cached tile
   const size_t new_row = (size_t)seq * a.seq_new_rows + (size_t)head * a.B;
 
-  float row_max = -INFINITY, row_sum = 0.f;  // the softmax warps': in log2 units
-  if (warp < 4) {
-    const uint32_t lanes = tm + ((uint32_t)warp << 21);  // this warp's 32 lanes
-    const int row = row0 + (int)threadIdx.x;
-    const bool valid = row < a.rows;
-    const int token = min(row, a.rows - 1) / a.group;
-    const uint16_t* q = a.q + ((((size_t)seq * a.B + token) * a.heads + head) * a.group +
-                               row % a.group) * kD;
-    // Q: scaled so that the row's largest value lies in [1, 2), for bf16, or in [2^13, 2^14)
-    uint32_t top = 0;
-    if (count > 0 && valid)
-#pragma unroll 4
-      for (int i = 0; i < kD / 8; ++i) {
-        const uint4 x = ld_cg16(q + 8 * i);
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  const int row = row0 + (int)threadIdx.x;                   // of the softmax threads
+  const uint32_t lanes = tm + ((uint32_t)(warp & 3) << 21);  // their warp's 32 lanes
+  const int token = min(row, a.rows - 1) / a.group;
+  float row_max = -INFINITY, row_sum = 0.f;  // in log2 units
+  if (role == 0) {
+    regs_take<kSoftRegs>();
+    if (count > 0) {
+      const uint32_t q_col = lanes + Sh::kColQ;
+      // Q: scaled so that the row's largest value lies in [1, 2), for bf16, or in [2^13, 2^14)
+      float unit_scale;
+      {
+        const uint16_t* q = a.q + ((((size_t)seq * a.B + token) * a.heads + head) * a.group +
+                                   row % a.group) * kD;
+        uint32_t w[16 * M];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7fffu, (w[e] >> 16) & 0x7fffu));
-      }
-    const uint32_t ex = top ? min(253u, max(1u, top >> 7)) : 127u;
-    const float up = __uint_as_float((254 - ex) << 23);
-    const float unit = __uint_as_float(ex << 23) * (a.scale * kLog2e);
-    auto write_q = [&](bool bf16) {
-      const float f = bf16 ? 1.f : 0x1p13f;
-#pragma unroll 1
-      for (int i = 0; i < M; ++i) {
-        uint32_t w[16];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int i = 0; i < 4 * M; ++i) {
           uint4 x = make_uint4(0, 0, 0, 0);
-          if (valid) x = ld_cg16(q + 32 * i + 8 * j);
-          w[4 * j] = x.x, w[4 * j + 1] = x.y, w[4 * j + 2] = x.z, w[4 * j + 3] = x.w;
+          if (row < a.rows) x = ld_cg16(q + 8 * i);
+          w[4 * i] = x.x, w[4 * i + 1] = x.y, w[4 * i + 2] = x.z, w[4 * i + 3] = x.w;
         }
+        uint32_t top = 0;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const float lo = __uint_as_float(w[j] << 16) * up * f;
-          const float hi = __uint_as_float(w[j] & 0xffff0000u) * up * f;
-          w[j] = bf16 ? pack_bf16(lo, hi) : pack_f16(lo, hi);
+        for (int i = 0; i < 16 * M; ++i)
+          top = max(top, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
+        const uint32_t ex = top ? min(253u, max(1u, top >> 7)) : 127u;
+        const uint32_t up = ((254 - ex) << 7) * 0x00010001u;
+        unit_scale = __uint_as_float(ex << 23) * (a.scale * kLog2e);
+#pragma unroll
+        for (int i = 0; i < 16 * M; ++i) {
+          asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(w[i]) : "r"(up));
+          if (fresh == 0)
+            w[i] = pack_f16(__uint_as_float(w[i] << 16) * 0x1p13f,
+                            __uint_as_float(w[i] & 0xffff0000u) * 0x1p13f);
         }
         __syncwarp();
-        tmem_st16(lanes + Sh::kColQ + 16 * i, w);
+#pragma unroll
+        for (int i = 0; i < M; ++i) tmem_st16(q_col + 16 * i, w + 16 * i);
+        tmem_wait_st();
+        tc_fence_before();
+        warp_arrive(q_full);
       }
-      tmem_wait_st();
-      tc_fence_before();
-      mbar_arrive(q_full);
-    };
-    __syncwarp();
-    if (count > 0) write_q(fresh > 0);
-    for (int i = 0; i < count; ++i) {
-      const uint32_t s_col = lanes + (i & 1) * kKeys;
-      if (!warp_wait(s_full + 8 * (i & 1), (i >> 1) & 1, a.status, kWaitLimit, dead))
-        break;
-      tc_fence_after();
-      if (i == fresh - 1 && fresh < count) write_q(false);  // the last product of the bf16 form
-      const bool is_new = i < fresh;
-      // not 0, which would make a masked score a NaN
-      const float c = fmaxf(is_new ? unit : unit * 0x1p-13f, 0x1p-126f);
-      // tokens behind this row's last one do not count
-      const int seen = is_new ? token - (t0 + i) * kKeys
-                              : n - 1 - (cached0 + i - fresh) * kKeys;
-      const bool edge = __any_sync(kFull, seen < kKeys - 1);
-      // Half the columns at a time, the first half read once more for its weights: all of
-      // them at once would not fit the registers
-      constexpr int kPart = kKeys == 128 ? 64 : kKeys;
-      uint32_t s[kPart];
-      auto load = [&](int from) {
-        tmem_ld(s_col + from, s);
-        if (edge) {
-#pragma unroll
-          for (int j = 0; j < kPart; ++j)
-            if (from + j > seen) s[j] = 0xff800000u;
-        }
-      };
-      float m = -INFINITY;
-#pragma unroll
-      for (int from = 0; from < kKeys; from += kPart) {
-        load(from);
-#pragma unroll
-        for (int j = 0; j < kPart; ++j) m = fmaxf(m, __uint_as_float(s[j]));
-      }
-      m *= c;
-      bool waited = false;
-      // the weights stay below 2^8, and a row's first scores set its maximum
-      if (__any_sync(kFull, m > row_max + 8.f)) {
-        const float up_to = fmaxf(row_max, m);
-        const float f = up_to == -INFINITY ? 1.f : exp2_approx(row_max - up_to);
-        row_max = up_to;
-        row_sum *= f;
-        if (i > 0) {
-          waited = true;
-          if (!warp_wait(pv_done, (i - 1) & 1, a.status, kWaitLimit, dead))
-            break;
-          tc_fence_after();
+      for (int i = 0; i < count; ++i) {
+        const int b = i & 1;
+        const uint32_t s_col = lanes + b * kKeys;
+        if (!warp_wait(s_done + 8 * b, (i >> 1) & 1, a.status, a.wait_limit, dead)) break;
+        tc_fence_after();
+        if (i == fresh - 1 && fresh < count) {  // the last product with Q in bf16
 #pragma unroll 1
-          for (int j = 0; j < kD; j += 32) {
-            uint32_t o[32];
-            tmem_ld(lanes + Sh::kColO + j, o);
+          for (int j = 0; j < M; ++j) {
+            uint32_t w[16];
+            tmem_ld(q_col + 16 * j, w);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-            tmem_st32(lanes + Sh::kColO + j, o);
+            for (int e = 0; e < 16; ++e)
+              w[e] = pack_f16(__uint_as_float(w[e] << 16) * 0x1p13f,
+                              __uint_as_float(w[e] & 0xffff0000u) * 0x1p13f);
+            tmem_st16(q_col + 16 * j, w);
+          }
+          tmem_wait_st();
+          tc_fence_before();
+          warp_arrive(q_full);
+        }
+        const bool is_new = i < fresh;
+        // not 0, which would make a masked score a NaN
+        const float c = fmaxf(is_new ? unit_scale : unit_scale * 0x1p-13f, 0x1p-126f);
+        uint32_t s[kKeys];
+        tmem_ld2(s_col, s);
+        // tokens behind this row's last one do not count
+        const int seen = is_new ? token - (t0 + i) * kKeys
+                                : n - 1 - (cached0 + i - fresh) * kKeys;
+        if (__any_sync(kFull, seen < kKeys - 1)) {
+#pragma unroll
+          for (int j = 0; j < kKeys; ++j)
+            if (j > seen) s[j] = 0xff800000u;
+        }
+        float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int j = 0; j < kKeys; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(s[j]));
+        const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * c;
+        // the weights stay below 2^8, and a row's first scores set its maximum
+        if (__any_sync(kFull, m > row_max + 8.f)) {
+          const float top = fmaxf(row_max, m);
+          const float f = top == -INFINITY ? 1.f : exp2_approx(row_max - top);
+          row_max = top;
+          row_sum *= f;
+          if (i > 0) {
+            if (!warp_wait(o_done + 8 * (b ^ 1), ((i - 1) >> 1) & 1, a.status, a.wait_limit, dead))
+              break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int j = 0; j < kD; j += 32) {
+              uint32_t o[32];
+              tmem_ld(lanes + Sh::kColO + j, o);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+              tmem_st32(lanes + Sh::kColO + j, o);
+            }
           }
         }
-      }
-      const float shift = row_max == -INFINITY ? 0.f : -row_max;
-      const unsigned long long c2 = f2_pack(c, c), shift2 = f2_pack(shift, shift);
-      unsigned long long sum2 = 0;
+        const float shift = row_max == -INFINITY ? 0.f : -row_max;
+        const unsigned long long c2 = f2_pack(c, c), shift2 = f2_pack(shift, shift);
+        unsigned long long sum2[2] = {0, 0};
 #pragma unroll
-      for (int from = kKeys - kPart; from >= 0; from -= kPart) {
-        if (from < kKeys - kPart) load(from);
-#pragma unroll
-        for (int j = 0; j < kPart; j += 2) {
+        for (int j = 0; j < kKeys; j += 2) {
           float lo, hi;
           f2_unpack(f2_fma(f2_pack(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), c2, shift2),
                     lo, hi);
           lo = exp2_approx(lo);
           hi = exp2_approx(hi);
-          sum2 = f2_add(sum2, f2_pack(lo, hi));
+          sum2[(j >> 1) & 1] = f2_add(sum2[(j >> 1) & 1], f2_pack(lo, hi));
           s[j / 2] = is_new ? pack_bf16(lo, hi) : pack_f16(lo, hi);
+          if (j % 32 == 30) tmem_st16(s_col + (j - 30) / 2, s + (j - 30) / 2);
         }
-        if (from == kKeys - kPart && i > 0 && !waited) {
-          waited = warp_wait(pv_done, (i - 1) & 1, a.status, kWaitLimit, dead);
-          if (!waited) break;
-          tc_fence_after();
-        }
-#pragma unroll
-        for (int j = 0; j < kPart / 2; j += 16) tmem_st16(lanes + Sh::kColP + from / 2 + j, s + j);
+        tmem_wait_st();
+        tc_fence_before();
+        warp_arrive(p_full + 8 * b);
+        row_sum += f2_hsum(f2_add(sum2[0], sum2[1]));
       }
-      if (i > 0 && !waited) break;
-      row_sum += f2_hsum(sum2);
-      tmem_wait_st();
-      tc_fence_before();
-      mbar_arrive(p_full);
+      if (warp_wait(o_done + 8 * ((count - 1) & 1), ((count - 1) >> 1) & 1, a.status, a.wait_limit,
+                    dead))
+        tc_fence_after();
     }
-    if (count > 0 && warp_wait(pv_done, (count - 1) & 1, a.status, kWaitLimit, dead))
-      tc_fence_after();
-  } else if (warp < 8) {
-    const int t = threadIdx.x - 128;
+    __syncwarp();
+    regs_give<128>();
+  } else if (role < 3) {
+    regs_give<kTileRegs>();
+    const int t = threadIdx.x & 127, part = role - 1;  // 0: K, 1: V
+    const size_t at = ((size_t)seq * a.seq_rows + (size_t)head * a.cap + (size_t)cached0 * kKeys);
+    const uint8_t* codes = (part ? a.v : a.k) + at * (kD / 2);
+    const uint8_t* scales = (part ? a.vs : a.ks) + at * (kD / 16);
+    const uint16_t* fresh_rows = (part ? a.v_new : a.k_new) + (new_row + (size_t)t0 * kKeys) * kD;
+    int left = n - cached0 * kKeys;  // cached tokens from the next tile to load on
+    CodeTile<M> next;
+    if (fresh < count) next.load(codes, scales, left, t);
     for (int i = 0; i < count; ++i) {
-      const int b = i & 1;
-      const uint32_t again = (i >> 1) + 1;  // parity of the release before: b's (i >> 1)-th
-      const uint32_t kt = base + b * Sh::kTileBytes, vt = kt + 2 * Sh::kTileBytes;
-      if (i < fresh) {  // copies of the new rows; what is behind the last one is zero
-        const int key0 = (t0 + i) * kKeys;
-        for (int part = 0; part < 2; ++part) {
-          const uint16_t* src = (part ? a.v_new : a.k_new) + (new_row + key0) * kD;
-          const uint32_t dst = part ? vt : kt;
-          if (i > 1 && !warp_wait((part ? v_empty : k_empty) + 8 * b, again & 1, a.status,
-                                  kWaitLimit, dead))
-            break;
-#pragma unroll 4
-          for (int j = t; j < kKeys * (kD / 8); j += 128) {
-            const int key = j / (kD / 8), chunk = j % (kD / 8);
-            uint4 x = make_uint4(0, 0, 0, 0);
-            if (key0 + key < keys_new) x = ld_cg16(src + (size_t)key * kD + 8 * chunk);
-            if (part) {  // a value that is not finite is added at the end, to those that see it
-              uint32_t w[4] = {x.x, x.y, x.z, x.w};
-              bool found = false;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                if ((w[e] & 0x7f80u) == 0x7f80u) w[e] &= 0xffff0000u, found = true;
-                if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] &= 0xffffu, found = true;
-              }
-              if (found) *odd = 1;
-              x = make_uint4(w[0], w[1], w[2], w[3]);
-            }
-            st_shared16(dst + (chunk >> 3) * (kKeys * 128) + key * 128 +
-                            (((chunk & 7) ^ (key & 7)) << 4), x);
-          }
-          fence_proxy_async_smem();
-          mbar_arrive((part ? v_full : k_full) + 8 * b);
-        }
-        if (*dead) break;
-        continue;
-      }
-      const int ci = i - fresh, slot = ci % Sh::kRaw;
-      const int left = n - (cached0 + ci) * kKeys;  // cached tokens of the tile
-      const uint32_t raw = base + Sh::kRing + slot * Sh::kRawBytes;
-      if (!warp_wait(raw_full + 8 * slot, (ci / Sh::kRaw) & 1, a.status, a.wait_limit, dead))
+      const int b = part * kBufs + i % kBufs;
+      const uint32_t dst = base + b * Sh::kTileBytes;
+      if (i >= kBufs &&
+          !warp_wait(freed + 8 * b, (i / kBufs + 1) & 1, a.status, a.wait_limit, dead))
         break;
-      bool gone = false;
-      for (int part = 0; part < 2; ++part) {
-        const uint32_t codes = raw + part * Sh::kCodeBytes;
-        const uint32_t scales = raw + 2 * Sh::kCodeBytes + part * Sh::kScaleBytes;
-        const uint32_t dst = part ? vt : kt;
-        if (i > 1 && !warp_wait((part ? v_empty : k_empty) + 8 * b, again & 1, a.status,
-                                kWaitLimit, dead)) {
-          gone = true;
-          break;
+      if (i < fresh) {
+        const uint16_t* src = fresh_rows + (size_t)i * kKeys * kD;
+        const int there = keys_new - (t0 + i) * kKeys;
+        if (part) {  // what is not finite is added at the end, to the rows that see it
+          if (copy_rows<M, true>(src, there, dst, t)) *odd = 1;
+        } else {
+          copy_rows<M, false>(src, there, dst, t);
         }
-#pragma unroll 4
-        for (int j = t; j < kKeys * M; j += 128) {  // 32 values: 16 bytes of codes
-          const int key = j / M, blk = j % M;
-          uint4 x = ld_shared16(codes + j * 16);
-          uint32_t sb = ld_shared_u16(scales + 2 * j);
-          if (key >= left) x = make_uint4(0, 0, 0, 0), sb = 0;  // whatever lies there
-          // the order of the four 16-byte stores, so that 8 neighbouring lanes meet 8
-          // chunk positions
-          const int turn = M == 4 ? (blk & 2) : M == 8 ? (blk >> 1) & 3 : 0;
-          uint32_t w[4] = {x.x, x.y, x.z, x.w};
-          if (M % 4 == 0) {
-            if (turn & 1) {
-              uint32_t u = w[0]; w[0] = w[1]; w[1] = u;
-              u = w[2]; w[2] = w[3]; w[3] = u;
-            }
-            if (turn & 2) {
-              uint32_t u = w[0]; w[0] = w[2]; w[2] = u;
-              u = w[1]; w[1] = w[3]; w[3] = u;
-            }
-          }
-          const uint32_t s_lo = (sb & 255u) * 0x00800080u, s_hi = (sb >> 8) * 0x00800080u;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int at = e ^ turn;  // 8-value chunk of the 32
-            const uint32_t sc = at < 2 ? s_lo : s_hi;
-            uint32_t h[4];
-            q4_unpack4(w[e], h);
-            const int chunk = 4 * blk + at;
-            st_shared16(dst + (chunk >> 3) * (kKeys * 128) + key * 128 +
-                            (((chunk & 7) ^ (key & 7)) << 4),
-                        make_uint4(h2_mul(h[0], sc), h2_mul(h[1], sc), h2_mul(h[2], sc),
-                                   h2_mul(h[3], sc)));
-          }
-        }
-        fence_proxy_async_smem();
-        mbar_arrive((part ? v_full : k_full) + 8 * b);
+      } else {
+        const CodeTile<M> now = next;
+        codes += kKeys * (kD / 2);
+        scales += kKeys * (kD / 16);
+        left -= kKeys;
+        if (i + 1 < count) next.load(codes, scales, left, t);
+        now.unpack(dst, t);
       }
-      if (gone) break;
-      mbar_arrive(raw_empty + 8 * slot);
+      fence_proxy_async_smem();
+      warp_arrive(full + 8 * b);
     }
-  } else if (warp == 8) {
-    if (lane == 0) {
+  } else {
+    regs_give<kProductRegs>();
+    if (threadIdx.x == 384) {
       constexpr uint32_t kLead = kKeys * 128;
-      auto values = [&](int i) {  // O += P V of tile i
-        const bool bf16 = i < fresh;
-        const uint32_t desc = bf16 ? tc_desc(true, true, kD) : tc_desc(false, true, kD);
-        const uint32_t vt = base + (2 + (i & 1)) * Sh::kTileBytes;
-        if (!tile_wait(p_full, i & 1, a.status, kWaitLimit, dead) ||
-            !tile_wait(v_full + 8 * (i & 1), (i >> 1) & 1, a.status, kWaitLimit, dead))
-          return false;
-        tc_fence_after();
-#pragma unroll
-        for (int k = 0; k < kKeys / 16; ++k)
-          tc_mma(tm + Sh::kColO, tm + Sh::kColP + 8 * k, tc_smem(vt + 2048 * k, kLead), desc,
-                 i > 0 || k > 0);
-        tc_commit(v_empty + 8 * (i & 1));
-        tc_commit(pv_done);
-        return true;
-      };
       bool ok = true;
-      for (int i = 0; ok && i < count; ++i) {
-        const bool bf16 = i < fresh;
-        const uint32_t desc = bf16 ? tc_desc(true, false, kKeys) : tc_desc(false, false, kKeys);
-        const uint32_t kt = base + (i & 1) * Sh::kTileBytes;
-        if (i == 0) ok = tile_wait(q_full, 0, a.status, kWaitLimit, dead);
-        if (i == fresh && i > 0) ok = tile_wait(q_full, 1, a.status, kWaitLimit, dead);
-        ok = ok && tile_wait(k_full + 8 * (i & 1), (i >> 1) & 1, a.status, kWaitLimit, dead);
-        if (!ok) break;
+      auto await = [&](uint32_t bar, uint32_t parity) {
+        ok = ok && tile_wait(bar, parity, a.status, a.wait_limit, dead);
+      };
+      auto scores = [&](int i) {
+        if (i == 0) await(q_full, 0);
+        if (i == fresh && i > 0) await(q_full, 1);
+        await(full + 8 * (i % kBufs), (i / kBufs) & 1);
+        if (!ok) return;
         tc_fence_after();
+        const uint32_t desc = i < fresh ? tc_desc(true, false, kKeys) : tc_desc(false, false, kKeys);
+        const uint64_t kt = tc_smem(base + (i % kBufs) * Sh::kTileBytes, kLead);
+        const uint32_t s_col = tm + (i & 1) * kKeys;
 #pragma unroll
         for (int k = 0; k < kD / 16; ++k)
-          tc_mma(tm + (i & 1) * kKeys, tm + Sh::kColQ + 8 * k,
-                 tc_smem(kt + (k >> 2) * kLead + (k & 3) * 32, kLead), desc, k > 0);
-        tc_commit(k_empty + 8 * (i & 1));
-        tc_commit(s_full + 8 * (i & 1));
-        if (i > 0) ok = values(i - 1);
+          tc_mma(s_col, tm + Sh::kColQ + 8 * k, kt + (((k >> 2) * kLead + (k & 3) * 32) >> 4), desc,
+                 k > 0);
+        tc_commit(s_done + 8 * (i & 1));
+        tc_commit(freed + 8 * (i % kBufs));
+      };
+      auto values = [&](int i) {
+        await(full + 8 * (kBufs + i % kBufs), (i / kBufs) & 1);
+        await(p_full + 8 * (i & 1), (i >> 1) & 1);
+        if (!ok) return;
+        tc_fence_after();
+        const uint32_t desc = i < fresh ? tc_desc(true, true, kD) : tc_desc(false, true, kD);
+        const uint64_t vt = tc_smem(base + (kBufs + i % kBufs) * Sh::kTileBytes, kLead);
+        const uint32_t p_col = tm + (i & 1) * kKeys;
+#pragma unroll
+        for (int k = 0; k < kKeys / 16; ++k)
+          tc_mma(tm + Sh::kColO, p_col + 8 * k, vt + ((2048 * k) >> 4), desc, i > 0 || k > 0);
+        tc_commit(o_done + 8 * (i & 1));
+        tc_commit(freed + 8 * (kBufs + i % kBufs));
+      };
+      // Products run in the order of their issue: S of tile i + 2 may take the place of the
+      // weights of tile i, whose product was issued before.
+      if (count > 0) scores(0);
+      for (int i = 0; i < count && ok; ++i) {
+        if (i + 1 < count) scores(i + 1);
+        values(i);
       }
-      if (ok && count > 0) values(count - 1);
+      // every product that was issued is complete before the memory is used again
+      if (count > 0) {
+        tc_commit(drain);
+        mbar_wait(drain, 0, a.status, kWaitLimit);
+      }
     }
     __syncwarp();
-  } else {
-    if (lane == 0) {
-      const size_t unit_row = (size_t)seq * a.seq_rows + (size_t)head * a.cap;
-      const int cached = count - fresh;
-      int issued = 0;
-      for (; issued < cached; ++issued) {
-        const int slot = issued % Sh::kRaw;
-        if (issued >= Sh::kRaw && !tile_wait(raw_empty + 8 * slot, (issued / Sh::kRaw + 1) & 1,
-                                             a.status, kWaitLimit, dead))
-          break;
-        const size_t key0 = (size_t)(cached0 + issued) * kKeys;
-        const int keys = min(kKeys, n - (int)key0);
-        const uint32_t codes = (uint32_t)keys * (kD / 2);
-        const uint32_t scales = (uint32_t)((keys + 7) & ~7) * (kD / 16);  // within the capacity
-        const uint32_t dst = base + Sh::kRing + slot * Sh::kRawBytes, bar = raw_full + 8 * slot;
-        fence_proxy_async_smem();
-        mbar_expect_tx(bar, 2 * (codes + scales));
-        bulk_g2s(dst, a.k + (unit_row + key0) * (kD / 2), codes, bar);
-        bulk_g2s(dst + Sh::kCodeBytes, a.v + (unit_row + key0) * (kD / 2), codes, bar);
-        bulk_g2s(dst + 2 * Sh::kCodeBytes, a.ks + (unit_row + key0) * (kD / 16), scales, bar);
-        bulk_g2s(dst + 2 * Sh::kCodeBytes + Sh::kScaleBytes, a.vs + (unit_row + key0) * (kD / 16),
-                 scales, bar);
-      }
-      // nothing may be in flight when the ring's memory is used again
-      for (int i = max(0, issued - Sh::kRaw); i < issued; ++i)
-        mbar_wait(raw_full + 8 * (i % Sh::kRaw), (i / Sh::kRaw) & 1, a.status, kWaitLimit);
-    }
-    __syncwarp();
-  }
-  // every product that was issued is complete before the memory is used again
-  if (warp == 8 && lane == 0 && count > 0) {
-    tc_commit(drain);
-    mbar_wait(drain, 0, a.status, kWaitLimit);
   }
   __syncthreads();
 
+  // What follows runs on all warps: everyone to the launch's share again.  Behind the barrier:
+  // a warp that took registers before the softmax warps had taken and given theirs would
+  // leave them waiting.
+  if (role > 0) regs_take<128>();
+
   const bool none = n == 0 && !a.k_new;  // no token to attend to
   if (warp < 4) {
-    const uint32_t lanes = tm + ((uint32_t)warp << 21);
-    const int row = row0 + (int)threadIdx.x;
-    const int token = min(row, a.rows - 1) / a.group;
     const bool valid = row < a.rows && !bad_len;
     const size_t at = (((size_t)seq * a.B + token) * a.heads + head) * a.group + row % a.group;
     const float inv = none ? 0.f : 1.f / row_sum;
@@ -497,6 +503,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
             if ((x & 0x7f80u) == 0x7f80u)
               o[e] = __float_as_uint(__uint_as_float(o[e]) + __uint_as_float((uint32_t)x << 16));
           }
+        __syncwarp();
       }
       if (a.cluster == 1) {
         if (valid)
@@ -509,6 +516,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
                                __uint_as_float(o[e + 2 * f + 1]) * inv);
             st16(a.out + at * kD + j + e, make_uint4(w[0], w[1], w[2], w[3]));
           }
+        __syncwarp();
       } else {  // [dim / 4][row][4]
 #pragma unroll
         for (int e = 0; e < 32; e += 4)
@@ -522,39 +530,64 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
     cluster_sync();
   else
     __syncthreads();
-  if (warp == 8) {
+  if (warp == 12) {
     tc_fence_after();
     tmem_free(tm);
   }
   if (a.cluster == 1) return;
-  // each CTA writes its share of the rows, from all CTAs' results in rank order
-  const int share = kTileRows / a.cluster;
-  const uint32_t stats = base + Sh::kStats;
-  for (int i = threadIdx.x; i < share * (kD / 4) && !bad_len; i += kTileThreads) {
-    const int r = (int)rank * share + i % share, dim4 = i / share;
-    const int row = row0 + r;
-    if (row >= a.rows) continue;
-    float m = -INFINITY;
-    for (int q = 0; q < a.cluster; ++q) m = fmaxf(m, ld_cluster_f32(mapa(stats + 4 * r, q)));
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
-    for (int q = 0; q < a.cluster; ++q) {
-      const float mq = ld_cluster_f32(mapa(stats + 4 * r, q));
-      // a CTA without tokens has sums of zero; one whose scores were all NaN has NaN sums
-      const float f = mq == -INFINITY ? 1.f : exp2_approx(mq - m);
-      const uint32_t x = mapa(base + (dim4 * kTileRows + r) * 16, q);
-      acc.x = fmaf(ld_cluster_f32(x), f, acc.x);
-      acc.y = fmaf(ld_cluster_f32(x + 4), f, acc.y);
-      acc.z = fmaf(ld_cluster_f32(x + 8), f, acc.z);
-      acc.w = fmaf(ld_cluster_f32(x + 12), f, acc.w);
-      l = fmaf(ld_cluster_f32(mapa(stats + 4 * (kTileRows + r), q)), f, l);
-    }
-    const size_t at =
-        (((size_t)seq * a.B + row / a.group) * a.heads + head) * a.group + row % a.group;
+  // Each CTA writes its share of the rows (those that are there), from all CTAs' results in
+  // rank order: first every CTA's factor for every row of the share, then the sums.
+  const int rows = min(kTileRows, a.rows - row0);
+  const int share = (rows + a.cluster - 1) / a.cluster;
+  const int r0 = (int)rank * share, mine = bad_len ? 0 : max(0, min(share, rows - r0));
+  const uint32_t stats = base + Sh::kStats, factors = base + Sh::kFactors;
+  float* factor = reinterpret_cast<float*>(smem + Sh::kFactors);  // [cluster][share]
+  for (int r = threadIdx.x; r < mine; r += kTileThreads) {
+    float mx[16], l = 0.f, m = -INFINITY;
+#pragma unroll
+    for (int q = 0; q < 16; ++q)
+      mx[q] = q < a.cluster ? ld_cluster_f32(mapa(stats + 4 * (r0 + r), q)) : -INFINITY;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) m = fmaxf(m, mx[q]);
+#pragma unroll
+    for (int q = 0; q < 16; ++q)
+      if (q < a.cluster) {
+        // a CTA without tokens has sums of zero; one whose scores were all NaN has NaN sums
+        mx[q] = mx[q] == -INFINITY ? 1.f : exp2_approx(mx[q] - m);
+        l = fmaf(ld_cluster_f32(mapa(stats + 4 * (kTileRows + r0 + r), q)), mx[q], l);
+      }
     const float inv = none ? 0.f : 1.f / l;
+#pragma unroll
+    for (int q = 0; q < 16; ++q)
+      if (q < a.cluster) factor[q * share + r] = mx[q] * inv;
+    const int gr = row0 + r0 + r;
+    if (a.lse)
+      a.lse[(((size_t)seq * a.B + gr / a.group) * a.heads + head) * a.group + gr % a.group] =
+          none ? -INFINITY : m / kLog2e + logf(l);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < mine * (kD / 4); i += kTileThreads) {
+    const int r = i % mine, dim4 = i / mine;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int q0 = 0; q0 < a.cluster; q0 += 2) {  // the cluster is even
+      float4 x[2];
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+        x[q] = ld_cluster_f32x4(mapa(base + (dim4 * kTileRows + r0 + r) * 16, q0 + q));
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const float f = ld_shared_f32(factors + 4 * ((q0 + q) * share + r));
+        acc.x = fmaf(x[q].x, f, acc.x);
+        acc.y = fmaf(x[q].y, f, acc.y);
+        acc.z = fmaf(x[q].z, f, acc.z);
+        acc.w = fmaf(x[q].w, f, acc.w);
+      }
+    }
+    const int gr = row0 + r0 + r;
+    const size_t at =
+        (((size_t)seq * a.B + gr / a.group) * a.heads + head) * a.group + gr % a.group;
     *reinterpret_cast<uint2*>(a.out + at * kD + 4 * dim4) =
-        make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-    if (dim4 == 0 && a.lse) a.lse[at] = none ? -INFINITY : m / kLog2e + logf(l);
+        make_uint2(pack_bf16(acc.x, acc.y), pack_bf16(acc.z, acc.w));
   }
   cluster_sync();  // no CTA leaves while its results are read
 }
