@@ -43,6 +43,8 @@ template <int M>
 struct TileShape {
   static constexpr int kD = 32 * M;
   static constexpr int kKeys = M <= 4 ? 128 : 64;   // tokens of a tile
+  // whether the softmax threads need more registers than their share of the launch's
+  static constexpr bool kShare = kKeys == 128 || M == 8;
   static constexpr int kBlocks = (kD + 63) / 64;    // 64-column blocks of a row
   static constexpr int kTileBytes = kBlocks * kKeys * 128;
   static constexpr int kBufs = 3;                   // of K and of V
@@ -51,7 +53,7 @@ struct TileShape {
   static constexpr int kStats = kUsed > kPartBytes ? kUsed : kPartBytes;  // row maxima, sums
   static constexpr int kFactors = kStats + 2 * kTileRows * 4;
   static constexpr int kBars = kFactors + kTileRows * 4;
-  static constexpr int kNumBars = 4 * kBufs + 8;
+  static constexpr int kNumBars = 2 * kBufs + 6;
   static constexpr int kMisc = kBars + kNumBars * 8;  // tensor memory address, flags
   // The base is rounded up to 1024.  Never two CTAs on an SM: the second would wait for
   // tensor memory, and the first, in one cluster with it, for the second.
@@ -64,18 +66,25 @@ struct TileShape {
   static_assert(kColQ + kD / 2 <= 512, "tensor memory");
 };
 
-// Waits like mbar_wait, and gives up as well once another role has.
+__device__ __forceinline__ bool mbar_done(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; "
+      "selp.u32 %0, 1, 0, p; }"
+      : "=r"(done)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return done != 0;
+}
+
+// Waits like mbar_wait, and gives up as well once another role has.  Short: the roles' loops
+// share the instruction cache, and unrolled polls cost the product thread 250 cycles a wait.
 __device__ __forceinline__ bool tile_wait(uint32_t bar, uint32_t parity, unsigned* status,
                                           uint32_t limit, volatile int* dead) {
+  if (mbar_done(bar, parity)) return true;
+#pragma unroll 1
   for (uint32_t i = 0; i < limit; ++i) {
-    uint32_t done;
-    asm volatile(
-        "{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; "
-        "selp.u32 %0, 1, 0, p; }"
-        : "=r"(done)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    if (done) return true;
+    if (mbar_done(bar, parity)) return true;
     if (*dead) return false;
   }
   *dead = 1;
@@ -112,18 +121,23 @@ struct CodeTile {
   __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int left,
                                        int t) {
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      const int j = t + 128 * u;
-      x[u] = make_uint4(0, 0, 0, 0);
-      sb[u] = 0;
-      if (j / M < min(left, kKeys)) {
-        x[u] = ld_cg16(codes + (size_t)j * 16);
-        sb[u] = __ldcg(reinterpret_cast<const uint16_t*>(scales + 2 * j));
-      }
+    for (int u = 0; u < kUnits; ++u) load_unit(u, codes, scales, left, t);
+  }
+
+  __device__ __forceinline__ void load_unit(int u, const uint8_t* codes, const uint8_t* scales,
+                                            int left, int t) {
+    const int j = t + 128 * u;
+    x[u] = make_uint4(0, 0, 0, 0);
+    sb[u] = 0;
+    if (j / M < min(left, kKeys)) {
+      x[u] = ld_cg16(codes + (size_t)j * 16);
+      sb[u] = __ldcg(reinterpret_cast<const uint16_t*>(scales + 2 * j));
     }
   }
 
-  __device__ __forceinline__ void unpack(uint32_t dst, int t) const {
+  // The tile to shared memory; a unit's registers take the next tile's codes at once.
+  __device__ __forceinline__ void unpack(uint32_t dst, int t, const uint8_t* codes,
+                                         const uint8_t* scales, int left) {
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
       const int j = t + 128 * u;
@@ -144,6 +158,7 @@ struct CodeTile {
         y = w[1], w[1] = w[3], w[3] = y;
       }
       const uint32_t s_lo = (sb[u] & 255u) * 0x00800080u, s_hi = (sb[u] >> 8) * 0x00800080u;
+      load_unit(u, codes, scales, left, t);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int at = e ^ turn;  // 8-value chunk of the 32
@@ -211,23 +226,21 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
   const unsigned unit = item / a.tiles;
   const int seq = unit / a.heads, head = unit % a.heads;
 
-  // of the buffers of K and V: filled, and free again; of the two S: scores there, weights
-  // there, added to O; Q written; all products complete
-  const uint32_t bars = base + Sh::kBars;
-  const uint32_t full = bars, freed = full + 16 * kBufs;  // K's, then V's
-  const uint32_t s_done = freed + 16 * kBufs, p_full = s_done + 16, o_done = p_full + 16;
-  const uint32_t q_full = o_done + 16, drain = q_full + 8;
+  // full[b]: K of a tile and V of the tile before it are there; done[b]: a tile is added to
+  // O, and its buffers are free; s_done, p_full: scores and weights in one of the two S;
+  // Q written; all products complete
+  const uint32_t full = base + Sh::kBars, done = full + 8 * kBufs, s_done = done + 8 * kBufs;
+  const uint32_t p_full = s_done + 16, q_full = p_full + 16, drain = q_full + 8;
   volatile int* dead = reinterpret_cast<volatile int*>(smem + Sh::kMisc + 4);
   volatile int* odd = dead + 1;  // a new row of V holds a value that is not finite
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 2 * kBufs; ++i) {
-      mbar_init(full + 8 * i, 4);
-      mbar_init(freed + 8 * i, 1);
+    for (int i = 0; i < kBufs; ++i) {
+      mbar_init(full + 8 * i, 8);
+      mbar_init(done + 8 * i, 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(s_done + 8 * i, 1);
       mbar_init(p_full + 8 * i, 4);
-      mbar_init(o_done + 8 * i, 1);
     }
     mbar_init(q_full, 4);
     mbar_init(drain, 1);
@@ -263,7 +276,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
   const int token = min(row, a.rows - 1) / a.group;
   float row_max = -INFINITY, row_sum = 0.f;  // in log2 units
   if (role == 0) {
-    regs_take<kSoftRegs>();
+    if (Sh::kShare) regs_take<kSoftRegs>();
     if (count > 0) {
       const uint32_t q_col = lanes + Sh::kColQ;
       // Q: scaled so that the row's largest value lies in [1, 2), for bf16, or in [2^13, 2^14)
@@ -343,22 +356,23 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
           row_max = top;
           row_sum *= f;
           if (i > 0) {
-            if (!warp_wait(o_done + 8 * (b ^ 1), ((i - 1) >> 1) & 1, a.status, a.wait_limit, dead))
+            if (!warp_wait(done + 8 * ((i - 1) % kBufs), ((i - 1) / kBufs) & 1, a.status,
+                           a.wait_limit, dead))
               break;
             tc_fence_after();
 #pragma unroll 1
-            for (int j = 0; j < kD; j += 32) {
-              uint32_t o[32];
+            for (int j = 0; j < kD; j += 16) {
+              uint32_t o[16];
               tmem_ld(lanes + Sh::kColO + j, o);
 #pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-              tmem_st32(lanes + Sh::kColO + j, o);
+              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+              tmem_st16(lanes + Sh::kColO + j, o);
             }
           }
         }
         const float shift = row_max == -INFINITY ? 0.f : -row_max;
         const unsigned long long c2 = f2_pack(c, c), shift2 = f2_pack(shift, shift);
-        unsigned long long sum2[2] = {0, 0};
+        unsigned long long sum2 = 0;
 #pragma unroll
         for (int j = 0; j < kKeys; j += 2) {
           float lo, hi;
@@ -366,23 +380,23 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
                     lo, hi);
           lo = exp2_approx(lo);
           hi = exp2_approx(hi);
-          sum2[(j >> 1) & 1] = f2_add(sum2[(j >> 1) & 1], f2_pack(lo, hi));
+          sum2 = f2_add(sum2, f2_pack(lo, hi));
           s[j / 2] = is_new ? pack_bf16(lo, hi) : pack_f16(lo, hi);
           if (j % 32 == 30) tmem_st16(s_col + (j - 30) / 2, s + (j - 30) / 2);
         }
         tmem_wait_st();
         tc_fence_before();
         warp_arrive(p_full + 8 * b);
-        row_sum += f2_hsum(f2_add(sum2[0], sum2[1]));
+        row_sum += f2_hsum(sum2);
       }
-      if (warp_wait(o_done + 8 * ((count - 1) & 1), ((count - 1) >> 1) & 1, a.status, a.wait_limit,
-                    dead))
+      if (warp_wait(done + 8 * ((count - 1) % kBufs), ((count - 1) / kBufs) & 1, a.status,
+                    a.wait_limit, dead))
         tc_fence_after();
     }
     __syncwarp();
-    regs_give<128>();
+    if (Sh::kShare) regs_give<128>();
   } else if (role < 3) {
-    regs_give<kTileRegs>();
+    if (Sh::kShare) regs_give<kTileRegs>();
     const int t = threadIdx.x & 127, part = role - 1;  // 0: K, 1: V
     const size_t at = ((size_t)seq * a.seq_rows + (size_t)head * a.cap + (size_t)cached0 * kKeys);
     const uint8_t* codes = (part ? a.v : a.k) + at * (kD / 2);
@@ -391,11 +405,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
     int left = n - cached0 * kKeys;  // cached tokens from the next tile to load on
     CodeTile<M> next;
     if (fresh < count) next.load(codes, scales, left, t);
+    if (part && count > 0) warp_arrive(full);  // of the tile before the first
     for (int i = 0; i < count; ++i) {
-      const int b = part * kBufs + i % kBufs;
-      const uint32_t dst = base + b * Sh::kTileBytes;
-      if (i >= kBufs &&
-          !warp_wait(freed + 8 * b, (i / kBufs + 1) & 1, a.status, a.wait_limit, dead))
+      const int b = i % kBufs;
+      const uint32_t dst = base + (part * kBufs + b) * Sh::kTileBytes;
+      if (i >= kBufs && !warp_wait(done + 8 * b, (i / kBufs + 1) & 1, a.status, a.wait_limit, dead))
         break;
       if (i < fresh) {
         const uint16_t* src = fresh_rows + (size_t)i * kKeys * kD;
@@ -406,30 +420,26 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
           copy_rows<M, false>(src, there, dst, t);
         }
       } else {
-        const CodeTile<M> now = next;
         codes += kKeys * (kD / 2);
         scales += kKeys * (kD / 16);
         left -= kKeys;
-        if (i + 1 < count) next.load(codes, scales, left, t);
-        now.unpack(dst, t);
+        next.unpack(dst, t, codes, scales, i + 1 < count ? left : 0);
       }
       fence_proxy_async_smem();
-      warp_arrive(full + 8 * b);
+      warp_arrive(full + 8 * ((i + part) % kBufs));
+      if (!part && i == count - 1) warp_arrive(full + 8 * (count % kBufs));  // there is none
     }
   } else {
-    regs_give<kProductRegs>();
-    if (threadIdx.x == 384) {
+    if (Sh::kShare) regs_give<kProductRegs>();
+    if (threadIdx.x == 384 && count > 0) {
       constexpr uint32_t kLead = kKeys * 128;
       bool ok = true;
       auto await = [&](uint32_t bar, uint32_t parity) {
-        ok = ok && tile_wait(bar, parity, a.status, a.wait_limit, dead);
+        if (!tile_wait(bar, parity, a.status, a.wait_limit, dead)) ok = false;
       };
+      // K of tile i and V of tile i - 1
+      auto operands = [&](int i) { await(full + 8 * (i % kBufs), (i / kBufs) & 1); };
       auto scores = [&](int i) {
-        if (i == 0) await(q_full, 0);
-        if (i == fresh && i > 0) await(q_full, 1);
-        await(full + 8 * (i % kBufs), (i / kBufs) & 1);
-        if (!ok) return;
-        tc_fence_after();
         const uint32_t desc = i < fresh ? tc_desc(true, false, kKeys) : tc_desc(false, false, kKeys);
         const uint64_t kt = tc_smem(base + (i % kBufs) * Sh::kTileBytes, kLead);
         const uint32_t s_col = tm + (i & 1) * kKeys;
@@ -438,34 +448,33 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
           tc_mma(s_col, tm + Sh::kColQ + 8 * k, kt + (((k >> 2) * kLead + (k & 3) * 32) >> 4), desc,
                  k > 0);
         tc_commit(s_done + 8 * (i & 1));
-        tc_commit(freed + 8 * (i % kBufs));
       };
       auto values = [&](int i) {
-        await(full + 8 * (kBufs + i % kBufs), (i / kBufs) & 1);
-        await(p_full + 8 * (i & 1), (i >> 1) & 1);
-        if (!ok) return;
-        tc_fence_after();
         const uint32_t desc = i < fresh ? tc_desc(true, true, kD) : tc_desc(false, true, kD);
         const uint64_t vt = tc_smem(base + (kBufs + i % kBufs) * Sh::kTileBytes, kLead);
         const uint32_t p_col = tm + (i & 1) * kKeys;
 #pragma unroll
         for (int k = 0; k < kKeys / 16; ++k)
           tc_mma(tm + Sh::kColO, p_col + 8 * k, vt + ((2048 * k) >> 4), desc, i > 0 || k > 0);
-        tc_commit(o_done + 8 * (i & 1));
-        tc_commit(freed + 8 * (kBufs + i % kBufs));
+        tc_commit(done + 8 * (i % kBufs));
       };
       // Products run in the order of their issue: S of tile i + 2 may take the place of the
       // weights of tile i, whose product was issued before.
-      if (count > 0) scores(0);
-      for (int i = 0; i < count && ok; ++i) {
-        if (i + 1 < count) scores(i + 1);
+#pragma unroll 1
+      for (int i = -1; i < count; ++i) {
+        operands(i + 1);
+        if (i + 1 < count && (i + 1 == 0 || i + 1 == fresh)) await(q_full, i + 1 == 0 ? 0 : 1);
+        tc_fence_after();
+        if (ok && i + 1 < count) scores(i + 1);
+        if (i < 0) continue;
+        await(p_full + 8 * (i & 1), (i >> 1) & 1);
+        if (!ok) break;
+        tc_fence_after();
         values(i);
       }
       // every product that was issued is complete before the memory is used again
-      if (count > 0) {
-        tc_commit(drain);
-        mbar_wait(drain, 0, a.status, kWaitLimit);
-      }
+      tc_commit(drain);
+      mbar_wait(drain, 0, a.status, kWaitLimit);
     }
     __syncwarp();
   }
@@ -474,7 +483,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
   // What follows runs on all warps: everyone to the launch's share again.  Behind the barrier:
   // a warp that took registers before the softmax warps had taken and given theirs would
   // leave them waiting.
-  if (role > 0) regs_take<128>();
+  if (Sh::kShare && role > 0) regs_take<128>();
 
   const bool none = n == 0 && !a.k_new;  // no token to attend to
   if (warp < 4) {
