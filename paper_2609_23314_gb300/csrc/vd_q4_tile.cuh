@@ -8,15 +8,16 @@
 // memory, so that shared memory carries K and V only:
 //   S = Q K^T   (128 x kKeys, K's rows along the depth)
 //   O += P V    (128 x head_dim, V's rows along the columns)
-// Roles of the four warpgroups, which meet only at mbarriers:
-//   0  a row per thread: maximum, weights, their sum; O is rescaled where the maximum has
-//      risen by more than 2^8 (a smaller rise only makes the weights exceed 1);
-//   1  K's tiles: cached codes to fp16 in the swizzled layout of the products (exact), or
-//      copies of the new tokens' bf16 rows.  The next tile's codes are loaded from memory
-//      before this one's are unpacked;
-//   2  V's tiles, the same;
-//   3  one thread issues the products: S of tile i + 1 before O takes tile i, so that the
-//      softmax of one tile runs beside the products of its neighbours.
+// Roles of the warps, which meet only at mbarriers:
+//   0-7   softmax, a row per pair of threads with half the columns each: maximum, weights,
+//         their sum; O is rescaled where the maximum has risen by more than 2^8 (a smaller
+//         rise only makes the weights exceed 1);
+//   8-11  K's tiles, a slice of the tokens each: cached codes, which come by bulk copies into
+//         the warp's own ring, to fp16 in the swizzled layout of the products (exact), or
+//         copies of the new tokens' bf16 rows;
+//   12-14 V's tiles, the same;
+//   15    one thread issues the products: S of tile i + 1 before O takes tile i, so that the
+//         softmax of one tile runs beside the products of its neighbours.
 // The new tokens' tiles come first, in bf16, then Q is rewritten in fp16 (rows scaled by
 // powers of two, as in the streaming kernel) for the cached ones.  A cluster splits the
 // tiles of a unit and joins the results through distributed shared memory.
@@ -24,6 +25,7 @@
 
 #include <cstdint>
 #include <cuda_runtime.h>
+#include <type_traits>
 
 #include "vd_device.cuh"
 #include "vd_q4.cuh"
@@ -35,33 +37,36 @@ namespace vd {
 constexpr int kTileRows = 128;  // rows of a block
 
 constexpr int kTileThreads = 512;
-// registers of the warpgroups' threads: 512 x 128 are launched
-constexpr int kSoftRegs = 208, kTileRegs = 104, kProductRegs = 96;
-static_assert(kSoftRegs + 2 * kTileRegs + kProductRegs <= 4 * 128, "registers");
+constexpr int kSoftWarps = 8, kKeyWarps = 4, kValueWarps = 3, kProductWarp = 15;
 
 template <int M>
 struct TileShape {
   static constexpr int kD = 32 * M;
   static constexpr int kKeys = M <= 4 ? 128 : 64;   // tokens of a tile
-  // whether the softmax threads need more registers than their share of the launch's
-  static constexpr bool kShare = kKeys == 128 || M == 8;
   static constexpr int kBlocks = (kD + 63) / 64;    // 64-column blocks of a row
   static constexpr int kTileBytes = kBlocks * kKeys * 128;
-  static constexpr int kBufs = 3;                   // of K and of V
-  static constexpr int kUsed = 2 * kBufs * kTileBytes;
+  static constexpr int kKeyBufs = 2, kValueBufs = 3;
+  static constexpr int kRaw = 3;                    // tiles of codes and scales on their way
+  static constexpr int kRawCodes = kKeys * 16 * M, kRawScales = kKeys * 2 * M;
+  static constexpr int kRawBytes = 2 * (kRawCodes + kRawScales);
+  static constexpr int kRing = (kKeyBufs + kValueBufs) * kTileBytes;
+  static constexpr int kUsed = kRing + kRaw * kRawBytes;
   static constexpr int kPartBytes = kTileRows * kD * 4;
   static constexpr int kStats = kUsed > kPartBytes ? kUsed : kPartBytes;  // row maxima, sums
-  static constexpr int kFactors = kStats + 2 * kTileRows * 4;
-  static constexpr int kBars = kFactors + kTileRows * 4;
-  static constexpr int kNumBars = 2 * kBufs + 6;
+  static constexpr int kFactors = kStats + 3 * kTileRows * 4;  // two sums a row
+  static constexpr int kSwap = kFactors + kTileRows * 4;  // [2][2][row]: halves' maxima
+  static constexpr int kBars = kSwap + 4 * kTileRows * 4;
+  static constexpr int kNumBars = 18 + (kKeyWarps + kValueWarps) * kRaw;
   static constexpr int kMisc = kBars + kNumBars * 8;  // tensor memory address, flags
   // The base is rounded up to 1024.  Never two CTAs on an SM: the second would wait for
   // tensor memory, and the first, in one cluster with it, for the second.
   static constexpr int kNeed = kMisc + 16 + 1024;
   static constexpr int kTotal = kNeed > 120 * 1024 ? kNeed : 120 * 1024;
-  // columns of tensor memory: two S, O, Q (16-bit pairs).  P (16-bit pairs) takes the lower
-  // half of its S, which has been read by then
-  static constexpr int kColO = 2 * kKeys;
+  // columns of tensor memory: two S, P, O, Q (P and Q 16-bit pairs).  At head_dim 256 there
+  // is no room for P, which then takes the lower half of its S
+  static constexpr bool kAlias = M == 8;
+  static constexpr int kColP = 2 * kKeys;
+  static constexpr int kColO = kColP + (kAlias ? 0 : kKeys / 2);
   static constexpr int kColQ = kColO + kD;
   static_assert(kColQ + kD / 2 <= 512, "tensor memory");
 };
@@ -108,93 +113,46 @@ __device__ __forceinline__ void warp_arrive(uint32_t bar) {
   __syncwarp();
 }
 
-// A warpgroup's part of a tile of K or V: cached codes.  32 values, 16 bytes of codes, are a
-// unit.
-template <int M>
-struct CodeTile {
-  static constexpr int kKeys = TileShape<M>::kKeys;
-  static constexpr int kUnits = (kKeys * M + 127) / 128;
-  uint4 x[kUnits];
-  uint32_t sb[kUnits];
-
-  // codes, scales: of the tile's first token; left: tokens that are there
-  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int left,
-                                       int t) {
-#pragma unroll
-    for (int u = 0; u < kUnits; ++u) load_unit(u, codes, scales, left, t);
-  }
-
-  __device__ __forceinline__ void load_unit(int u, const uint8_t* codes, const uint8_t* scales,
-                                            int left, int t) {
-    const int j = t + 128 * u;
-    x[u] = make_uint4(0, 0, 0, 0);
-    sb[u] = 0;
-    if (j / M < min(left, kKeys)) {
-      x[u] = ld_cg16(codes + (size_t)j * 16);
-      sb[u] = __ldcg(reinterpret_cast<const uint16_t*>(scales + 2 * j));
-    }
-  }
-
-  // The tile to shared memory; a unit's registers take the next tile's codes at once.
-  __device__ __forceinline__ void unpack(uint32_t dst, int t, const uint8_t* codes,
-                                         const uint8_t* scales, int left) {
-#pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      const int j = t + 128 * u;
-      if (kKeys * M % 128 != 0 && j >= kKeys * M) break;
-      const int key = j / M, blk = j % M;
-      // the order of the four 16-byte stores, so that 8 neighbouring lanes meet 8 chunk
-      // positions
-      const int turn = M == 4 ? (blk & 2) : M == 8 ? (blk >> 1) & 3 : 0;
-      uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
-      if (M == 8 && (turn & 1)) {
-        uint32_t y = w[0];
-        w[0] = w[1], w[1] = y;
-        y = w[2], w[2] = w[3], w[3] = y;
-      }
-      if (M % 4 == 0 && (turn & 2)) {
-        uint32_t y = w[0];
-        w[0] = w[2], w[2] = y;
-        y = w[1], w[1] = w[3], w[3] = y;
-      }
-      const uint32_t s_lo = (sb[u] & 255u) * 0x00800080u, s_hi = (sb[u] >> 8) * 0x00800080u;
-      load_unit(u, codes, scales, left, t);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int at = e ^ turn;  // 8-value chunk of the 32
-        const uint32_t sc = at < 2 ? s_lo : s_hi;
-        uint32_t h[4];
-        q4_unpack4(w[e], h);
-        const int chunk = 4 * blk + at;
-        st_shared16(dst + (chunk >> 3) * (kKeys * 128) + key * 128 +
-                        (((chunk & 7) ^ (key & 7)) << 4),
-                    make_uint4(h2_mul(h[0], sc), h2_mul(h[1], sc), h2_mul(h[2], sc),
-                               h2_mul(h[3], sc)));
-      }
-    }
+// The tokens of a tile that a warp of `warps` takes: multiples of 8, as scales are copied.
+template <int KEYS>
+struct Slice {
+  int first, count;
+  __device__ __forceinline__ Slice(int warp, int warps) {
+    const int a = (KEYS / 8 * warp + warps - 1) / warps;
+    const int b = (KEYS / 8 * (warp + 1) + warps - 1) / warps;
+    first = 8 * a;
+    count = 8 * (b - a);
   }
 };
 
-// The same for new tokens: bf16 rows as they are, zeros behind the last one (left: rows that
+// Swizzled place of a row's 16-byte chunk.
+template <int M>
+__device__ __forceinline__ uint32_t tile_at(uint32_t dst, int key, int chunk) {
+  return dst + (chunk >> 3) * (TileShape<M>::kKeys * 128) + key * 128 +
+         (((chunk & 7) ^ (key & 7)) << 4);
+}
+
+// New tokens' rows of a slice: bf16 as they are, zeros behind the last one (left: rows that
 // are there).  FINITE: what is not finite becomes zero too; returns whether there was any.
 template <int M, bool FINITE>
-__device__ __forceinline__ bool copy_rows(const uint16_t* src, int left, uint32_t dst, int t) {
-  constexpr int kD = 32 * M, kKeys = TileShape<M>::kKeys;
-  constexpr int kChunks = kKeys * (kD / 8) / 128;  // 16 bytes each, of a thread
+__device__ __forceinline__ bool copy_rows(const uint16_t* src, int left, uint32_t dst, int first,
+                                          int count, int lane) {
+  constexpr int kD = 32 * M;
+  constexpr int kAhead = M <= 4 ? 4 : 2;  // chunks of 16 bytes loaded together
   bool found = false;
 #pragma unroll 1
-  for (int u0 = 0; u0 < kChunks; u0 += 4) {
-    uint4 x[4];
+  for (int j0 = lane; j0 < count * (kD / 8); j0 += 32 * kAhead) {
+    uint4 x[kAhead];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int j = t + 128 * (u0 + u), key = j / (kD / 8), chunk = j % (kD / 8);
+    for (int u = 0; u < kAhead; ++u) {
+      const int j = j0 + 32 * u, key = first + j / (kD / 8), chunk = j % (kD / 8);
       x[u] = make_uint4(0, 0, 0, 0);
-      if (u0 + u < kChunks && key < left) x[u] = ld_cg16(src + (size_t)key * kD + 8 * chunk);
+      if (j < count * (kD / 8) && key < left) x[u] = ld_cg16(src + (size_t)key * kD + 8 * chunk);
     }
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      if (u0 + u >= kChunks) break;
-      const int j = t + 128 * (u0 + u), key = j / (kD / 8), chunk = j % (kD / 8);
+    for (int u = 0; u < kAhead; ++u) {
+      const int j = j0 + 32 * u, key = first + j / (kD / 8), chunk = j % (kD / 8);
+      if (j >= count * (kD / 8)) break;
       if (FINITE) {
         uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
 #pragma unroll
@@ -204,51 +162,117 @@ __device__ __forceinline__ bool copy_rows(const uint16_t* src, int left, uint32_
         }
         x[u] = make_uint4(w[0], w[1], w[2], w[3]);
       }
-      st_shared16(dst + (chunk >> 3) * (kKeys * 128) + key * 128 +
-                      (((chunk & 7) ^ (key & 7)) << 4), x[u]);
+      st_shared16(tile_at<M>(dst, key, chunk), x[u]);
     }
   }
   return found;
 }
 
+// A slice of cached codes to fp16.  32 values, 16 bytes of codes, are a unit.
+template <int M, int UNITS>
+struct CodeSlice {
+  uint4 x[UNITS];
+  uint32_t sb[UNITS];
+
+  // there: the slice's tokens that are there; what lies behind them reads as zero
+  __device__ __forceinline__ void load(uint32_t codes, uint32_t scales, int there, int lane) {
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+      const int j = lane + 32 * u;
+      x[u] = make_uint4(0, 0, 0, 0);
+      sb[u] = 0;
+      if (j < there * M) {
+        x[u] = ld_shared16(codes + 16 * j);
+        sb[u] = ld_shared_u16(scales + 2 * j);
+      }
+    }
+  }
+
+  // The order of a unit's four 16-byte stores, so that 8 neighbouring lanes meet 8 chunk
+  // positions: the unit's e-th store is its chunk e ^ turn.
+  static __device__ __forceinline__ int turn_of(int blk) {
+    return M == 4 ? (blk & 2) : M == 8 ? (blk >> 1) & 3 : 0;
+  }
+
+  __device__ __forceinline__ void unpack(uint32_t dst, int first, int count, int lane) const {
+    // where 32 lanes are a multiple of 8 tokens, a lane's units differ by a constant
+    constexpr bool kRegular = M == 1 || M == 2 || M == 4;
+    uint32_t place[4];
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+      const int j = lane + 32 * u;
+      if (j >= count * M) break;
+      const int key = first + j / M, blk = j % M, turn = turn_of(blk);
+      if (u == 0 || !kRegular)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) place[e] = tile_at<M>(dst, key, 4 * blk + (e ^ turn));
+      uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+      uint32_t sc[2] = {(sb[u] & 255u) * 0x00800080u, (sb[u] >> 8) * 0x00800080u};
+      if (M == 8 && (turn & 1)) {
+        uint32_t y = w[0];
+        w[0] = w[1], w[1] = y;
+        y = w[2], w[2] = w[3], w[3] = y;
+      }
+      if (M % 4 == 0 && (turn & 2)) {
+        uint32_t y = w[0];
+        w[0] = w[2], w[2] = y;
+        y = w[1], w[1] = w[3], w[3] = y;
+        y = sc[0], sc[0] = sc[1], sc[1] = y;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        uint32_t h[4];
+        q4_unpack4(w[e], h);
+        st_shared16(place[e] + (kRegular ? u * (32 / M) * 128 : 0),
+                    make_uint4(h2_mul(h[0], sc[e >> 1]), h2_mul(h[1], sc[e >> 1]),
+                               h2_mul(h[2], sc[e >> 1]), h2_mul(h[3], sc[e >> 1])));
+      }
+    }
+  }
+};
+
 template <int M>
 __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) {
   using Sh = TileShape<M>;
-  constexpr int kD = Sh::kD, kKeys = Sh::kKeys, kBufs = Sh::kBufs;
+  constexpr int kD = Sh::kD, kKeys = Sh::kKeys;
+  constexpr int kKeyBufs = Sh::kKeyBufs, kValueBufs = Sh::kValueBufs, kRaw = Sh::kRaw;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw_base = smem_addr(smem_raw);
   const uint32_t base = (raw_base + 1023u) & ~1023u;
   unsigned char* smem = smem_raw + (base - raw_base);
-  const int warp = threadIdx.x >> 5, role = threadIdx.x >> 7;
+  const int warp = threadIdx.x >> 5;
   const unsigned rank = blockIdx.x % a.cluster;
   const unsigned item = blockIdx.x / a.cluster;
   const int tile = item % a.tiles;
   const unsigned unit = item / a.tiles;
   const int seq = unit / a.heads, head = unit % a.heads;
 
-  // full[b]: K of a tile and V of the tile before it are there; done[b]: a tile is added to
-  // O, and its buffers are free; s_done, p_full: scores and weights in one of the two S;
-  // Q written; all products complete
-  const uint32_t full = base + Sh::kBars, done = full + 8 * kBufs, s_done = done + 8 * kBufs;
-  const uint32_t p_full = s_done + 16, q_full = p_full + 16, drain = q_full + 8;
+  // full[i % 4]: K of tile i and V of the tile before it are there (V's warps may be three
+  // tiles ahead of K's: with fewer barriers they would arrive for a tile to come); s_done[i % 2]: the tile's
+  // scores are, and its K buffer is free; o_done[i % 3]: it is added to O, and its V buffer
+  // free; p_full[i % 2]: its weights are there; swap: a pair of softmax warps has exchanged its
+  // rows' maxima; Q written; all products complete; a warp's codes are there
+  const uint32_t full = base + Sh::kBars, s_done = full + 32, o_done = s_done + 16;
+  const uint32_t p_full = o_done + 24, swap = p_full + 16, q_full = swap + 32;
+  const uint32_t drain = q_full + 8, raw_full = drain + 8;
   volatile int* dead = reinterpret_cast<volatile int*>(smem + Sh::kMisc + 4);
   volatile int* odd = dead + 1;  // a new row of V holds a value that is not finite
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kBufs; ++i) {
-      mbar_init(full + 8 * i, 8);
-      mbar_init(done + 8 * i, 1);
-    }
+    for (int i = 0; i < 4; ++i) mbar_init(full + 8 * i, kKeyWarps + kValueWarps);
+    for (int i = 0; i < 3; ++i) mbar_init(o_done + 8 * i, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(s_done + 8 * i, 1);
-      mbar_init(p_full + 8 * i, 4);
+      mbar_init(p_full + 8 * i, kSoftWarps);
     }
-    mbar_init(q_full, 4);
+    for (int i = 0; i < (kKeyWarps + kValueWarps) * kRaw; ++i) mbar_init(raw_full + 8 * i, 1);
+    for (int i = 0; i < 4; ++i) mbar_init(swap + 8 * i, 2);
+    mbar_init(q_full, kSoftWarps);
     mbar_init(drain, 1);
     fence_mbar_init();
     *dead = 0;
     *odd = 0;
   }
-  if (warp == 12) tmem_alloc(base + Sh::kMisc);
+  if (warp == kProductWarp) tmem_alloc(base + Sh::kMisc);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -271,35 +295,50 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
   const int cached0 = t0 + fresh - tiles_new;  // its first cached tile
   const size_t new_row = (size_t)seq * a.seq_new_rows + (size_t)head * a.B;
 
-  const int row = row0 + (int)threadIdx.x;                   // of the softmax threads
+  const int half = (warp >> 2) & 1, lane_row = threadIdx.x & 127;  // of the softmax threads
+  const int row = row0 + lane_row;
   const uint32_t lanes = tm + ((uint32_t)(warp & 3) << 21);  // their warp's 32 lanes
   const int token = min(row, a.rows - 1) / a.group;
-  float row_max = -INFINITY, row_sum = 0.f;  // in log2 units
-  if (role == 0) {
-    if (Sh::kShare) regs_take<kSoftRegs>();
+  float row_max = -INFINITY, row_sum = 0.f;  // in log2 units; the sum: of this half
+  if (warp < kSoftWarps) {
+    constexpr int kHalf = kKeys / 2;
+    float* swapped = reinterpret_cast<float*>(smem + Sh::kSwap) + lane_row;
+    // the larger of both halves' m; `turn` counts the calls
+    auto exchange = [&](float& m, int turn) {
+      float* at = swapped + (turn & 1) * 2 * kTileRows;
+      at[half * kTileRows] = m;
+      warp_arrive(swap + 8 * (warp & 3));
+      if (!warp_wait(swap + 8 * (warp & 3), turn & 1, a.status, a.wait_limit, dead)) return false;
+      m = fmaxf(m, at[(half ^ 1) * kTileRows]);
+      return true;
+    };
     if (count > 0) {
-      const uint32_t q_col = lanes + Sh::kColQ;
+      const uint32_t q_col = lanes + Sh::kColQ + half * 8 * M;
       // Q: scaled so that the row's largest value lies in [1, 2), for bf16, or in [2^13, 2^14)
       float unit_scale;
+      bool ok;
       {
         const uint16_t* q = a.q + ((((size_t)seq * a.B + token) * a.heads + head) * a.group +
-                                   row % a.group) * kD;
-        uint32_t w[16 * M];
+                                   row % a.group) * kD + half * 16 * M;
+        uint32_t w[8 * M];
 #pragma unroll
-        for (int i = 0; i < 4 * M; ++i) {
+        for (int i = 0; i < 2 * M; ++i) {
           uint4 x = make_uint4(0, 0, 0, 0);
           if (row < a.rows) x = ld_cg16(q + 8 * i);
           w[4 * i] = x.x, w[4 * i + 1] = x.y, w[4 * i + 2] = x.z, w[4 * i + 3] = x.w;
         }
         uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < 16 * M; ++i)
+        for (int i = 0; i < 8 * M; ++i)
           top = max(top, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
+        float both = (float)top;
+        ok = exchange(both, 0);
+        top = (uint32_t)both;
         const uint32_t ex = top ? min(253u, max(1u, top >> 7)) : 127u;
         const uint32_t up = ((254 - ex) << 7) * 0x00010001u;
         unit_scale = __uint_as_float(ex << 23) * (a.scale * kLog2e);
 #pragma unroll
-        for (int i = 0; i < 16 * M; ++i) {
+        for (int i = 0; i < 8 * M; ++i) {
           asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(w[i]) : "r"(up));
           if (fresh == 0)
             w[i] = pack_f16(__uint_as_float(w[i] << 16) * 0x1p13f,
@@ -307,26 +346,26 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
         }
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < M; ++i) tmem_st16(q_col + 16 * i, w + 16 * i);
+        for (int i = 0; i < M; ++i) tmem_st8(q_col + 8 * i, w + 8 * i);
         tmem_wait_st();
         tc_fence_before();
         warp_arrive(q_full);
       }
-      for (int i = 0; i < count; ++i) {
-        const int b = i & 1;
-        const uint32_t s_col = lanes + b * kKeys;
-        if (!warp_wait(s_done + 8 * b, (i >> 1) & 1, a.status, a.wait_limit, dead)) break;
+      for (int i = 0; ok && i < count; ++i) {
+        const uint32_t s_col = lanes + (i & 1) * kKeys;
+        ok = warp_wait(s_done + 8 * (i & 1), (i >> 1) & 1, a.status, a.wait_limit, dead);
+        if (!ok) break;
         tc_fence_after();
         if (i == fresh - 1 && fresh < count) {  // the last product with Q in bf16
 #pragma unroll 1
           for (int j = 0; j < M; ++j) {
-            uint32_t w[16];
-            tmem_ld(q_col + 16 * j, w);
+            uint32_t w[8];
+            tmem_ld(q_col + 8 * j, w);
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
+            for (int e = 0; e < 8; ++e)
               w[e] = pack_f16(__uint_as_float(w[e] << 16) * 0x1p13f,
                               __uint_as_float(w[e] & 0xffff0000u) * 0x1p13f);
-            tmem_st16(q_col + 16 * j, w);
+            tmem_st8(q_col + 8 * j, w);
           }
           tmem_wait_st();
           tc_fence_before();
@@ -335,20 +374,33 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
         const bool is_new = i < fresh;
         // not 0, which would make a masked score a NaN
         const float c = fmaxf(is_new ? unit_scale : unit_scale * 0x1p-13f, 0x1p-126f);
-        uint32_t s[kKeys];
-        tmem_ld2(s_col, s);
+        uint32_t s[kHalf];
+        tmem_ld(s_col + half * kHalf, s);
         // tokens behind this row's last one do not count
-        const int seen = is_new ? token - (t0 + i) * kKeys
-                                : n - 1 - (cached0 + i - fresh) * kKeys;
-        if (__any_sync(kFull, seen < kKeys - 1)) {
+        const int seen = (is_new ? token - (t0 + i) * kKeys
+                                 : n - 1 - (cached0 + i - fresh) * kKeys) - half * kHalf;
+        if (__any_sync(kFull, seen < kHalf - 1)) {
 #pragma unroll
-          for (int j = 0; j < kKeys; ++j)
+          for (int j = 0; j < kHalf; ++j)
             if (j > seen) s[j] = 0xff800000u;
         }
         float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int j = 0; j < kKeys; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(s[j]));
-        const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * c;
+        for (int j = 0; j < kHalf; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(s[j]));
+        float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * c;
+        // with P over S: both halves have read their scores before either writes weights
+        if (Sh::kAlias) tc_fence_before();
+        ok = exchange(m, i + 1);
+        if (!ok) break;
+        if (Sh::kAlias) tc_fence_after();
+        bool added = i == 0;  // the tile before is in O, and P is free
+        auto wait_added = [&] {
+          if (!added)
+            added = warp_wait(o_done + 8 * ((i - 1) % 3), ((i - 1) / 3) & 1, a.status,
+                              a.wait_limit, dead);
+          if (added) tc_fence_after();
+          return added;
+        };
         // the weights stay below 2^8, and a row's first scores set its maximum
         if (__any_sync(kFull, m > row_max + 8.f)) {
           const float top = fmaxf(row_max, m);
@@ -356,92 +408,152 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
           row_max = top;
           row_sum *= f;
           if (i > 0) {
-            if (!warp_wait(done + 8 * ((i - 1) % kBufs), ((i - 1) / kBufs) & 1, a.status,
-                           a.wait_limit, dead))
-              break;
-            tc_fence_after();
+            ok = wait_added();
+            if (!ok) break;
 #pragma unroll 1
-            for (int j = 0; j < kD; j += 16) {
+            for (int j = 0; j < kD / 2; j += 16) {
               uint32_t o[16];
-              tmem_ld(lanes + Sh::kColO + j, o);
+              const uint32_t at = lanes + Sh::kColO + half * (kD / 2) + j;
+              tmem_ld(at, o);
 #pragma unroll
               for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-              tmem_st16(lanes + Sh::kColO + j, o);
+              tmem_st16(at, o);
             }
           }
         }
         const float shift = row_max == -INFINITY ? 0.f : -row_max;
         const unsigned long long c2 = f2_pack(c, c), shift2 = f2_pack(shift, shift);
         unsigned long long sum2 = 0;
+        auto weights = [&](auto pack) {
 #pragma unroll
-        for (int j = 0; j < kKeys; j += 2) {
-          float lo, hi;
-          f2_unpack(f2_fma(f2_pack(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), c2, shift2),
-                    lo, hi);
-          lo = exp2_approx(lo);
-          hi = exp2_approx(hi);
-          sum2 = f2_add(sum2, f2_pack(lo, hi));
-          s[j / 2] = is_new ? pack_bf16(lo, hi) : pack_f16(lo, hi);
-          if (j % 32 == 30) tmem_st16(s_col + (j - 30) / 2, s + (j - 30) / 2);
+          for (int j = 0; j < kHalf; j += 2) {
+            float lo, hi;
+            f2_unpack(f2_fma(f2_pack(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), c2, shift2),
+                      lo, hi);
+            lo = exp2_approx(lo);
+            hi = exp2_approx(hi);
+            sum2 = f2_add(sum2, f2_pack(lo, hi));
+            s[j / 2] = pack(lo, hi);
+          }
+        };
+        if (is_new)
+          weights([](float lo, float hi) { return pack_bf16(lo, hi); });
+        else
+          weights([](float lo, float hi) { return pack_f16(lo, hi); });
+        if (!Sh::kAlias) ok = wait_added();
+        if (!ok) break;
+        const uint32_t p_col =
+            (Sh::kAlias ? s_col : lanes + Sh::kColP) + half * (kHalf / 2);
+        if (kHalf >= 64) {
+          tmem_st16(p_col, s);
+          tmem_st16(p_col + 16, s + 16);
+        } else {
+          tmem_st16(p_col, s);
         }
         tmem_wait_st();
         tc_fence_before();
-        warp_arrive(p_full + 8 * b);
+        warp_arrive(p_full + 8 * (i & 1));
         row_sum += f2_hsum(sum2);
       }
-      if (warp_wait(done + 8 * ((count - 1) % kBufs), ((count - 1) / kBufs) & 1, a.status,
+      if (warp_wait(o_done + 8 * ((count - 1) % 3), ((count - 1) / 3) & 1, a.status,
                     a.wait_limit, dead))
         tc_fence_after();
     }
-    __syncwarp();
-    if (Sh::kShare) regs_give<128>();
-  } else if (role < 3) {
-    if (Sh::kShare) regs_give<kTileRegs>();
-    const int t = threadIdx.x & 127, part = role - 1;  // 0: K, 1: V
-    const size_t at = ((size_t)seq * a.seq_rows + (size_t)head * a.cap + (size_t)cached0 * kKeys);
-    const uint8_t* codes = (part ? a.v : a.k) + at * (kD / 2);
-    const uint8_t* scales = (part ? a.vs : a.ks) + at * (kD / 16);
-    const uint16_t* fresh_rows = (part ? a.v_new : a.k_new) + (new_row + (size_t)t0 * kKeys) * kD;
-    int left = n - cached0 * kKeys;  // cached tokens from the next tile to load on
-    CodeTile<M> next;
-    if (fresh < count) next.load(codes, scales, left, t);
-    if (part && count > 0) warp_arrive(full);  // of the tile before the first
-    for (int i = 0; i < count; ++i) {
-      const int b = i % kBufs;
-      const uint32_t dst = base + (part * kBufs + b) * Sh::kTileBytes;
-      if (i >= kBufs && !warp_wait(done + 8 * b, (i / kBufs + 1) & 1, a.status, a.wait_limit, dead))
-        break;
-      if (i < fresh) {
-        const uint16_t* src = fresh_rows + (size_t)i * kKeys * kD;
-        const int there = keys_new - (t0 + i) * kKeys;
-        if (part) {  // what is not finite is added at the end, to the rows that see it
-          if (copy_rows<M, true>(src, there, dst, t)) *odd = 1;
-        } else {
-          copy_rows<M, false>(src, there, dst, t);
+  } else if (warp < kProductWarp) {
+    // K's warps or V's: their slices of the tiles, as the buffers become free
+    auto slices = [&](auto part_) {
+      constexpr int kPart = decltype(part_)::value;  // 0: K, 1: V
+      constexpr int kWarpsOf = kPart ? kValueWarps : kKeyWarps;
+      constexpr int kBufs = kPart ? kValueBufs : kKeyBufs;
+      constexpr int kUnits = ((kKeys / 8 + kWarpsOf - 1) / kWarpsOf * 8 * M + 31) / 32;
+      const int lane = threadIdx.x & 31, which = warp - kSoftWarps;
+      const Slice<kKeys> slice(which - kPart * kKeyWarps, kWarpsOf);
+      const size_t at = (size_t)seq * a.seq_rows + (size_t)head * a.cap +
+                        (size_t)cached0 * kKeys + slice.first;
+      const uint8_t* codes = (kPart ? a.v : a.k) + at * (kD / 2);
+      const uint8_t* scales = (kPart ? a.vs : a.ks) + at * (kD / 16);
+      const uint16_t* fresh_rows = (kPart ? a.v_new : a.k_new) + (new_row + (size_t)t0 * kKeys) * kD;
+      const uint32_t raw = base + Sh::kRing + kPart * Sh::kRawCodes + slice.first * (kD / 2);
+      const uint32_t raw_scales = base + Sh::kRing + 2 * Sh::kRawCodes + kPart * Sh::kRawScales +
+                                  slice.first * (kD / 16);
+      const uint32_t bar = raw_full + 8 * kRaw * which;
+      const int cached = count - fresh, left = n - cached0 * kKeys - slice.first;
+      // tokens of the slice in the CTA's cached tile ci
+      auto there = [&](int ci) { return min(slice.count, max(0, left - ci * kKeys)); };
+      auto fetch = [&](int ci) {
+        const int keys = there(ci), slot = ci % kRaw;
+        if (keys == 0) return;
+        const uint32_t scale_bytes = (uint32_t)((keys + 7) & ~7) * (kD / 16);  // within the capacity
+        mbar_expect_tx(bar + 8 * slot, keys * (kD / 2) + scale_bytes);
+        bulk_g2s(raw + slot * Sh::kRawBytes, codes + (size_t)ci * kKeys * (kD / 2), keys * (kD / 2),
+                 bar + 8 * slot);
+        bulk_g2s(raw_scales + slot * Sh::kRawBytes, scales + (size_t)ci * kKeys * (kD / 16),
+                 scale_bytes, bar + 8 * slot);
+      };
+      if (lane == 0)
+        for (int ci = 0; ci < min(kRaw, cached); ++ci) fetch(ci);
+      int fetched = min(kRaw, cached);
+      if (kPart && count > 0) warp_arrive(full);  // of the tile before the first
+      bool ok = true;
+      for (int i = 0; i < count; ++i) {
+        const uint32_t dst =
+            base + (kPart ? kKeyBufs + i % kValueBufs : i % kKeyBufs) * Sh::kTileBytes;
+        CodeSlice<M, kUnits> x;
+        if (i >= fresh) {
+          const int ci = i - fresh, slot = ci % kRaw, keys = there(ci);
+          if (keys > 0)
+            ok = warp_wait(bar + 8 * slot, (ci / kRaw) & 1, a.status, a.wait_limit, dead);
+          if (!ok) break;
+          x.load(raw + slot * Sh::kRawBytes, raw_scales + slot * Sh::kRawBytes, keys, lane);
+          __syncwarp();
+          if (fetched < cached) {
+            if (lane == 0) {
+              fence_proxy_async_smem();
+              fetch(fetched);
+            }
+            ++fetched;
+          }
         }
-      } else {
-        codes += kKeys * (kD / 2);
-        scales += kKeys * (kD / 16);
-        left -= kKeys;
-        next.unpack(dst, t, codes, scales, i + 1 < count ? left : 0);
+        if (i >= kBufs)
+          ok = warp_wait((kPart ? o_done : s_done) + 8 * (i % kBufs), (i / kBufs + 1) & 1, a.status,
+                         a.wait_limit, dead);
+        if (!ok) break;
+        if (i < fresh) {
+          const uint16_t* src = fresh_rows + (size_t)i * kKeys * kD;
+          // what is not finite in V is added at the end, to the rows that see it
+          if (copy_rows<M, kPart != 0>(src, keys_new - (t0 + i) * kKeys, dst, slice.first,
+                                       slice.count, lane))
+            *odd = 1;
+        } else {
+          x.unpack(dst, slice.first, slice.count, lane);
+        }
+        fence_proxy_async_smem();
+        warp_arrive(full + 8 * ((i + kPart) & 3));
+        if (!kPart && i == count - 1) warp_arrive(full + 8 * (count & 3));  // there is none
       }
-      fence_proxy_async_smem();
-      warp_arrive(full + 8 * ((i + part) % kBufs));
-      if (!part && i == count - 1) warp_arrive(full + 8 * (count % kBufs));  // there is none
-    }
+      // nothing may be in flight when the ring's memory is used again
+      if (!ok && lane == 0)
+        for (int ci = max(0, fetched - kRaw); ci < fetched; ++ci)
+          if (there(ci) > 0)
+            mbar_wait(bar + 8 * (ci % kRaw), (ci / kRaw) & 1, a.status, kWaitLimit);
+      __syncwarp();
+    };
+    if (warp < kSoftWarps + kKeyWarps)
+      slices(std::integral_constant<int, 0>{});
+    else
+      slices(std::integral_constant<int, 1>{});
   } else {
-    if (Sh::kShare) regs_give<kProductRegs>();
-    if (threadIdx.x == 384 && count > 0) {
+    if ((threadIdx.x & 31) == 0 && count > 0) {
       constexpr uint32_t kLead = kKeys * 128;
       bool ok = true;
       auto await = [&](uint32_t bar, uint32_t parity) {
         if (!tile_wait(bar, parity, a.status, a.wait_limit, dead)) ok = false;
       };
       // K of tile i and V of tile i - 1
-      auto operands = [&](int i) { await(full + 8 * (i % kBufs), (i / kBufs) & 1); };
+      auto operands = [&](int i) { await(full + 8 * (i & 3), (i >> 2) & 1); };
       auto scores = [&](int i) {
         const uint32_t desc = i < fresh ? tc_desc(true, false, kKeys) : tc_desc(false, false, kKeys);
-        const uint64_t kt = tc_smem(base + (i % kBufs) * Sh::kTileBytes, kLead);
+        const uint64_t kt = tc_smem(base + (i % kKeyBufs) * Sh::kTileBytes, kLead);
         const uint32_t s_col = tm + (i & 1) * kKeys;
 #pragma unroll
         for (int k = 0; k < kD / 16; ++k)
@@ -451,18 +563,18 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
       };
       auto values = [&](int i) {
         const uint32_t desc = i < fresh ? tc_desc(true, true, kD) : tc_desc(false, true, kD);
-        const uint64_t vt = tc_smem(base + (kBufs + i % kBufs) * Sh::kTileBytes, kLead);
-        const uint32_t p_col = tm + (i & 1) * kKeys;
+        const uint64_t vt = tc_smem(base + (kKeyBufs + i % kValueBufs) * Sh::kTileBytes, kLead);
+        const uint32_t p_col = tm + (Sh::kAlias ? (i & 1) * kKeys : Sh::kColP);
 #pragma unroll
         for (int k = 0; k < kKeys / 16; ++k)
           tc_mma(tm + Sh::kColO, p_col + 8 * k, vt + ((2048 * k) >> 4), desc, i > 0 || k > 0);
-        tc_commit(done + 8 * (i % kBufs));
+        tc_commit(o_done + 8 * (i % 3));
       };
-      // Products run in the order of their issue: S of tile i + 2 may take the place of the
-      // weights of tile i, whose product was issued before.
 #pragma unroll 1
       for (int i = -1; i < count; ++i) {
         operands(i + 1);
+        // S of tile i + 1 takes the place of the weights of tile i - 1
+        if (Sh::kAlias && i > 0) await(o_done + 8 * ((i - 1) % 3), ((i - 1) / 3) & 1);
         if (i + 1 < count && (i + 1 == 0 || i + 1 == fresh)) await(q_full, i + 1 == 0 ? 0 : 1);
         tc_fence_after();
         if (ok && i + 1 < count) scores(i + 1);
@@ -480,34 +592,33 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
   }
   __syncthreads();
 
-  // What follows runs on all warps: everyone to the launch's share again.  Behind the barrier:
-  // a warp that took registers before the softmax warps had taken and given theirs would
-  // leave them waiting.
-  if (Sh::kShare && role > 0) regs_take<128>();
-
   const bool none = n == 0 && !a.k_new;  // no token to attend to
-  if (warp < 4) {
+  float* stat = reinterpret_cast<float*>(smem + Sh::kStats);  // [max, sum, sum][row]
+  if (warp < kSoftWarps) {
+    if (half == 0) stat[lane_row] = row_max;
+    stat[(1 + half) * kTileRows + lane_row] = row_sum;
+  }
+  __syncthreads();
+  if (warp < kSoftWarps) {
     const bool valid = row < a.rows && !bad_len;
     const size_t at = (((size_t)seq * a.B + token) * a.heads + head) * a.group + row % a.group;
+    row_sum = stat[kTileRows + lane_row] + stat[2 * kTileRows + lane_row];
     const float inv = none ? 0.f : 1.f / row_sum;
-    if (a.cluster == 1 && valid && a.lse)
+    if (a.cluster == 1 && valid && a.lse && half == 0)
       a.lse[at] = none ? -INFINITY : row_max / kLog2e + logf(row_sum);
-    float* stat = reinterpret_cast<float*>(smem + Sh::kStats);
-    stat[threadIdx.x] = row_max;
-    stat[kTileRows + threadIdx.x] = row_sum;
 #pragma unroll 1
-    for (int j = 0; j < kD; j += 32) {
-      uint32_t o[32];
+    for (int j = half * (kD / 2); j < (half + 1) * (kD / 2); j += 16) {
+      uint32_t o[16];
       if (count > 0) {
         tmem_ld(lanes + Sh::kColO + j, o);
       } else {
 #pragma unroll
-        for (int e = 0; e < 32; ++e) o[e] = 0;
+        for (int e = 0; e < 16; ++e) o[e] = 0;
       }
       if (*odd) {  // the values that were left out
         for (int key = t0 * kKeys; key < min((t0 + fresh) * kKeys, token + 1); ++key)
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
+          for (int e = 0; e < 16; ++e) {
             const uint16_t x = a.v_new[(new_row + key) * kD + j + e];
             if ((x & 0x7f80u) == 0x7f80u)
               o[e] = __float_as_uint(__uint_as_float(o[e]) + __uint_as_float((uint32_t)x << 16));
@@ -517,7 +628,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
       if (a.cluster == 1) {
         if (valid)
 #pragma unroll
-          for (int e = 0; e < 32; e += 8) {
+          for (int e = 0; e < 16; e += 8) {
             uint32_t w[4];
 #pragma unroll
             for (int f = 0; f < 4; ++f)
@@ -528,8 +639,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
         __syncwarp();
       } else {  // [dim / 4][row][4]
 #pragma unroll
-        for (int e = 0; e < 32; e += 4)
-          st_shared16(base + (((j + e) / 4) * kTileRows + threadIdx.x) * 16,
+        for (int e = 0; e < 16; e += 4)
+          st_shared16(base + (((j + e) / 4) * kTileRows + lane_row) * 16,
                       make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]));
       }
     }
@@ -539,7 +650,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
     cluster_sync();
   else
     __syncthreads();
-  if (warp == 12) {
+  if (warp == kProductWarp) {
     tc_fence_after();
     tmem_free(tm);
   }
@@ -563,7 +674,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
       if (q < a.cluster) {
         // a CTA without tokens has sums of zero; one whose scores were all NaN has NaN sums
         mx[q] = mx[q] == -INFINITY ? 1.f : exp2_approx(mx[q] - m);
-        l = fmaf(ld_cluster_f32(mapa(stats + 4 * (kTileRows + r0 + r), q)), mx[q], l);
+        l = fmaf(ld_cluster_f32(mapa(stats + 4 * (kTileRows + r0 + r), q)) +
+                     ld_cluster_f32(mapa(stats + 4 * (2 * kTileRows + r0 + r), q)),
+                 mx[q], l);
       }
     const float inv = none ? 0.f : 1.f / l;
 #pragma unroll

@@ -226,6 +226,25 @@ def test_same_call_same_bytes(B, group):
 
 
 @pytest.mark.usefixtures("route")
+@pytest.mark.parametrize("d", [64, 128, 192, 256])
+@pytest.mark.parametrize("B,new", [(2, True), (40, True), (40, False)])
+def test_cold_and_warm_reads_give_the_same_bytes(d, B, new):
+    """The parts of a CTA run at different speeds when their rows come from memory and
+    when they come from the L2 cache; the results have to be the same."""
+    c, q, k_new, v_new = state([300, 90], 1, 2, 4, d, B, 304)
+    if not new:
+        k_new = v_new = None
+    flush = torch.empty(80 << 20, dtype=torch.int32, device="cuda")
+    first, _ = check(c, q, k_new, v_new)
+    for i in range(12):
+        if i % 2:
+            flush.fill_(i)
+        out = torch.full_like(q, 9.0)
+        vd.vd_q4_attend(c, q, out, k_new, v_new)
+        assert torch.equal(out, first), f"call {i}"
+
+
+@pytest.mark.usefixtures("route")
 @pytest.mark.parametrize("B", [1, 40])
 def test_a_wait_that_gives_up(B, monkeypatch):
     """With no polls left every copy counts as late: the call returns, the status says
