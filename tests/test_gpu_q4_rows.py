@@ -102,6 +102,36 @@ def test_pack_and_unpack(d, lens, caps, kind):
                 assert torch.equal(a[s, :, :, :n], b[s, :, :, :n])
 
 
+def test_buffers_at_16_byte_boundaries():
+    """bf16 buffers that are 16-byte but not 32-byte aligned."""
+    def shifted(t):
+        flat = torch.zeros(t.numel() + 8, dtype=t.dtype, device="cuda")
+        assert flat.data_ptr() % 32 == 0
+        flat[8:].copy_(t.reshape(-1))
+        return flat[8:].view(t.shape)
+
+    kn, vn = (shifted(rows((2, 2, 3, 5, 96), s)) for s in (1, 2))
+    c = q4_filled(2, 2, 3, 16, 96)
+    vd.vd_q4_append(c, kn, vn, 5)
+    for x, codes, scales in ((kn, c.k, c.k_scale), (vn, c.v, c.v_scale)):
+        wc, ws = ref.quantise(x.cpu())
+        assert torch.equal(codes[:, :, :, :5].cpu(), wc)
+        assert torch.equal(scales[:, :, :, :5].cpu(), ws)
+    cache = vd.Cache(shifted(torch.zeros(2, 2, 3, 16, 96, dtype=torch.bfloat16)),
+                     shifted(torch.zeros(2, 2, 3, 16, 96, dtype=torch.bfloat16)), c.len.clone())
+    vd.vd_q4_unpack(c, cache)
+    for t, codes, scales in ((cache.k, c.k, c.k_scale), (cache.v, c.v, c.v_scale)):
+        want = ref.values(codes[:, :, :, :5].cpu(), scales[:, :, :, :5].cpu())
+        assert torch.equal(t[:, :, :, :5].cpu().double(), want)
+    again = q4_filled(2, 2, 3, 16, 96, seed=9)
+    cache.k.fill_(1.25)
+    cache.v.fill_(-3.0)
+    vd.vd_q4_pack(again, cache)
+    wc, ws = ref.quantise(cache.v[:, :, :, :5].cpu())
+    assert torch.equal(again.v[:, :, :, :5].cpu(), wc)
+    assert torch.equal(again.v_scale[:, :, :, :5].cpu(), ws)
+
+
 def test_layers_one_by_one():
     """A bf16 cache of one layer serves as the staging buffer of every layer in turn; the
     lengths follow the last layer."""
