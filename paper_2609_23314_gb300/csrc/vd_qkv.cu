@@ -22,12 +22,13 @@ struct QkvArgs {
   const float* inv_freq;
   const int32_t* pos_first_new;
   uint16_t *q_out, *k_new, *v_new;
-  long long tokens;
-  int B, n_q, n_kv, d, rd, layer, n_layer;
+  int tokens, B, n_q, n_kv, d, rd, layer, n_layer;
   int items, lanes;  // chunk pairs of a head, lanes that share a head (a power of two)
   int tokens_per_cta;
   float eps;
 };
+
+constexpr int kMaxTokens = 8;  // of a CTA
 
 // Angle over pi, reduced to [-1, 1].  The product and its reduction are in fp64:
 // in fp32 a position of 10^6 would leave an error of 0.06.
@@ -51,27 +52,14 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
 template <bool INTERLEAVED>
 __global__ void __launch_bounds__(kThreads) qkv_norm_rope_kernel(QkvArgs a) {
   extern __shared__ __align__(16) float table[];  // [token][cos half | sin half]
-  grid_dependency_wait();
-  grid_launch_dependents();
+  __shared__ size_t new_row[kMaxTokens];          // a token's row of the new rows' first head
   const int half = a.rd >> 1;
-  const long long tok0 = (long long)blockIdx.x * a.tokens_per_cta;
-  const int n_tok = (int)(a.tokens - tok0 < a.tokens_per_cta ? a.tokens - tok0
-                                                              : a.tokens_per_cta);
-  for (int i = threadIdx.x; i < n_tok * half; i += kThreads) {
-    const int t = i / half, f = i % half;
-    const long long tok = tok0 + t;
-    const double pos = (double)((long long)a.pos_first_new[tok / a.B] + tok % a.B);
-    float sn, cs;
-    sincospif(half_turns(pos, a.inv_freq[f]), &sn, &cs);
-    table[t * a.rd + f] = cs;
-    table[t * a.rd + half + f] = sn;
-  }
-  __syncthreads();
+  const int tok0 = (int)blockIdx.x * a.tokens_per_cta;
+  const int n_tok = min(a.tokens - tok0, a.tokens_per_cta);
   const int heads = a.n_q + 2 * a.n_kv;
   const int j = threadIdx.x % a.lanes, slots = kThreads / a.lanes;
   const int rot8 = a.rd >> 3, d8 = a.d >> 3;  // chunks that turn, chunks
   int c0, c1;
-  bool second;
   if (INTERLEAVED || j >= rot8 / 2) {
     c0 = 2 * j;
     c1 = 2 * j + 1;
@@ -79,23 +67,41 @@ __global__ void __launch_bounds__(kThreads) qkv_norm_rope_kernel(QkvArgs a) {
     c0 = j;
     c1 = j + rot8 / 2;
   }
-  const bool active = j < a.items;
-  second = active && c1 < d8;
-  for (int it = threadIdx.x / a.lanes; it < n_tok * heads; it += slots) {
+  const bool active = j < a.items, second = active && c1 < d8;
+  const int items = n_tok * heads;
+  grid_dependency_wait();
+  grid_launch_dependents();
+  const uint16_t* src = a.qkv + (size_t)tok0 * heads * a.d;
+  uint4 n0 = make_uint4(0, 0, 0, 0), n1 = n0;  // the next item's chunks
+  auto fetch = [&](int it) {
+    const uint16_t* p = src + (size_t)it * a.d;
+    if (active && it < items) n0 = ld_cg16(p + c0 * 8);
+    if (second && it < items) n1 = ld_cg16(p + c1 * 8);
+  };
+  fetch(threadIdx.x / a.lanes);
+  if (threadIdx.x < n_tok) {
+    const int tok = tok0 + threadIdx.x;
+    new_row[threadIdx.x] = ((size_t)(tok / a.B) * a.n_layer + a.layer) * a.n_kv * a.B + tok % a.B;
+  }
+  for (int i = threadIdx.x; i < n_tok * half; i += kThreads) {
+    const int t = i / half, f = i % half, tok = tok0 + t;
+    const double pos = (double)((long long)a.pos_first_new[tok / a.B] + tok % a.B);
+    float sn, cs;
+    sincospif(half_turns(pos, a.inv_freq[f]), &sn, &cs);
+    table[t * a.rd + f] = cs;
+    table[t * a.rd + half + f] = sn;
+  }
+  __syncthreads();
+  for (int it = threadIdx.x / a.lanes; it < items; it += slots) {
     const int t = it / heads, h = it % heads;
-    const long long tok = tok0 + t;
-    const uint16_t* src = a.qkv + ((size_t)tok * heads + h) * a.d;
-    uint4 w0 = make_uint4(0, 0, 0, 0), w1 = w0;
-    if (active) w0 = ld_cg16(src + c0 * 8);
-    if (second) w1 = ld_cg16(src + c1 * 8);
+    uint4 w0 = n0, w1 = n1;
+    fetch(it + slots);
     uint16_t* dst;
     if (h < a.n_q) {
-      dst = a.q_out + ((size_t)tok * a.n_q + h) * a.d;
+      dst = a.q_out + ((size_t)(tok0 + t) * a.n_q + h) * a.d;
     } else {
       const int kh = h < a.n_q + a.n_kv ? h - a.n_q : h - a.n_q - a.n_kv;
-      const long long s = tok / a.B, b = tok % a.B;
-      dst = (h < a.n_q + a.n_kv ? a.k_new : a.v_new) +
-            ((((size_t)s * a.n_layer + a.layer) * a.n_kv + kh) * a.B + b) * a.d;
+      dst = (h < a.n_q + a.n_kv ? a.k_new : a.v_new) + (new_row[t] + (size_t)kh * a.B) * a.d;
     }
     if (h < a.n_q + a.n_kv) {
       float x[8], y[8];
@@ -186,7 +192,10 @@ extern "C" vd_status vd_qkv_norm_rope(const void* qkv, int32_t n_seq, int32_t B,
   a.q_out = static_cast<uint16_t*>(q_out);
   a.k_new = static_cast<uint16_t*>(k_new);
   a.v_new = static_cast<uint16_t*>(v_new);
-  a.tokens = (long long)n_seq * B;
+  const long long tokens = (long long)n_seq * B;
+  if (tokens > INT_MAX - kMaxTokens || (long long)n_q_head + 2LL * n_kv_head > 65536)
+    return VD_ERR_UNSUPPORTED;
+  a.tokens = (int)tokens;
   a.B = B;
   a.n_q = n_q_head;
   a.n_kv = n_kv_head;
@@ -198,9 +207,8 @@ extern "C" vd_status vd_qkv_norm_rope(const void* qkv, int32_t n_seq, int32_t B,
   a.lanes = 1;
   while (a.lanes < a.items) a.lanes <<= 1;
   a.eps = eps;
-  a.tokens_per_cta = a.tokens >= 8LL * dev.sms ? 4 : 1;
-  const long long grid = (a.tokens + a.tokens_per_cta - 1) / a.tokens_per_cta;
-  if (grid > INT_MAX || (long long)n_q_head + 2LL * n_kv_head > 65536) return VD_ERR_UNSUPPORTED;
+  a.tokens_per_cta = tokens >= 8LL * dev.sms ? 4 : 1;
+  const long long grid = (tokens + a.tokens_per_cta - 1) / a.tokens_per_cta;
   const size_t smem = (size_t)a.tokens_per_cta * rotary_dim * sizeof(float);
   return launch_clusters((unsigned)grid, kThreads, 1, smem, reinterpret_cast<cudaStream_t>(stream),
                          interleaved ? qkv_norm_rope_kernel<true> : qkv_norm_rope_kernel<false>,
