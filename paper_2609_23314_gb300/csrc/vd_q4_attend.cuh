@@ -165,42 +165,9 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
   grid_dependency_wait();
   grid_launch_dependents();
 
-  const int n = __ldcg(a.len + seq);
-  if (n < 0 || n > a.cap) {  // the whole cluster leaves
-    if (rank == 0 && tile == 0 && head == 0 && threadIdx.x == 0)
-      record_status(a.status, kStDeviceLen);
-    return;
-  }
+  // Q: lane (r, c) holds row r of each n-tile, dims k_dim(w, c) .. + 7 for every w.  Loaded
+  // before the length is waited for
   const int row0 = tile * Sh::kRows;
-  const size_t unit_row = (size_t)seq * a.seq_rows + (size_t)head * a.cap;
-  const uint8_t* gk = a.k + unit_row * (kD / 2);
-  const uint8_t* gv = a.v + unit_row * (kD / 2);
-  const uint8_t* gks = a.ks + unit_row * (kD / 16);
-  const uint8_t* gvs = a.vs + unit_row * (kD / 16);
-
-  // this warp's stages: first, first + kWarps, ... below `last`
-  const int stages = (n + kStageKeys - 1) / kStageKeys;
-  const int begin = (int)((long long)stages * rank / a.cluster);
-  const int last = (int)((long long)stages * (rank + 1) / a.cluster);
-  const uint32_t ring = base + warp * Sh::kStages * Sh::kStageBytes;
-  auto fetch = [&](int stage, int slot) {  // lane 0
-    const int key0 = stage * kStageKeys;
-    const int keys = min(kStageKeys, n - key0);
-    const uint32_t codes = (uint32_t)keys * (kD / 2);
-    const uint32_t scales = (uint32_t)((keys + 7) & ~7) * (kD / 16);  // within the capacity
-    const uint32_t dst = ring + slot * Sh::kStageBytes, bar = bars + 8 * slot;
-    mbar_expect_tx(bar, 2 * (codes + scales));
-    bulk_g2s(dst, gk + (size_t)key0 * (kD / 2), codes, bar);
-    bulk_g2s(dst + Sh::kCodeBytes, gv + (size_t)key0 * (kD / 2), codes, bar);
-    bulk_g2s(dst + 2 * Sh::kCodeBytes, gks + (size_t)key0 * (kD / 16), scales, bar);
-    bulk_g2s(dst + 2 * Sh::kCodeBytes + Sh::kScaleBytes, gvs + (size_t)key0 * (kD / 16), scales,
-             bar);
-  };
-  if (lane == 0)
-    for (int i = 0; i < Sh::kStages; ++i)
-      if (begin + warp + i * kWarps < last) fetch(begin + warp + i * kWarps, i);
-
-  // Q: lane (r, c) holds row r of each n-tile, dims k_dim(w, c) .. + 7 for every w
   uint32_t qf[NT][M][4];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
@@ -217,6 +184,39 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
       qf[t][w][2] = x.z;
       qf[t][w][3] = x.w;
     }
+  }
+  const int n = __ldcg(a.len + seq);
+  if (n < 0 || n > a.cap) {  // the whole cluster leaves
+    if (rank == 0 && tile == 0 && head == 0 && threadIdx.x == 0)
+      record_status(a.status, kStDeviceLen);
+    return;
+  }
+  const size_t unit_row = (size_t)seq * a.seq_rows + (size_t)head * a.cap;
+
+  // this warp's stages: first, first + kWarps, ... below `last`
+  const int stages = (n + kStageKeys - 1) / kStageKeys;
+  const int begin = (int)((long long)stages * rank / a.cluster);
+  const int last = (int)((long long)stages * (rank + 1) / a.cluster);
+  const uint32_t ring = base + warp * Sh::kStages * Sh::kStageBytes;
+  // Copy `what` of a stage (codes of K and V, scales of K and V): four lanes issue a stage's
+  // copies together, and in the beginning 4 * kStages lanes those of all stages
+  auto fetch = [&](int stage, int slot, int what) {
+    const int key0 = stage * kStageKeys;
+    const int keys = min(kStageKeys, n - key0);
+    const uint32_t codes = (uint32_t)keys * (kD / 2);
+    const uint32_t scales = (uint32_t)((keys + 7) & ~7) * (kD / 16);  // within the capacity
+    const uint32_t dst = ring + slot * Sh::kStageBytes + (what & 1) * (what < 2 ? Sh::kCodeBytes
+                                                                               : Sh::kScaleBytes) +
+                         (what < 2 ? 0 : 2 * Sh::kCodeBytes);
+    const uint32_t bar = bars + 8 * slot;
+    const uint8_t* src = what == 0 ? a.k : what == 1 ? a.v : what == 2 ? a.ks : a.vs;
+    if (what == 0) mbar_expect_tx(bar, 2 * (codes + scales));
+    bulk_g2s(dst, src + (unit_row + key0) * (what < 2 ? kD / 2 : kD / 16),
+             what < 2 ? codes : scales, bar);
+  };
+  if (lane < 4 * Sh::kStages) {
+    const int stage = begin + warp + (lane >> 2) * kWarps;
+    if (stage < last) fetch(stage, lane >> 2, lane & 3);
   }
 
   float o[NT][2 * M][4];
@@ -316,11 +316,30 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
         for (int e = 0; e < 4; ++e) s[0][t][e] = 0.f;
       const bool in0 = k0 + r < a.B, in1 = k0 + r + 8 < a.B;
       const uint16_t* kr = a.k_new + (new_row + k0 + r) * kD;
+      const uint16_t* vr = a.v_new + (new_row + k0) * kD;
+      uint4 kx[M], ky[M];
 #pragma unroll
       for (int w = 0; w < M; ++w) {
-        uint4 x = make_uint4(0, 0, 0, 0), y = x;
-        if (in0) x = ld_cg16(kr + k_dim<M>(w, c));
-        if (in1) y = ld_cg16(kr + 8 * kD + k_dim<M>(w, c));
+        kx[w] = ky[w] = make_uint4(0, 0, 0, 0);
+        if (in0) kx[w] = ld_cg16(kr + k_dim<M>(w, c));
+        if (in1) ky[w] = ld_cg16(kr + 8 * kD + k_dim<M>(w, c));
+      }
+      uint32_t vx[2 * M][4];  // of every m-tile two dims of tokens 2c, 2c + 1, 2c + 8, 2c + 9
+      // A value that is not finite must not reach the tokens before its own, whose weight
+      // for it is 0: then the products are made one by one, for those that see it.
+      bool odd = false;
+#pragma unroll
+      for (int i = 0; i < 2 * M; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int key = 2 * c + (e & 1) + (e >> 1) * 8;
+          vx[i][e] = k0 + key < keys ? __ldcg(reinterpret_cast<const uint32_t*>(
+                                           vr + (size_t)key * kD + v_dim<M>(i, r)))
+                                     : 0u;
+        }
+#pragma unroll
+      for (int w = 0; w < M; ++w) {
+        const uint4 x = kx[w], y = ky[w];
         const uint32_t f0[4] = {x.x, y.x, x.y, y.y}, f1[4] = {x.z, y.z, x.w, y.w};
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -338,21 +357,11 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
           s[0][t][e] = key <= token ? s[0][t][e] * qs[t][e & 1] : -INFINITY;
         }
       soften(s);
-      const uint16_t* vr = a.v_new + (new_row + k0) * kD;
-      // A value that is not finite must not reach the tokens before its own, whose weight
-      // for it is 0: then the products are made one by one, for those that see it.
-      bool odd = false;
 #pragma unroll
       for (int i = 0; i < 2 * M; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int key = 2 * c + (e & 1) + (e >> 1) * 8;
-          if (k0 + key < keys) {
-            const uint32_t x =
-                __ldcg(reinterpret_cast<const uint32_t*>(vr + (size_t)key * kD + v_dim<M>(i, r)));
-            odd |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
-          }
-        }
+        for (int e = 0; e < 4; ++e)
+          odd |= (vx[i][e] & 0x7f80u) == 0x7f80u || (vx[i][e] & 0x7f800000u) == 0x7f800000u;
       if (__any_sync(kFull, odd)) {
         for (int key = 0; key < 16 && k0 + key < keys; ++key) {
 #pragma unroll
@@ -385,14 +394,7 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
       }
 #pragma unroll
       for (int i = 0; i < 2 * M; ++i) {
-        uint32_t x[4];  // two dims of tokens 2c, 2c + 1, 2c + 8, 2c + 9
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int key = 2 * c + (e & 1) + (e >> 1) * 8;
-          x[e] = k0 + key < keys ? __ldcg(reinterpret_cast<const uint32_t*>(
-                                       vr + (size_t)key * kD + v_dim<M>(i, r)))
-                                 : 0u;
-        }
+        const uint32_t(&x)[4] = vx[i];
         const uint32_t f[4] = {__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[0], x[1], 0x7632),
                                __byte_perm(x[2], x[3], 0x5410), __byte_perm(x[2], x[3], 0x7632)};
 #pragma unroll
@@ -575,9 +577,9 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
       }
     }
     __syncwarp();
-    if (lane == 0 && issued < last) {
+    if (lane < 4 && issued < last) {
       fence_proxy_async_smem();
-      fetch(issued, slot);
+      fetch(issued, slot, lane);
     }
     issued += kWarps;
     if (++slot == Sh::kStages) {
@@ -651,37 +653,64 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
     cluster_sync();
   else
     __syncthreads();
-  // each CTA writes its share of the tile, from all CTAs' results in rank order
+  // Each CTA writes its share of the tile, from all CTAs' results in rank order: first every
+  // CTA's factor for every row, then the sums.
   const uint32_t cta_addr = smem_addr(cta);
   const uint32_t m_addr = smem_addr(stat_m + kWarps * Sh::kRows);
   const uint32_t l_addr = smem_addr(stat_l + kWarps * Sh::kRows);
-  const int total = Sh::kRows * (kD / 4);
   const bool none = n == 0 && !a.k_new;  // no token to attend to
+  float* all_m = part;                   // [cluster][row], over the warps' results
+  float* all_l = all_m + 16 * Sh::kRows;
+  if ((int)threadIdx.x < a.cluster * Sh::kRows) {
+    const int q = threadIdx.x / Sh::kRows, row = threadIdx.x % Sh::kRows;
+    all_m[threadIdx.x] = ld_cluster_f32(mapa(m_addr + 4 * row, q));
+    all_l[threadIdx.x] = ld_cluster_f32(mapa(l_addr + 4 * row, q));
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < Sh::kRows) {
+    const int row = threadIdx.x;
+    float m = -INFINITY, l = 0.f;
+    for (int q = 0; q < a.cluster; ++q) m = fmaxf(m, all_m[q * Sh::kRows + row]);
+    for (int q = 0; q < a.cluster; ++q) {
+      const float mq = all_m[q * Sh::kRows + row];
+      // a CTA without tokens has sums of zero; one whose scores were all NaN has NaN sums
+      const float f = mq == -INFINITY ? 1.f : exp2_approx(mq - m);
+      l = fmaf(all_l[q * Sh::kRows + row], f, l);
+      all_m[q * Sh::kRows + row] = f;
+    }
+    all_l[row] = none ? 0.f : 1.f / l;  // q == 0's, which is read above by this thread alone
+    const int gr = row0 + row;
+    if (a.lse && rank == 0 && gr < a.rows)
+      a.lse[(((size_t)seq * a.B + gr / a.group) * a.heads + head) * a.group + gr % a.group] =
+          none ? -INFINITY : m / kLog2e + logf(l);
+  }
+  __syncthreads();
+  const int total = min(Sh::kRows, a.rows - row0) * (kD / 4);
   for (int i = (int)rank * kThreads + threadIdx.x; i < total; i += kThreads * a.cluster) {
     const int row = i / (kD / 4), dim = i % (kD / 4) * 4;
-    if (row0 + row >= a.rows) break;
-    float m = -INFINITY;
-    for (int q = 0; q < a.cluster; ++q)
-      m = fmaxf(m, ld_cluster_f32(mapa(m_addr + 4 * row, q)));
+    const uint32_t x_addr = cta_addr + 4 * (row * Sh::kPart + dim);
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
-    for (int q = 0; q < a.cluster; ++q) {
-      const float mq = ld_cluster_f32(mapa(m_addr + 4 * row, q));
-      const float f = mq == -INFINITY ? 1.f : exp2_approx(mq - m);
-      const uint32_t x = mapa(cta_addr + 4 * (row * Sh::kPart + dim), q);
-      acc.x = fmaf(ld_cluster_f32(x), f, acc.x);
-      acc.y = fmaf(ld_cluster_f32(x + 4), f, acc.y);
-      acc.z = fmaf(ld_cluster_f32(x + 8), f, acc.z);
-      acc.w = fmaf(ld_cluster_f32(x + 12), f, acc.w);
-      l = fmaf(ld_cluster_f32(mapa(l_addr + 4 * row, q)), f, l);
+    for (int q0 = 0; q0 < a.cluster; q0 += 8) {
+      float4 x[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        if (q0 + q < a.cluster) x[q] = ld_cluster_f32x4(mapa(x_addr, q0 + q));
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        if (q0 + q < a.cluster) {
+          const float f = all_m[(q0 + q) * Sh::kRows + row];
+          acc.x = fmaf(x[q].x, f, acc.x);
+          acc.y = fmaf(x[q].y, f, acc.y);
+          acc.z = fmaf(x[q].z, f, acc.z);
+          acc.w = fmaf(x[q].w, f, acc.w);
+        }
     }
     const int gr = row0 + row;
     const size_t at =
         (((size_t)seq * a.B + gr / a.group) * a.heads + head) * a.group + gr % a.group;
-    const float inv = none ? 0.f : 1.f / l;
+    const float inv = all_l[row];
     *reinterpret_cast<uint2*>(a.out + at * kD + dim) =
         make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-    if (dim == 0 && a.lse) a.lse[at] = none ? -INFINITY : m / kLog2e + logf(l);
   }
   if (a.cluster > 1) cluster_sync();  // no CTA leaves while its results are read
 }
