@@ -85,6 +85,26 @@ vd_status slots_of(const DeviceInfo& dev, int m, const Slots** out) {
   return VD_OK;
 }
 
+// 0, 1: the streaming kernel with tiles of 8 or 16 query rows, 2: the block kernel.  us at
+// 8 KV heads a sequence, 8-row tiles / 16-row tiles / block:
+//   up to 16 rows always stream (8 sequences of 4000 tokens, 16 rows, 22.2 / 19.4 / 33.7;
+//   head_dim 256 38.4 / - / 53.7), more only in one wave (head_dim 256, 8 sequences, 500
+//   tokens, 24 rows 21.2 / - / 18.5) and up to 32 rows (8 sequences of 4000 tokens 37.4 / 31.3 /
+//   34.1) or with little work (one sequence, 500 tokens, 128 rows 9.0 / 9.0 / 13.5, 4000
+//   tokens, 64 rows 15.0 / 13.6 / 16.6, 128 rows 22.9 / 19.6 / 18.8);
+//   8-row tiles, which read the cache once for each, with little work (one sequence of 4000
+//   tokens, 32 rows 11.0 / 13.2, 64 rows 15.0 / 13.6; 32000 tokens, 16 rows 38.1 / 31.9).
+int choose_kernel(int m, long long rows, long long units, long long capacity, const Slots& slots) {
+  const long long tiles8 = (rows + 7) / 8;
+  const int kind =
+      rows <= 8 || units * tiles8 * capacity <= (1 << 17) ? 0 : 1;
+  const long long ctas = units * ((rows + kKernel[m][kind].rows - 1) / kKernel[m][kind].rows);
+  if (rows <= 16) return kind;
+  if (ctas <= slots.at[kind][0] && (rows <= 32 || units * rows * capacity <= (1 << 21)))
+    return kind;
+  return 2;
+}
+
 bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
 }  // namespace
@@ -117,7 +137,7 @@ extern "C" vd_status vd_q4_attend(const vd_q4_cache* c, int32_t layer, const voi
   if (r != VD_OK) return r;
 
   const int want = env_int("VD_Q4_KERNEL", -1);
-  const int kind = want >= 0 && want < kKinds ? want : rows > 24 ? 2 : rows > 8 ? 1 : 0;
+  const int kind = want >= 0 && want < kKinds ? want : choose_kernel(m, rows, units, c->capacity, *slots);
   const Kernel& k = kKernel[m][kind];
   AttendArgs a;
   const size_t unit0 = (size_t)layer * c->n_kv_head * c->capacity;
@@ -145,9 +165,17 @@ extern "C" vd_status vd_q4_attend(const vd_q4_cache* c, int32_t layer, const voi
   a.scale = scale;
   a.wait_limit = wait_limit();
   const long long base = units * a.tiles;
+  // The largest cluster that runs in one wave and leaves each CTA enough tokens to pay for
+  // the join; two streaming CTAs run on an SM, and clusters of 16, which do not fill the
+  // GPU's groups of SMs, have to gain more.  us, C = 4, 8, 16: one sequence, 8 KV heads of
+  // 500 tokens 5.6, 5.8, 7.4; 5 sequences, 3 heads, 2500 tokens 7.7, 8.2, 17.8; one
+  // sequence, 8 heads, 4096 tokens 10.0, 7.9, 8.3, 32000 tokens 44, 25, 22.3; two
+  // sequences, 131000 tokens 164, 132, 109.
   int e = 0;
-  const int least = kind == 2 ? 128 : kStageKeys * kWarps;  // tokens that a CTA is worth
-  while (e < 4 && (base << (e + 1)) <= slots->at[kind][e + 1] && c->capacity >= least << (e + 1))
+  const int least[5] = {0, 128, 128, kind == 2 ? 128 : 512, kind == 2 ? 128 : 2048};
+  while (e < 4 && slots->at[kind][e + 1] > 0 &&
+         (base << (e + 1)) <= slots->at[kind][kind < 2 && e == 3 ? 0 : e + 1] &&
+         c->capacity >= least[e + 1] << (e + 1))
     ++e;
   const int want_cluster = env_int("VD_Q4_CLUSTER", 0);
   for (int i = 0; i < 5; ++i)

@@ -432,6 +432,13 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
       break;
     }
     const int left = n - stage * kStageKeys;  // tokens of this stage, at least 1
+    if (left < kStageKeys) {  // whatever lies behind the last token counts as zero
+      const uint32_t scales = at + 2 * Sh::kCodeBytes + Sh::kScaleBytes;
+      for (int i = left * 2 * M + 2 * lane; i < Sh::kScaleBytes; i += 64)
+        asm volatile("st.shared.u16 [%0], %1;" ::"r"(scales + i), "h"((unsigned short)0)
+                     : "memory");
+      __syncwarp();
+    }
     float s[2][NT][4];
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
@@ -546,7 +553,6 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
         for (int e = 0; e < 4; ++e) {
           sb[e] = ld_shared_u8(at + 2 * Sh::kCodeBytes + Sh::kScaleBytes + prow[e] * (2 * M) +
                                group);
-          if (left < kStageKeys && prow[e] >= left) sb[e] = 0;  // whatever lies there
         }
         s01 = sb[0] * 0x80u + sb[1] * 0x800000u;
         s23 = sb[2] * 0x80u + sb[3] * 0x800000u;

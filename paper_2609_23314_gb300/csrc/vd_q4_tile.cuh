@@ -105,6 +105,13 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, unsigne
   return ok;
 }
 
+// The largest of three, NaN left aside like fmaxf.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
 // One arrival for a warp: 128 single ones would take the barrier's word in turn.
 __device__ __forceinline__ void warp_arrive(uint32_t bar) {
   __syncwarp();
@@ -386,7 +393,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
         }
         float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int j = 0; j < kHalf; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(s[j]));
+        for (int j = 0; j < kHalf; j += 2)
+          m4[(j >> 1) & 3] =
+              max3(m4[(j >> 1) & 3], __uint_as_float(s[j]), __uint_as_float(s[j + 1]));
         float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * c;
         // with P over S: both halves have read their scores before either writes weights
         if (Sh::kAlias) tc_fence_before();
