@@ -493,9 +493,12 @@ def vd_running_sum_init(cache: Cache, running_sum, stream=None) -> None:
 
 def _on_current(device):
     """Kernels launch on the current device: refuse tensors of another one."""
-    if device.type == "cuda" and device.index != _torch().cuda.current_device():
+    torch = _torch()
+    if device.type != "cuda" or not torch.cuda.is_initialized():
+        return  # CPU tensors never reach a launch
+    if device.index != torch._C._cuda_getDevice():
         raise ValueError(f"the tensors live on {device}, the current device is "
-                         f"cuda:{_torch().cuda.current_device()}")
+                         f"cuda:{torch.cuda.current_device()}")
 
 
 def vd_q4_append(cache: Q4Cache, k_new, v_new, B: int, stream=None) -> None:

@@ -16,8 +16,8 @@
 // head dims on the 16-row side of m16n8k16, so that 8 query rows fill a tile: decode
 // has 1 to 8 rows (the query heads that share a KV head) per token.  K and V go from
 // codes to fp16 in registers (exact), Q goes to fp16 with each row scaled by a power of
-// two (exact but for values 2^-27 of the row's largest and below), sums are fp32, and P
-// is rounded to fp16 (2^-11 of a weight, its error averaged over the tokens).
+// two (QueryScale), sums are fp32, and P is rounded to fp16 (2^-11 of a weight, its error
+// averaged over the tokens).
 #pragma once
 
 #include <cstdint>
@@ -87,6 +87,23 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4],
         "{%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// A query row's power of two: its largest magnitude goes to [2^-9, 2^-8) (a query of 2^118
+// and more to at most 1), exact in bf16, so that no finite key row makes a score overflow.
+// For fp16 kTo16 more, which rounds what lies below 2^-19 of the row's largest value to
+// 2^-29 of it.
+constexpr float kTo16 = 0x1p13f, kFrom16 = 0x1p-13f;
+
+struct QueryScale {
+  uint32_t up;  // the factor in bf16, twice
+  float down;   // its inverse
+};
+
+// top: the row's largest magnitude as bf16 bits
+__device__ __forceinline__ QueryScale scale_of(uint32_t top) {
+  const uint32_t ex = top ? min(244u, max(1u, top >> 7)) : 118u;
+  return {((245u - ex) << 7) * 0x00010001u, __uint_as_float((ex + 9u) << 23)};
 }
 
 __device__ __forceinline__ uint32_t ld_shared_u8(uint32_t addr) {
@@ -275,8 +292,8 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
       }
   };
 
-  // Each row of Q times a power of two that takes its largest value to [1, 2), exact in
-  // bf16; qs: what a column's scores have to be multiplied by for log2 units
+  // Each row of Q times its power of two; qs: what a column's scores have to be multiplied by
+  // for log2 units
   float qs[NT][2];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
@@ -290,14 +307,14 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
       }
     top = max(top, __shfl_xor_sync(kFull, top, 1));
     top = max(top, __shfl_xor_sync(kFull, top, 2));
-    const uint32_t ex = min(253u, max(1u, top >> 7));  // biased exponent
-    const uint32_t up = ((254 - ex) << 7) * 0x00010001u;
+    const QueryScale f = scale_of(top);
+    const uint32_t up = f.up;
 #pragma unroll
     for (int w = 0; w < M; ++w)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(qf[t][w][e]) : "r"(up));
-    const float down = __uint_as_float(ex << 23) * (a.scale * kLog2e);
+    const float down = f.down * (a.scale * kLog2e);
     qs[t][0] = __shfl_sync(kFull, down, 8 * c);
     qs[t][1] = __shfl_sync(kFull, down, 8 * c + 4);
   }
@@ -403,18 +420,18 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
     }
   }
 
-  // Q to fp16, each row's largest value now in [2^13, 2^14)
+  // Q to fp16
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    qs[t][0] *= 0x1p-13f;
-    qs[t][1] *= 0x1p-13f;
+    qs[t][0] *= kFrom16;
+    qs[t][1] *= kFrom16;
 #pragma unroll
     for (int w = 0; w < M; ++w)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const uint32_t x = qf[t][w][e];
-        qf[t][w][e] = pack_f16(__uint_as_float(x << 16) * 0x1p13f,
-                               __uint_as_float(x & 0xffff0000u) * 0x1p13f);
+        qf[t][w][e] = pack_f16(__uint_as_float(x << 16) * kTo16,
+                               __uint_as_float(x & 0xffff0000u) * kTo16);
       }
   }
 

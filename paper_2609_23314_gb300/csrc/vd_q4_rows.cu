@@ -15,7 +15,7 @@ vd_status validate_q4(const vd_q4_cache* c) {
   if (c->n_seq < 1 || c->n_layer < 1 || c->n_kv_head < 1 || c->capacity < 1 || c->head_dim < 1)
     return VD_ERR_INVALID_ARG;
   if (c->head_dim % 32 != 0 || c->capacity % 8 != 0) return VD_ERR_ALIGNMENT;
-  if (c->head_dim > 256) return VD_ERR_UNSUPPORTED;
+  if (c->head_dim > 256 || c->capacity > (1 << 30)) return VD_ERR_UNSUPPORTED;
   if ((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v) |
        reinterpret_cast<uintptr_t>(c->k_scale) | reinterpret_cast<uintptr_t>(c->v_scale)) & 15u)
     return VD_ERR_ALIGNMENT;

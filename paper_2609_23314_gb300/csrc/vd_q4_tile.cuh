@@ -58,10 +58,10 @@ struct TileShape {
   static constexpr int kBars = kSwap + 4 * kTileRows * 4;
   static constexpr int kNumBars = 18 + (kKeyWarps + kValueWarps) * kRaw;
   static constexpr int kMisc = kBars + kNumBars * 8;  // tensor memory address, flags
-  // The base is rounded up to 1024.  Never two CTAs on an SM: the second would wait for
-  // tensor memory, and the first, in one cluster with it, for the second.
+  // The base is rounded up to 1024.  So much that no other CTA with tensor memory fits on the
+  // SM: it would wait for this one's, and, in one cluster with it, this one for it.
   static constexpr int kNeed = kMisc + 16 + 1024;
-  static constexpr int kTotal = kNeed > 120 * 1024 ? kNeed : 120 * 1024;
+  static constexpr int kTotal = kNeed > 200 * 1024 ? kNeed : 200 * 1024;
   // columns of tensor memory: two S, P, O, Q (P and Q 16-bit pairs).  At head_dim 256 there
   // is no room for P, which then takes the lower half of its S
   static constexpr bool kAlias = M == 8;
@@ -321,7 +321,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
     };
     if (count > 0) {
       const uint32_t q_col = lanes + Sh::kColQ + half * 8 * M;
-      // Q: scaled so that the row's largest value lies in [1, 2), for bf16, or in [2^13, 2^14)
+      // Q as in the streaming kernel (scale_of)
       float unit_scale;
       bool ok;
       {
@@ -341,15 +341,15 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
         float both = (float)top;
         ok = exchange(both, 0);
         top = (uint32_t)both;
-        const uint32_t ex = top ? min(253u, max(1u, top >> 7)) : 127u;
-        const uint32_t up = ((254 - ex) << 7) * 0x00010001u;
-        unit_scale = __uint_as_float(ex << 23) * (a.scale * kLog2e);
+        const QueryScale qs = scale_of(top);
+        const uint32_t up = qs.up;
+        unit_scale = qs.down * (a.scale * kLog2e);
 #pragma unroll
         for (int i = 0; i < 8 * M; ++i) {
           asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(w[i]) : "r"(up));
           if (fresh == 0)
-            w[i] = pack_f16(__uint_as_float(w[i] << 16) * 0x1p13f,
-                            __uint_as_float(w[i] & 0xffff0000u) * 0x1p13f);
+            w[i] = pack_f16(__uint_as_float(w[i] << 16) * kTo16,
+                            __uint_as_float(w[i] & 0xffff0000u) * kTo16);
         }
         __syncwarp();
 #pragma unroll
@@ -370,8 +370,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
             tmem_ld(q_col + 8 * j, w);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-              w[e] = pack_f16(__uint_as_float(w[e] << 16) * 0x1p13f,
-                              __uint_as_float(w[e] & 0xffff0000u) * 0x1p13f);
+              w[e] = pack_f16(__uint_as_float(w[e] << 16) * kTo16,
+                              __uint_as_float(w[e] & 0xffff0000u) * kTo16);
             tmem_st8(q_col + 8 * j, w);
           }
           tmem_wait_st();
@@ -380,7 +380,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
         }
         const bool is_new = i < fresh;
         // not 0, which would make a masked score a NaN
-        const float c = fmaxf(is_new ? unit_scale : unit_scale * 0x1p-13f, 0x1p-126f);
+        const float c = fmaxf(is_new ? unit_scale : unit_scale * kFrom16, 0x1p-126f);
         uint32_t s[kHalf];
         tmem_ld(s_col + half * kHalf, s);
         // tokens behind this row's last one do not count

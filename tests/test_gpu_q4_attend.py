@@ -149,6 +149,22 @@ def test_queries_of_any_size(factor, B):
 
 
 @pytest.mark.usefixtures("route")
+@pytest.mark.parametrize("B", [2, 40])
+def test_new_keys_near_the_largest_number(B):
+    """Scores whose products with small queries are ordinary numbers."""
+    c, q, k_new, v_new = state([0, 33], 1, 2, 4, 128, B, 40)
+    check(c, (q.double() * 1e-37).to(torch.bfloat16),
+          (k_new.double() * 5e37).to(torch.bfloat16), v_new, scale=0.02)
+
+
+@pytest.mark.usefixtures("route")
+@pytest.mark.parametrize("B", [2, 40])
+def test_queries_near_the_largest_number(B):
+    c, q, k_new, v_new = state([70, 33], 1, 2, 4, 128, B, 72)
+    check(c, (q.double() * 1e36).to(torch.bfloat16), k_new, v_new, scale=8e-38)
+
+
+@pytest.mark.usefixtures("route")
 @pytest.mark.parametrize("B", [3, 40])
 @pytest.mark.parametrize("d", [96, 128])
 @pytest.mark.parametrize("value", [float("nan"), float("inf")])

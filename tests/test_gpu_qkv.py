@@ -168,3 +168,16 @@ def test_together():
     for t, old in zip((c.k, c.v, c.k_scale, c.v_scale), before):
         idx = kept.long()[..., None].expand(-1, -1, -1, -1, t.shape[-1])
         assert torch.equal(t[:, :, :, :N], torch.gather(old, 3, idx))
+
+
+def test_readme_example_of_the_4_bit_cache():
+    """The README's examples run as written, one after the other."""
+    import os
+    import re
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    with open(os.path.join(root, "README.md")) as f:
+        blocks = re.findall(r"```python\n(.*?)```", f.read(), flags=re.S)
+    names = {}
+    exec(compile("\n".join(blocks[:2]), "README.md", "exec"), names)
+    assert names["q4"].len.tolist() == [names["N"]] * names["n_seq"]
+    assert bool(torch.isfinite(names["out"]).all())

@@ -29,7 +29,7 @@ def _cache(n_seq=1, n_layer=1, n_kv_head=2, head_dim=64, capacity=128, k=0x1000)
 @pytest.mark.parametrize("fields,code", [
     (dict(k=0), 1), (dict(vs=0), 1), (dict(ln=0), 1), (dict(n_layer=0), 1), (dict(capacity=0), 1),
     (dict(head_dim=0), 1), (dict(head_dim=48), 2), (dict(capacity=129), 2), (dict(k=0x1008), 2),
-    (dict(vs=0x4001), 2), (dict(head_dim=288), 3), (dict(n_seq=1 << 20, n_layer=64), 3),
+    (dict(vs=0x4001), 2), (dict(head_dim=288), 3), (dict(capacity=(1 << 30) + 8), 3), (dict(n_seq=1 << 20, n_layer=64), 3),
 ])
 def test_bad_cache(lib, fields, code):
     c = _q4(**fields)
@@ -116,3 +116,15 @@ def test_the_binding_checks_its_tensors():
         vd.vd_qkv_norm_rope(qkv, q, bf(2, 3, 1, 1, 64), new)
     with pytest.raises(ValueError, match="contiguous"):
         vd.vd_qkv_norm_rope(bf(2, 1, 12, 128)[..., :64], q, new, new)
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """A call launches on the current device; tensors of another one do not reach it."""
+    import paper_2609_23314_gb300 as vd
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    vd._on_current(torch.device("cuda", 0))
+    vd._on_current(torch.device("cpu"))
+    with pytest.raises(ValueError, match="current device"):
+        vd._on_current(torch.device("cuda", 1))
