@@ -18,6 +18,10 @@
 // codes to fp16 in registers (exact), Q goes to fp16 with each row scaled by a power of
 // two (QueryScale), sums are fp32, and P is rounded to fp16 (2^-11 of a weight, its error
 // averaged over the tokens).
+// Bound by instruction issue: about 22 warp instructions a token at head_dim 128, 5.3 ns a
+// token and SM (its 144 bytes take 3.2 at the copy peak).  us: 512 KV heads around 4096
+// tokens 62.3 (3.7 TB/s), 16 heads of 131000 tokens 107.5 (2.8 TB/s; the copies alone 48),
+// 8 heads of 4096 tokens 8.0.
 #pragma once
 
 #include <cstdint>
