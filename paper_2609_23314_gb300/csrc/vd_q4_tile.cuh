@@ -21,6 +21,12 @@
 // The new tokens' tiles come first, in bf16, then Q is rewritten in fp16 (rows scaled by
 // powers of two, as in the streaming kernel) for the cached ones.  A cluster splits the
 // tiles of a unit and joins the results through distributed shared memory.
+//
+// Per tile of 128 tokens at head_dim 128: the products take 1024 cycles at 4096
+// multiply-adds a cycle, the roles issue 5700 warp instructions, 1425 a scheduler.  us: 512 new
+// tokens over 32768 cached ones, 8 KV heads of 4 query heads, 352 alone and 384 in a row
+// (277 GFLOP: 790 and 720 TFLOP/s; without the softmax 280, without the unpacking 263,
+// without the products 330); 128 new tokens over 2048 18.5.
 #pragma once
 
 #include <cstdint>

@@ -4,7 +4,9 @@
 // Per head of a query or key,  y = x * w / sqrt(mean(x^2) + eps),  and its first
 // rotary_dim values turn in pairs (a, b) -> (a cos t - b sin t, b cos t + a sin t) by
 // t = position * inv_freq.  Values are copied.  One read and one write of every value:
-// bound by DRAM for prompts, by the latency of one dependent load for single tokens.
+// bound by DRAM for prompts (16384 tokens of 48 heads of 128 values 69.7 us, 85 % of the copy
+// peak; 82.5 without the early load of the next head), by launch and latency for single
+// tokens (4.1 us in a graph).
 #include <cuda_runtime.h>
 
 #include <climits>
@@ -207,6 +209,8 @@ extern "C" vd_status vd_qkv_norm_rope(const void* qkv, int32_t n_seq, int32_t B,
   a.lanes = 1;
   while (a.lanes < a.items) a.lanes <<= 1;
   a.eps = eps;
+  // four tokens share a CTA's sines where there are enough (us at 16384 tokens: 2 tokens 74.4,
+  // 4 69.7, 8 72.6)
   a.tokens_per_cta = tokens >= 8LL * dev.sms ? 4 : 1;
   const long long grid = (tokens + a.tokens_per_cta - 1) / a.tokens_per_cta;
   const size_t smem = (size_t)a.tokens_per_cta * rotary_dim * sizeof(float);
