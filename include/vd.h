@@ -388,7 +388,8 @@ vd_status vd_q4_unpack(const vd_q4_cache* src, int32_t layer0, const vd_cache* d
  *   lse_out       nullable fp32 device [n_seq][B][n_q_head]: log sum_j exp(s_j).
  * A token that sees no row (len 0, no new rows) gets out = 0 and lse = -inf.
  * A sequence with len out of [0, capacity] gets no output (VD_ERR_DEVICE_LEN).
- * The cache is not modified.  Scores, softmax statistics and sums are fp32; a weight
+ * The cache is not modified; of slots >= len at most the scale bytes up to the next
+ * multiple of 8 are read, and ignored.  Scores, softmax statistics and sums are fp32; a weight
  * is rounded to fp16 (bf16 for the new rows) before it multiplies its value.  out must
  * not overlap the inputs.  VD_ERR_TIMEOUT: the outputs are unspecified. */
 vd_status vd_q4_attend(const vd_q4_cache* c, int32_t layer, const void* q, int32_t n_q_head,

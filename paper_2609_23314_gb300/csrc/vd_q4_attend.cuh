@@ -76,6 +76,16 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
   return r;
 }
 
+// c = a b in fp16, and c += a b.
+__device__ __forceinline__ void mma_16816_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0,
+                                                uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+      "{%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+
 template <bool BF16>
 __device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0,
                                           uint32_t b1) {
@@ -251,25 +261,28 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[t][i][e] = 0.f;
   }
-  // Takes the scores of 16 or 32 tokens (in log2 units) into the running state and turns
-  // them into weights.  The maximum is renewed only where a score exceeds it.
-  auto soften = [&](auto& s) {
+  // Takes the scores of 16 or 32 tokens (qs times them: log2 units) into the running state and
+  // turns them into weights.  The maximum is renewed only where a score exceeds it.
+  auto soften = [&](auto& s, const float (&qs)[NT][2]) {
     constexpr int kChunks = sizeof(s) / sizeof(s[0]);
+    float top[NT][2];
     bool above = false;
 #pragma unroll
-    for (int g = 0; g < kChunks; ++g)
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+      for (int e = 0; e < 2; ++e) {
+        float m = fmaxf(s[0][t][e], s[0][t][e + 2]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) above |= s[g][t][e] > mx[t][e & 1];
+        for (int g = 1; g < kChunks; ++g) m = fmaxf(m, fmaxf(s[g][t][e], s[g][t][e + 2]));
+        top[t][e] = m * qs[t][e];
+        above |= top[t][e] > mx[t][e];
+      }
     if (__any_sync(kFull, above)) {
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float m = mx[t][e];
-#pragma unroll
-          for (int g = 0; g < kChunks; ++g) m = fmaxf(m, fmaxf(s[g][t][e], s[g][t][e + 2]));
+          float m = fmaxf(mx[t][e], top[t][e]);
 #pragma unroll
           for (int off = 4; off < 32; off <<= 1) m = fmaxf(m, __shfl_xor_sync(kFull, m, off));
           const float f = m == -INFINITY ? 1.f : exp2_approx(mx[t][e] - m);
@@ -286,11 +299,11 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float m = mx[t][e] == -INFINITY ? 0.f : mx[t][e];
+        const float shift = mx[t][e] == -INFINITY ? 0.f : -mx[t][e];
 #pragma unroll
         for (int g = 0; g < kChunks; ++g) {
-          s[g][t][e] = exp2_approx(s[g][t][e] - m);
-          s[g][t][e + 2] = exp2_approx(s[g][t][e + 2] - m);
+          s[g][t][e] = exp2_approx(fmaf(s[g][t][e], qs[t][e], shift));
+          s[g][t][e + 2] = exp2_approx(fmaf(s[g][t][e + 2], qs[t][e], shift));
           sum[t][e] += s[g][t][e] + s[g][t][e + 2];
         }
       }
@@ -318,7 +331,8 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(qf[t][w][e]) : "r"(up));
-    const float down = f.down * (a.scale * kLog2e);
+    // not 0, which would make a masked score a NaN
+    const float down = fmaxf(f.down * (a.scale * kLog2e), 0x1p-126f);
     qs[t][0] = __shfl_sync(kFull, down, 8 * c);
     qs[t][1] = __shfl_sync(kFull, down, 8 * c + 4);
   }
@@ -375,9 +389,9 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
           const int row = row0 + 8 * t + 2 * c + (e & 1), key = k0 + r + (e >> 1) * 8;
           // rows behind the last see what the last one sees
           const int token = min(row, a.rows - 1) / a.group;
-          s[0][t][e] = key <= token ? s[0][t][e] * qs[t][e & 1] : -INFINITY;
+          if (key > token) s[0][t][e] = -INFINITY;
         }
-      soften(s);
+      soften(s, qs);
 #pragma unroll
       for (int i = 0; i < 2 * M; ++i)
 #pragma unroll
@@ -427,8 +441,8 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
   // Q to fp16
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    qs[t][0] *= kFrom16;
-    qs[t][1] *= kFrom16;
+    qs[t][0] = fmaxf(qs[t][0] * kFrom16, 0x1p-126f);
+    qs[t][1] = fmaxf(qs[t][1] * kFrom16, 0x1p-126f);
 #pragma unroll
     for (int w = 0; w < M; ++w)
 #pragma unroll
@@ -463,10 +477,6 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
     float s[2][NT][4];
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[g][t][e] = 0.f;
       const int pr = 16 * g + (r & 6) + ((r ^ (r >> 1)) & 1);  // rows pr and pr + 8
       uint32_t w0[M], w1[M], sc0[M], sc1[M];
       const uint32_t k0 = at + pr * (16 * M), k1 = k0 + 8 * 16 * M;
@@ -516,14 +526,13 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
         const uint32_t f0[4] = {x[0], y[0], x[1], y[1]}, f1[4] = {x[2], y[2], x[3], y[3]};
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          mma_16816<false>(s[g][t], f0, qf[t][w][0], qf[t][w][1]);
+          if (w == 0)
+            mma_16816_first(s[g][t], f0, qf[t][w][0], qf[t][w][1]);
+          else
+            mma_16816<false>(s[g][t], f0, qf[t][w][0], qf[t][w][1]);
           mma_16816<false>(s[g][t], f1, qf[t][w][2], qf[t][w][3]);
         }
       }
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[g][t][e] *= qs[t][e & 1];
       if (left < kStageKeys) {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -532,7 +541,7 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
             if (pr + (e >> 1) * 8 >= left) s[g][t][e] = -INFINITY;
       }
     }
-    soften(s);
+    soften(s, qs);
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       uint32_t p[NT][2];
