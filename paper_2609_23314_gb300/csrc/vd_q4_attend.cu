@@ -155,7 +155,6 @@ extern "C" vd_status vd_q4_attend(const vd_q4_cache* c, int32_t layer, const voi
   a.status = dev.status;
   a.seq_rows = (size_t)c->n_layer * c->n_kv_head * c->capacity;
   a.seq_new_rows = (size_t)c->n_layer * c->n_kv_head * B;
-  a.n_seq = c->n_seq;
   a.heads = c->n_kv_head;
   a.group = group;
   a.B = B;

@@ -41,7 +41,7 @@ struct AttendArgs {
   unsigned* status;
   size_t seq_rows;      // rows between two sequences of the cache
   size_t seq_new_rows;  // and of the new rows
-  int n_seq, heads, group, B, cap;
+  int heads, group, B, cap;
   int rows;    // query rows per KV head: B * group
   int tiles;   // row tiles of a KV head
   int cluster;

@@ -23,15 +23,15 @@
 // tiles of a unit and joins the results through distributed shared memory.
 //
 // Per tile of 128 tokens at head_dim 128: the products take 1024 cycles at 4096
-// multiply-adds a cycle, the roles issue 5700 warp instructions, 1425 a scheduler.  us: 512 new
-// tokens over 32768 cached ones, 8 KV heads of 4 query heads, 352 alone and 384 in a row
-// (277 GFLOP: 790 and 720 TFLOP/s; without the softmax 280, without the unpacking 263,
-// without the products 330); 128 new tokens over 2048 18.5.
+// multiply-adds a cycle, the roles issue 5700 warp instructions, 1425 a scheduler, from code
+// that no longer fits the instruction cache (14 % of the stalls): K and V share theirs (385
+// with one each).  us: 512 new tokens over 32768 cached ones, 8 KV heads of 4 query heads, 343
+// (277 GFLOP, 810 TFLOP/s); without the softmax 280, without the unpacking 263, without the
+// products 330 of a 352 us form; 128 new tokens over 2048 18.0.
 #pragma once
 
 #include <cstdint>
 #include <cuda_runtime.h>
-#include <type_traits>
 
 #include "vd_device.cuh"
 #include "vd_q4.cuh"
@@ -146,10 +146,10 @@ __device__ __forceinline__ uint32_t tile_at(uint32_t dst, int key, int chunk) {
 }
 
 // New tokens' rows of a slice: bf16 as they are, zeros behind the last one (left: rows that
-// are there).  FINITE: what is not finite becomes zero too; returns whether there was any.
-template <int M, bool FINITE>
+// are there).  finite: what is not finite becomes zero too; returns whether there was any.
+template <int M>
 __device__ __forceinline__ bool copy_rows(const uint16_t* src, int left, uint32_t dst, int first,
-                                          int count, int lane) {
+                                          int count, int lane, bool finite) {
   constexpr int kD = 32 * M;
   constexpr int kAhead = M <= 4 ? 4 : 2;  // chunks of 16 bytes loaded together
   bool found = false;
@@ -166,7 +166,7 @@ __device__ __forceinline__ bool copy_rows(const uint16_t* src, int left, uint32_
     for (int u = 0; u < kAhead; ++u) {
       const int j = j0 + 32 * u, key = first + j / (kD / 8), chunk = j % (kD / 8);
       if (j >= count * (kD / 8)) break;
-      if (FINITE) {
+      if (finite) {
         uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -476,87 +476,81 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
     }
   } else if (warp < kProductWarp) {
     // K's warps or V's: their slices of the tiles, as the buffers become free
-    auto slices = [&](auto part_) {
-      constexpr int kPart = decltype(part_)::value;  // 0: K, 1: V
-      constexpr int kWarpsOf = kPart ? kValueWarps : kKeyWarps;
-      constexpr int kBufs = kPart ? kValueBufs : kKeyBufs;
-      constexpr int kUnits = ((kKeys / 8 + kWarpsOf - 1) / kWarpsOf * 8 * M + 31) / 32;
-      const int lane = threadIdx.x & 31, which = warp - kSoftWarps;
-      const Slice<kKeys> slice(which - kPart * kKeyWarps, kWarpsOf);
-      const size_t at = (size_t)seq * a.seq_rows + (size_t)head * a.cap +
-                        (size_t)cached0 * kKeys + slice.first;
-      const uint8_t* codes = (kPart ? a.v : a.k) + at * (kD / 2);
-      const uint8_t* scales = (kPart ? a.vs : a.ks) + at * (kD / 16);
-      const uint16_t* fresh_rows = (kPart ? a.v_new : a.k_new) + (new_row + (size_t)t0 * kKeys) * kD;
-      const uint32_t raw = base + Sh::kRing + kPart * Sh::kRawCodes + slice.first * (kD / 2);
-      const uint32_t raw_scales = base + Sh::kRing + 2 * Sh::kRawCodes + kPart * Sh::kRawScales +
-                                  slice.first * (kD / 16);
-      const uint32_t bar = raw_full + 8 * kRaw * which;
-      const int cached = count - fresh, left = n - cached0 * kKeys - slice.first;
-      // tokens of the slice in the CTA's cached tile ci
-      auto there = [&](int ci) { return min(slice.count, max(0, left - ci * kKeys)); };
-      auto fetch = [&](int ci) {
-        const int keys = there(ci), slot = ci % kRaw;
-        if (keys == 0) return;
-        const uint32_t scale_bytes = (uint32_t)((keys + 7) & ~7) * (kD / 16);  // within the capacity
-        mbar_expect_tx(bar + 8 * slot, keys * (kD / 2) + scale_bytes);
-        bulk_g2s(raw + slot * Sh::kRawBytes, codes + (size_t)ci * kKeys * (kD / 2), keys * (kD / 2),
-                 bar + 8 * slot);
-        bulk_g2s(raw_scales + slot * Sh::kRawBytes, scales + (size_t)ci * kKeys * (kD / 16),
-                 scale_bytes, bar + 8 * slot);
-      };
-      if (lane == 0)
-        for (int ci = 0; ci < min(kRaw, cached); ++ci) fetch(ci);
-      int fetched = min(kRaw, cached);
-      if (kPart && count > 0) warp_arrive(full);  // of the tile before the first
-      bool ok = true;
-      for (int i = 0; i < count; ++i) {
-        const uint32_t dst =
-            base + (kPart ? kKeyBufs + i % kValueBufs : i % kKeyBufs) * Sh::kTileBytes;
-        CodeSlice<M, kUnits> x;
-        if (i >= fresh) {
-          const int ci = i - fresh, slot = ci % kRaw, keys = there(ci);
-          if (keys > 0)
-            ok = warp_wait(bar + 8 * slot, (ci / kRaw) & 1, a.status, a.wait_limit, dead);
-          if (!ok) break;
-          x.load(raw + slot * Sh::kRawBytes, raw_scales + slot * Sh::kRawBytes, keys, lane);
-          __syncwarp();
-          if (fetched < cached) {
-            if (lane == 0) {
-              fence_proxy_async_smem();
-              fetch(fetched);
-            }
-            ++fetched;
-          }
-        }
-        if (i >= kBufs)
-          ok = warp_wait((kPart ? o_done : s_done) + 8 * (i % kBufs), (i / kBufs + 1) & 1, a.status,
-                         a.wait_limit, dead);
-        if (!ok) break;
-        if (i < fresh) {
-          const uint16_t* src = fresh_rows + (size_t)i * kKeys * kD;
-          // what is not finite in V is added at the end, to the rows that see it
-          if (copy_rows<M, kPart != 0>(src, keys_new - (t0 + i) * kKeys, dst, slice.first,
-                                       slice.count, lane))
-            *odd = 1;
-        } else {
-          x.unpack(dst, slice.first, slice.count, lane);
-        }
-        fence_proxy_async_smem();
-        warp_arrive(full + 8 * ((i + kPart) & 3));
-        if (!kPart && i == count - 1) warp_arrive(full + 8 * (count & 3));  // there is none
-      }
-      // nothing may be in flight when the ring's memory is used again
-      if (!ok && lane == 0)
-        for (int ci = max(0, fetched - kRaw); ci < fetched; ++ci)
-          if (there(ci) > 0)
-            mbar_wait(bar + 8 * (ci % kRaw), (ci / kRaw) & 1, a.status, kWaitLimit);
-      __syncwarp();
+    // one code for both: the roles share the instruction cache
+    constexpr int kUnits = ((kKeys / 8 + kValueWarps - 1) / kValueWarps * 8 * M + 31) / 32;
+    const int lane = threadIdx.x & 31, which = warp - kSoftWarps;
+    const int part = which >= kKeyWarps;  // 0: K, 1: V
+    const int bufs = part ? kValueBufs : kKeyBufs;
+    const Slice<kKeys> slice(part ? which - kKeyWarps : which, part ? kValueWarps : kKeyWarps);
+    const size_t at = (size_t)seq * a.seq_rows + (size_t)head * a.cap +
+                      (size_t)cached0 * kKeys + slice.first;
+    const uint8_t* codes = (part ? a.v : a.k) + at * (kD / 2);
+    const uint8_t* scales = (part ? a.vs : a.ks) + at * (kD / 16);
+    const uint16_t* fresh_rows = (part ? a.v_new : a.k_new) + (new_row + (size_t)t0 * kKeys) * kD;
+    const uint32_t raw = base + Sh::kRing + part * Sh::kRawCodes + slice.first * (kD / 2);
+    const uint32_t raw_scales = base + Sh::kRing + 2 * Sh::kRawCodes + part * Sh::kRawScales +
+                                slice.first * (kD / 16);
+    const uint32_t bar = raw_full + 8 * kRaw * which;
+    const int cached = count - fresh, left = n - cached0 * kKeys - slice.first;
+    // tokens of the slice in the CTA's cached tile ci
+    auto there = [&](int ci) { return min(slice.count, max(0, left - ci * kKeys)); };
+    auto fetch = [&](int ci) {
+      const int keys = there(ci), slot = ci % kRaw;
+      if (keys == 0) return;
+      const uint32_t scale_bytes = (uint32_t)((keys + 7) & ~7) * (kD / 16);  // within the capacity
+      mbar_expect_tx(bar + 8 * slot, keys * (kD / 2) + scale_bytes);
+      bulk_g2s(raw + slot * Sh::kRawBytes, codes + (size_t)ci * kKeys * (kD / 2), keys * (kD / 2),
+               bar + 8 * slot);
+      bulk_g2s(raw_scales + slot * Sh::kRawBytes, scales + (size_t)ci * kKeys * (kD / 16),
+               scale_bytes, bar + 8 * slot);
     };
-    if (warp < kSoftWarps + kKeyWarps)
-      slices(std::integral_constant<int, 0>{});
-    else
-      slices(std::integral_constant<int, 1>{});
+    if (lane == 0)
+      for (int ci = 0; ci < min(kRaw, cached); ++ci) fetch(ci);
+    int fetched = min(kRaw, cached);
+    if (part && count > 0) warp_arrive(full);  // of the tile before the first
+    bool ok = true;
+    for (int i = 0; i < count; ++i) {
+      const uint32_t dst =
+          base + (part ? kKeyBufs + i % kValueBufs : i % kKeyBufs) * Sh::kTileBytes;
+      CodeSlice<M, kUnits> x;
+      if (i >= fresh) {
+        const int ci = i - fresh, slot = ci % kRaw, keys = there(ci);
+        if (keys > 0)
+          ok = warp_wait(bar + 8 * slot, (ci / kRaw) & 1, a.status, a.wait_limit, dead);
+        if (!ok) break;
+        x.load(raw + slot * Sh::kRawBytes, raw_scales + slot * Sh::kRawBytes, keys, lane);
+        __syncwarp();
+        if (fetched < cached) {
+          if (lane == 0) {
+            fence_proxy_async_smem();
+            fetch(fetched);
+          }
+          ++fetched;
+        }
+      }
+      if (i >= bufs)
+        ok = warp_wait((part ? o_done : s_done) + 8 * (i % bufs), (i / bufs + 1) & 1, a.status,
+                       a.wait_limit, dead);
+      if (!ok) break;
+      if (i < fresh) {
+        const uint16_t* src = fresh_rows + (size_t)i * kKeys * kD;
+        // what is not finite in V is added at the end, to the rows that see it
+        if (copy_rows<M>(src, keys_new - (t0 + i) * kKeys, dst, slice.first, slice.count, lane,
+                         part != 0))
+          *odd = 1;
+      } else {
+        x.unpack(dst, slice.first, slice.count, lane);
+      }
+      fence_proxy_async_smem();
+      warp_arrive(full + 8 * ((i + part) & 3));
+      if (!part && i == count - 1) warp_arrive(full + 8 * (count & 3));  // there is none
+    }
+    // nothing may be in flight when the ring's memory is used again
+    if (!ok && lane == 0)
+      for (int ci = max(0, fetched - kRaw); ci < fetched; ++ci)
+        if (there(ci) > 0)
+          mbar_wait(bar + 8 * (ci % kRaw), (ci / kRaw) & 1, a.status, kWaitLimit);
+    __syncwarp();
   } else {
     if ((threadIdx.x & 31) == 0 && count > 0) {
       constexpr uint32_t kLead = kKeys * 128;
@@ -675,56 +669,58 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
   const int rows = min(kTileRows, a.rows - row0);
   const int share = (rows + a.cluster - 1) / a.cluster;
   const int r0 = (int)rank * share, mine = bad_len ? 0 : max(0, min(share, rows - r0));
-  const uint32_t stats = base + Sh::kStats, factors = base + Sh::kFactors;
-  float* factor = reinterpret_cast<float*>(smem + Sh::kFactors);  // [cluster][share]
-  for (int r = threadIdx.x; r < mine; r += kTileThreads) {
-    float mx[16], l = 0.f, m = -INFINITY;
-#pragma unroll
-    for (int q = 0; q < 16; ++q)
-      mx[q] = q < a.cluster ? ld_cluster_f32(mapa(stats + 4 * (r0 + r), q)) : -INFINITY;
-#pragma unroll
-    for (int q = 0; q < 16; ++q) m = fmaxf(m, mx[q]);
-#pragma unroll
-    for (int q = 0; q < 16; ++q)
-      if (q < a.cluster) {
-        // a CTA without tokens has sums of zero; one whose scores were all NaN has NaN sums
-        mx[q] = mx[q] == -INFINITY ? 1.f : exp2_approx(mx[q] - m);
-        l = fmaf(ld_cluster_f32(mapa(stats + 4 * (kTileRows + r0 + r), q)) +
-                     ld_cluster_f32(mapa(stats + 4 * (2 * kTileRows + r0 + r), q)),
-                 mx[q], l);
-      }
-    const float inv = none ? 0.f : 1.f / l;
-#pragma unroll
-    for (int q = 0; q < 16; ++q)
-      if (q < a.cluster) factor[q * share + r] = mx[q] * inv;
-    const int gr = row0 + r0 + r;
+  const uint32_t stats = base + Sh::kStats;
+  float* factor = reinterpret_cast<float*>(smem + Sh::kFactors);  // [cluster][share], maxima first
+  float* sums = reinterpret_cast<float*>(smem + Sh::kSwap);       // the same
+  for (int i = threadIdx.x; i < mine * a.cluster; i += kTileThreads) {
+    const int q = i / mine, r = i % mine;
+    factor[q * share + r] = ld_cluster_f32(mapa(stats + 4 * (r0 + r), q));
+    sums[q * share + r] = ld_cluster_f32(mapa(stats + 4 * (kTileRows + r0 + r), q)) +
+                          ld_cluster_f32(mapa(stats + 4 * (2 * kTileRows + r0 + r), q));
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < mine) {
+    const int r = threadIdx.x, gr = row0 + r0 + r;
+    float m = -INFINITY, l = 0.f;
+    for (int q = 0; q < a.cluster; ++q) m = fmaxf(m, factor[q * share + r]);
+    for (int q = 0; q < a.cluster; ++q) {
+      const float mq = factor[q * share + r];
+      // a CTA without tokens has sums of zero; one whose scores were all NaN has NaN sums
+      const float f = mq == -INFINITY ? 1.f : exp2_approx(mq - m);
+      l = fmaf(sums[q * share + r], f, l);
+      factor[q * share + r] = f;
+    }
+    sums[r] = none ? 0.f : 1.f / l;  // the first CTA's, which this thread alone has read
     if (a.lse)
       a.lse[(((size_t)seq * a.B + gr / a.group) * a.heads + head) * a.group + gr % a.group] =
           none ? -INFINITY : m / kLog2e + logf(l);
   }
   __syncthreads();
   for (int i = threadIdx.x; i < mine * (kD / 4); i += kTileThreads) {
-    const int r = i % mine, dim4 = i / mine;
+    const int r = i % mine, dim4 = i / mine;  // neighbouring threads read neighbouring rows
+    const uint32_t x_addr = base + (dim4 * kTileRows + r0 + r) * 16;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int q0 = 0; q0 < a.cluster; q0 += 2) {  // the cluster is even
-      float4 x[2];
+    for (int q0 = 0; q0 < a.cluster; q0 += 4) {
+      float4 x[4];
 #pragma unroll
-      for (int q = 0; q < 2; ++q)
-        x[q] = ld_cluster_f32x4(mapa(base + (dim4 * kTileRows + r0 + r) * 16, q0 + q));
+      for (int q = 0; q < 4; ++q)
+        if (q0 + q < a.cluster) x[q] = ld_cluster_f32x4(mapa(x_addr, q0 + q));
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const float f = ld_shared_f32(factors + 4 * ((q0 + q) * share + r));
-        acc.x = fmaf(x[q].x, f, acc.x);
-        acc.y = fmaf(x[q].y, f, acc.y);
-        acc.z = fmaf(x[q].z, f, acc.z);
-        acc.w = fmaf(x[q].w, f, acc.w);
-      }
+      for (int q = 0; q < 4; ++q)
+        if (q0 + q < a.cluster) {
+          const float f = factor[(q0 + q) * share + r];
+          acc.x = fmaf(x[q].x, f, acc.x);
+          acc.y = fmaf(x[q].y, f, acc.y);
+          acc.z = fmaf(x[q].z, f, acc.z);
+          acc.w = fmaf(x[q].w, f, acc.w);
+        }
     }
     const int gr = row0 + r0 + r;
     const size_t at =
         (((size_t)seq * a.B + gr / a.group) * a.heads + head) * a.group + gr % a.group;
+    const float inv = sums[r];
     *reinterpret_cast<uint2*>(a.out + at * kD + 4 * dim4) =
-        make_uint2(pack_bf16(acc.x, acc.y), pack_bf16(acc.z, acc.w));
+        make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
   }
   cluster_sync();  // no CTA leaves while its results are read
 }
