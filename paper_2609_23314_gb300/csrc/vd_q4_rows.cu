@@ -1,8 +1,8 @@
 // vd_q4_rows.cu -- rows into a cache held in 4 bits and back: vd_q4_append,
 // vd_q4_pack, vd_q4_unpack (include/vd.h; the row format is in vd_q4.cuh).
 //
-// Bound by DRAM: 288 units of 4096 rows of 128 values into 4 bits and back 232 us for 1.55
-// GB, 98 % of the copy peak (two lanes a group, 16-byte accesses: 417).
+// Bound by DRAM: 288 units of 4096 rows of 128 values into 4 bits and back 228 us for 1.55
+// GB, the copy peak (two lanes a group, 16-byte accesses: 417).
 #include <cuda_runtime.h>
 
 #include <climits>
@@ -31,8 +31,12 @@ namespace {
 
 // A thread takes a group of 16 values of K and the same one of V: a 32-byte access to each
 // bf16 row, so that a warp's accesses are contiguous, and a group's scale is its own affair.
-// kGroups such pairs are loaded before the first is turned, for loads in flight.
-constexpr int kGroups = 2;
+// kGroups such pairs are loaded before the first is turned, for loads in flight, in CTAs of
+// kRowThreads, small ones for an even end.  us for (groups, threads) = (2, 256), (4, 256),
+// (2, 128), (4, 128), (8, 128), (4, 64): pack_odd of perf/operators.py 38.6, 33.1, 38.0, 31.7, 35.6,
+// 36.7; append_decode_ragged 39.4, 38.5, 39.2, 37.5, 41.7, 36.9; pack_cache 233, 230, 228, 228,
+// 248, 232.
+constexpr int kGroups = 4, kRowThreads = 128;
 
 enum RowsOp { kAppend, kPack, kUnpack };
 
@@ -143,7 +147,7 @@ __device__ __forceinline__ Row16 values(const uint2& code, uint32_t scale) {
 // append: bf16 rows [0, B) of the source to slots [len, len + B); pack: rows [0, len);
 // unpack: the way back.  G: groups of a row.
 template <int OP, int G>
-__global__ void __launch_bounds__(kThreads) q4_rows_kernel(RowsArgs a) {
+__global__ void __launch_bounds__(kRowThreads) q4_rows_kernel(RowsArgs a) {
   grid_dependency_wait();
   grid_launch_dependents();
   bool on[kGroups];
@@ -151,7 +155,7 @@ __global__ void __launch_bounds__(kThreads) q4_rows_kernel(RowsArgs a) {
   if (OP == kAppend) {
 #pragma unroll
     for (int k = 0; k < kGroups; ++k) {
-      const long long i = ((long long)blockIdx.x * kGroups + k) * kThreads + threadIdx.x;
+      const long long i = ((long long)blockIdx.x * kGroups + k) * kRowThreads + threadIdx.x;
       on[k] = i < a.items;
       if (!on[k]) continue;
       const long long r = i / G;
@@ -182,7 +186,7 @@ __global__ void __launch_bounds__(kThreads) q4_rows_kernel(RowsArgs a) {
     const size_t row0 = (size_t)unit * a.row_cap * G;
 #pragma unroll
     for (int k = 0; k < kGroups; ++k) {
-      const size_t i = ((size_t)block * kGroups + k) * kThreads + threadIdx.x;
+      const size_t i = ((size_t)block * kGroups + k) * kRowThreads + threadIdx.x;
       on[k] = i < (size_t)n * G;
       row[k] = row0 + i;
       qrow[k] = q0 + i;
@@ -249,7 +253,7 @@ RowsKernel rows_kernel(int op, int d) {
 // units of `most` rows each at most
 vd_status launch_rows(int op, RowsArgs& a, long long units, int most, int d, cudaStream_t s) {
   a.wide = ((reinterpret_cast<uintptr_t>(a.rows[0]) | reinterpret_cast<uintptr_t>(a.rows[1])) & 31u) == 0;
-  const long long per = (long long)kGroups * kThreads, groups = (long long)most * (d / 16);
+  const long long per = (long long)kGroups * kRowThreads, groups = (long long)most * (d / 16);
   long long grid;
   if (op == kAppend) {
     a.items = units * groups;
@@ -259,7 +263,7 @@ vd_status launch_rows(int op, RowsArgs& a, long long units, int most, int d, cud
     grid = units * a.blocks;
   }
   if (grid > INT_MAX) return VD_ERR_UNSUPPORTED;
-  return launch_dependent((unsigned)grid, s, rows_kernel(op, d), a);
+  return launch_clusters((unsigned)grid, kRowThreads, 1, 0, s, rows_kernel(op, d), a);
 }
 
 RowsArgs rows_args(const vd_q4_cache* c, int layers, int layer0, unsigned* status) {
