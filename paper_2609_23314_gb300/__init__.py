@@ -150,7 +150,7 @@ def _ptr(t, dtype, shape, what, device):
     if t is None:
         return None
     try:
-        if (t.dtype == dtype and t.get_device() == device.index and t.is_contiguous()
+        if (t.dtype is dtype and t.get_device() == device.index and t.is_contiguous()
                 and t.shape == shape):
             return t.data_ptr()
         where, contiguous, got = t.device, t.is_contiguous(), t.shape
@@ -491,47 +491,50 @@ def vd_running_sum_init(cache: Cache, running_sum, stream=None) -> None:
     _check(load_library().vd_running_sum_init(cache.ref(), rp, _stream(stream)), "vd_running_sum_init")
 
 
-def _on_current(device):
-    """Kernels launch on the current device: refuse tensors of another one."""
+def _launch_stream(device, stream):
+    """The stream handle of a call.  Kernels launch on the current device: tensors of
+    another one are refused."""
     torch = _torch()
     if device.type != "cuda" or not torch.cuda.is_initialized():
-        return  # CPU tensors never reach a launch
-    if device.index != torch._C._cuda_getDevice():
-        raise ValueError(f"the tensors live on {device}, the current device is "
-                         f"cuda:{torch.cuda.current_device()}")
+        return None  # CPU tensors: the library refuses the call
+    index = torch._C._cuda_getDevice()
+    if device.index != index:
+        raise ValueError(f"the tensors live on {device}, the current device is cuda:{index}")
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(index) if stream is None and raw is not None else _stream(stream)
 
 
 def vd_q4_append(cache: Q4Cache, k_new, v_new, B: int, stream=None) -> None:
     """vd_append into a 4-bit cache; k_new, v_new: bf16
     [n_seq, n_layer, n_kv_head, B, head_dim]."""
     torch = _torch()
-    _on_current(cache.device)
+    s = _launch_stream(cache.device, stream)
     shape = cache.unit_shape() + (int(B), cache.head_dim)
     kp = _ptr(k_new, torch.bfloat16, shape, "k_new", cache.device)
     vp = _ptr(v_new, torch.bfloat16, shape, "v_new", cache.device)
-    _check(load_library().vd_q4_append(cache.ref(), kp, vp, int(B), _stream(stream)),
+    _check(load_library().vd_q4_append(cache.ref(), kp, vp, int(B), s),
            "vd_q4_append")
 
 
-def _same_device(q4: Q4Cache, cache: Cache):
+def _same_device(q4: Q4Cache, cache: Cache, stream):
     if q4.device != cache.device:
         raise ValueError(f"cache must live on {q4.device}, got {cache.device}")
-    _on_current(q4.device)
+    return _launch_stream(q4.device, stream)
 
 
 def vd_q4_pack(dst: Q4Cache, src: Cache, layer0: int = 0, stream=None) -> None:
     """Rows [0, src.len) of a bf16 cache into layers [layer0, layer0 + src.n_layer)
     of a 4-bit one; the call that writes the last layer also sets dst.len."""
-    _same_device(dst, src)
-    _check(load_library().vd_q4_pack(dst.ref(), int(layer0), src.ref(), _stream(stream)),
+    s = _same_device(dst, src, stream)
+    _check(load_library().vd_q4_pack(dst.ref(), int(layer0), src.ref(), s),
            "vd_q4_pack")
 
 
 def vd_q4_unpack(src: Q4Cache, dst: Cache, layer0: int = 0, stream=None) -> None:
     """Rows [0, src.len) of layers [layer0, layer0 + dst.n_layer) of a 4-bit cache to
     bf16 (exact) in dst, and dst.len = src.len."""
-    _same_device(src, dst)
-    _check(load_library().vd_q4_unpack(src.ref(), int(layer0), dst.ref(), _stream(stream)),
+    s = _same_device(src, dst, stream)
+    _check(load_library().vd_q4_unpack(src.ref(), int(layer0), dst.ref(), s),
            "vd_q4_unpack")
 
 
@@ -543,10 +546,10 @@ def vd_q4_attend(cache: Q4Cache, q, out, k_new=None, v_new=None, layer: int = 0,
     (every token sees the cached rows alone); scale: 1 / sqrt(head_dim) unless given;
     lse_out: fp32 [n_seq, B, n_q_head]."""
     torch = _torch()
-    _on_current(cache.device)
+    s = _launch_stream(cache.device, stream)
     if q.dim() != 4:
         raise ValueError("q must be [n_seq, B, n_q_head, head_dim]")
-    B, n_q = int(q.shape[1]), int(q.shape[2])
+    _, B, n_q, _ = q.shape
     shape = (cache.n_seq, B, n_q, cache.head_dim)
     new = cache.unit_shape() + (B, cache.head_dim)
     args = (
@@ -558,7 +561,7 @@ def vd_q4_attend(cache: Q4Cache, q, out, k_new=None, v_new=None, layer: int = 0,
     )
     scale = cache.head_dim ** -0.5 if scale is None else float(scale)
     _check(load_library().vd_q4_attend(cache.ref(), int(layer), args[0], n_q, args[1], args[2], B,
-                                       scale, args[3], args[4], _stream(stream)),
+                                       scale, args[3], args[4], s),
            "vd_q4_attend")
 
 
@@ -576,12 +579,12 @@ def vd_qkv_norm_rope(qkv, q_out, k_new, v_new, layer: int = 0, q_weight=None, k_
     if qkv.dim() != 4 or q_out.dim() != 4 or k_new.dim() != 5:
         raise ValueError("qkv and q_out must have 4 dimensions, k_new 5")
     dev = qkv.device
-    _on_current(dev)
-    n_seq, B, heads, d = (int(x) for x in qkv.shape)
-    n_q, n_layer = int(q_out.shape[2]), int(k_new.shape[1])
+    s = _launch_stream(dev, stream)
+    n_seq, B, heads, d = qkv.shape
+    n_q, n_layer = q_out.shape[2], k_new.shape[1]
     n_kv = (heads - n_q) // 2
     new = (n_seq, n_layer, n_kv, B, d)
-    pairs = 0 if inv_freq is None else int(inv_freq.numel())
+    pairs = 0 if inv_freq is None else inv_freq.numel()
     if heads != n_q + 2 * n_kv:
         raise ValueError(f"qkv has {heads} heads, which are not {n_q} query heads and as many "
                          "key as value heads")
@@ -597,8 +600,7 @@ def vd_qkv_norm_rope(qkv, q_out, k_new, v_new, layer: int = 0, q_weight=None, k_
     )
     _check(load_library().vd_qkv_norm_rope(args[0], n_seq, B, n_q, n_kv, d, args[1], args[2],
                                            float(eps), args[3], 2 * pairs, int(bool(interleaved)),
-                                           args[4], args[5], args[6], args[7], int(layer), n_layer,
-                                           _stream(stream)),
+                                           args[4], args[5], args[6], args[7], int(layer), n_layer, s),
            "vd_qkv_norm_rope")
 
 

@@ -123,8 +123,8 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
     import paper_2609_23314_gb300 as vd
     monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
     monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
-    vd._on_current(torch.device("cuda", 0))
-    vd._on_current(torch.device("cpu"))
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: 77 + i, raising=False)
+    assert vd._launch_stream(torch.device("cuda", 0), None) == 77
+    assert vd._launch_stream(torch.device("cpu"), None) is None
     with pytest.raises(ValueError, match="current device"):
-        vd._on_current(torch.device("cuda", 1))
+        vd._launch_stream(torch.device("cuda", 1), None)
