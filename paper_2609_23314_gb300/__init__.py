@@ -164,12 +164,19 @@ def _ptr(t, dtype, shape, what, device):
         raise ValueError(f"{what} must be contiguous")
     if got != shape:
         raise ValueError(f"{what} must have shape {tuple(shape)}, got {tuple(got)}")
-    return t.data_ptr()  # a CPU tensor of a CPU cache
+    return t.data_ptr()  # a CPU tensor of a CPU cache, which ref() refuses
 
 
 def _check(code: int, where: str):
     if code != 0:
         raise VdError(code, where)
+
+
+def _on_gpu(device):
+    """Refuses tensors that are not on a GPU: the library takes every address for a device
+    one, and a kernel would follow it into host memory."""
+    if device.type != "cuda":
+        raise ValueError(f"the tensors of a call must live on a CUDA device, got {device}")
 
 
 class Cache:
@@ -190,6 +197,7 @@ class Cache:
         self._s = _VdCache(k.data_ptr(), v.data_ptr(), len.data_ptr(), self.n_seq, self.n_layer,
                            self.n_kv_head, self.head_dim, self.capacity)
         self._ref = ctypes.byref(self._s)
+        self._gpu = self.device.type == "cuda"
         self._unit_shape = (self.n_seq, self.n_layer, self.n_kv_head)
 
     @classmethod
@@ -208,6 +216,9 @@ class Cache:
         return self._unit_shape
 
     def ref(self):
+        """What a call hands to the library; a cache that is not on a GPU is refused."""
+        if not self._gpu:
+            _on_gpu(self.device)
         return self._ref
 
 
@@ -235,6 +246,7 @@ class Q4Cache:
                              len.data_ptr(), self.n_seq, self.n_layer, self.n_kv_head,
                              self.head_dim, self.capacity)
         self._ref = ctypes.byref(self._s)
+        self._gpu = self.device.type == "cuda"
         self._unit_shape = (self.n_seq, self.n_layer, self.n_kv_head)
 
     @classmethod
@@ -254,6 +266,9 @@ class Q4Cache:
         return self._unit_shape
 
     def ref(self):
+        """What a call hands to the library; a cache that is not on a GPU is refused."""
+        if not self._gpu:
+            _on_gpu(self.device)
         return self._ref
 
 
@@ -496,7 +511,7 @@ def _launch_stream(device, stream):
     another one are refused."""
     torch = _torch()
     if device.type != "cuda" or not torch.cuda.is_initialized():
-        return None  # CPU tensors: the library refuses the call
+        return None  # CPU tensors: refused once the call's arguments are checked
     index = torch._C._cuda_getDevice()
     if device.index != index:
         raise ValueError(f"the tensors live on {device}, the current device is cuda:{index}")
@@ -598,6 +613,7 @@ def vd_qkv_norm_rope(qkv, q_out, k_new, v_new, layer: int = 0, q_weight=None, k_
         _ptr(k_new, torch.bfloat16, new, "k_new", dev),
         _ptr(v_new, torch.bfloat16, new, "v_new", dev),
     )
+    _on_gpu(dev)
     _check(load_library().vd_qkv_norm_rope(args[0], n_seq, B, n_q, n_kv, d, args[1], args[2],
                                            float(eps), args[3], 2 * pairs, int(bool(interleaved)),
                                            args[4], args[5], args[6], args[7], int(layer), n_layer, s),
@@ -605,7 +621,7 @@ def vd_qkv_norm_rope(qkv, q_out, k_new, v_new, layer: int = 0, q_weight=None, k_
 
 
 def vd_workspace_size(cache: Cache) -> int:
-    return int(load_library().vd_workspace_size(cache.ref()))
+    return int(load_library().vd_workspace_size(cache._ref))  # no launch: any device
 
 
 def vd_status_string(code: int) -> str:
