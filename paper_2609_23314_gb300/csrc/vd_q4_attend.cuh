@@ -262,21 +262,29 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
       for (int e = 0; e < 4; ++e) o[t][i][e] = 0.f;
   }
   // Takes the scores of 16 or 32 tokens (qs times them: log2 units) into the running state and
-  // turns them into weights.  The maximum is renewed only where a score exceeds it.
-  auto soften = [&](auto& s, const float (&qs)[NT][2]) {
+  // turns them into weights.  The maximum is renewed only where a score exceeds it.  Scores
+  // are rounded before the maximum is taken off them: a difference of the unrounded product
+  // would be off by half a unit of the maximum, 2^8 at 2^33.
+  auto soften = [&](auto& s, const unsigned long long (&qs)[NT]) {
     constexpr int kChunks = sizeof(s) / sizeof(s[0]);
     float top[NT][2];
     bool above = false;
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int g = 0; g < kChunks; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; e += 2)
+          f2_unpack(f2_mul(f2_pack(s[g][t][e], s[g][t][e + 1]), qs[t]), s[g][t][e], s[g][t][e + 1]);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         float m = fmaxf(s[0][t][e], s[0][t][e + 2]);
 #pragma unroll
         for (int g = 1; g < kChunks; ++g) m = fmaxf(m, fmaxf(s[g][t][e], s[g][t][e + 2]));
-        top[t][e] = m * qs[t][e];
-        above |= top[t][e] > mx[t][e];
+        top[t][e] = m;
+        above |= m > mx[t][e];
       }
+    }
     if (__any_sync(kFull, above)) {
 #pragma unroll
       for (int t = 0; t < NT; ++t)
@@ -296,22 +304,27 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
         }
     }
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int t = 0; t < NT; ++t) {
+      const unsigned long long shift = f2_pack(mx[t][0] == -INFINITY ? 0.f : -mx[t][0],
+                                               mx[t][1] == -INFINITY ? 0.f : -mx[t][1]);
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float shift = mx[t][e] == -INFINITY ? 0.f : -mx[t][e];
+      for (int g = 0; g < kChunks; ++g) {
 #pragma unroll
-        for (int g = 0; g < kChunks; ++g) {
-          s[g][t][e] = exp2_approx(fmaf(s[g][t][e], qs[t][e], shift));
-          s[g][t][e + 2] = exp2_approx(fmaf(s[g][t][e + 2], qs[t][e], shift));
-          sum[t][e] += s[g][t][e] + s[g][t][e + 2];
+        for (int e = 0; e < 4; e += 2) {
+          float lo, hi;
+          f2_unpack(f2_add(f2_pack(s[g][t][e], s[g][t][e + 1]), shift), lo, hi);
+          s[g][t][e] = exp2_approx(lo);
+          s[g][t][e + 1] = exp2_approx(hi);
         }
+        sum[t][0] += s[g][t][0] + s[g][t][2];
+        sum[t][1] += s[g][t][1] + s[g][t][3];
       }
+    }
   };
 
-  // Each row of Q times its power of two; qs: what a column's scores have to be multiplied by
-  // for log2 units
-  float qs[NT][2];
+  // Each row of Q times its power of two; qs: what the scores of columns 2 c and 2 c + 1
+  // have to be multiplied by for log2 units
+  unsigned long long qs[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     uint32_t top = 0;  // largest magnitude, as bits
@@ -333,8 +346,7 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
         asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(qf[t][w][e]) : "r"(up));
     // not 0, which would make a masked score a NaN
     const float down = fmaxf(f.down * (a.scale * kLog2e), 0x1p-126f);
-    qs[t][0] = __shfl_sync(kFull, down, 8 * c);
-    qs[t][1] = __shfl_sync(kFull, down, 8 * c + 4);
+    qs[t] = f2_pack(__shfl_sync(kFull, down, 8 * c), __shfl_sync(kFull, down, 8 * c + 4));
   }
   // the new rows, 16 at a time, in bf16: few, so a warp reads them straight from memory.
   // They go to the cluster's warps from the last one on.
@@ -441,8 +453,9 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
   // Q to fp16
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    qs[t][0] = fmaxf(qs[t][0] * kFrom16, 0x1p-126f);
-    qs[t][1] = fmaxf(qs[t][1] * kFrom16, 0x1p-126f);
+    float qs0, qs1;
+    f2_unpack(qs[t], qs0, qs1);
+    qs[t] = f2_pack(fmaxf(qs0 * kFrom16, 0x1p-126f), fmaxf(qs1 * kFrom16, 0x1p-126f));
 #pragma unroll
     for (int w = 0; w < M; ++w)
 #pragma unroll

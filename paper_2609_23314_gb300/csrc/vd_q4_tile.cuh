@@ -364,6 +364,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
         tc_fence_before();
         warp_arrive(q_full);
       }
+      bool large = false;  // a maximum of the warp's rows beyond 2^20
       for (int i = 0; ok && i < count; ++i) {
         const uint32_t s_col = lanes + (i & 1) * kKeys;
         ok = warp_wait(s_done + 8 * (i & 1), (i >> 1) & 1, a.status, a.wait_limit, dead);
@@ -417,11 +418,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
           return added;
         };
         // the weights stay below 2^8, and a row's first scores set its maximum
-        if (__any_sync(kFull, m > row_max + 8.f)) {
+        if (__any_sync(kFull, m - row_max > 8.f)) {
           const float top = fmaxf(row_max, m);
           const float f = top == -INFINITY ? 1.f : exp2_approx(row_max - top);
           row_max = top;
           row_sum *= f;
+          large = __any_sync(kFull, fabsf(row_max) > 0x1p20f && row_max > -INFINITY);
           if (i > 0) {
             ok = wait_added();
             if (!ok) break;
@@ -451,7 +453,18 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
             s[j / 2] = pack(lo, hi);
           }
         };
-        if (is_new)
+        if (large) {
+          // Scores are rounded before the maximum is taken off them, like the maximum itself:
+          // half a unit of it is 2^-4 at 2^20, but 2^8 at 2^33.  For all rows, this code takes
+          // the chunk of 512 tokens from 350 to 366 us (as a rare one 355)
+#pragma unroll
+          for (int j = 0; j < kHalf; j += 2) {
+            const float lo = exp2_approx(__fadd_rn(__fmul_rn(__uint_as_float(s[j]), c), shift));
+            const float hi = exp2_approx(__fadd_rn(__fmul_rn(__uint_as_float(s[j + 1]), c), shift));
+            sum2 = f2_add(sum2, f2_pack(lo, hi));
+            s[j / 2] = is_new ? pack_bf16(lo, hi) : pack_f16(lo, hi);
+          }
+        } else if (is_new)
           weights([](float lo, float hi) { return pack_bf16(lo, hi); });
         else
           weights([](float lo, float hi) { return pack_f16(lo, hi); });
