@@ -16,8 +16,10 @@
 // head dims on the 16-row side of m16n8k16, so that 8 query rows fill a tile: decode
 // has 1 to 8 rows (the query heads that share a KV head) per token.  K and V go from
 // codes to fp16 in registers (exact), Q goes to fp16 with each row scaled by a power of
-// two (QueryScale), sums are fp32, and P is rounded to fp16 (2^-11 of a weight, its error
-// averaged over the tokens).
+// two (QueryScale), sums are fp32, and P is rounded to fp16: 2^-11 of a weight, its error
+// averaged over the tokens.  Weights are relative to a point 2^15 below the running maximum
+// (kLift), so that those far below it keep their bits: the smallest that does not become 0 is
+// 2^-40 of the largest, 27 nats down (17 without the lift).
 // Bound by instruction issue: about 22 warp instructions a token at head_dim 128, 5.3 ns a
 // token and SM (its 144 bytes take 3.2 at the copy peak).  us: 512 KV heads around 4096
 // tokens 62.3 (3.7 TB/s), 16 heads of 131000 tokens 107.5 (2.8 TB/s; the copies alone 48),
@@ -50,6 +52,7 @@ struct AttendArgs {
 };
 
 constexpr int kStageKeys = 32;
+constexpr float kLift = 15.f;  // fp16's largest power of two
 constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ float exp2_approx(float x) {
@@ -251,7 +254,7 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
   }
 
   float o[NT][2 * M][4];
-  float mx[NT][2], sum[NT][2];  // of columns (query rows) 2 c and 2 c + 1
+  float mx[NT][2], sum[NT][2];  // references and sums of columns (query rows) 2 c and 2 c + 1
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     mx[t][0] = mx[t][1] = -INFINITY;
@@ -262,7 +265,8 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
       for (int e = 0; e < 4; ++e) o[t][i][e] = 0.f;
   }
   // Takes the scores of 16 or 32 tokens (qs times them: log2 units) into the running state and
-  // turns them into weights.  The maximum is renewed only where a score exceeds it.  Scores
+  // turns them into weights.  The reference mx, the maximum less kLift, is renewed only where
+  // a score exceeds it by more.  It is rounded up: no weight exceeds 2^kLift.  Scores
   // are rounded before the maximum is taken off them: a difference of the unrounded product
   // would be off by half a unit of the maximum, 2^8 at 2^33.
   auto soften = [&](auto& s, const unsigned long long (&qs)[NT]) {
@@ -281,8 +285,8 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
         float m = fmaxf(s[0][t][e], s[0][t][e + 2]);
 #pragma unroll
         for (int g = 1; g < kChunks; ++g) m = fmaxf(m, fmaxf(s[g][t][e], s[g][t][e + 2]));
-        top[t][e] = m;
-        above |= m > mx[t][e];
+        top[t][e] = __fadd_ru(m, -kLift);
+        above |= top[t][e] > mx[t][e];
       }
     }
     if (__any_sync(kFull, above)) {
@@ -731,7 +735,7 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
     const int gr = row0 + row;
     if (a.lse && rank == 0 && gr < a.rows)
       a.lse[(((size_t)seq * a.B + gr / a.group) * a.heads + head) * a.group + gr % a.group] =
-          none ? -INFINITY : m / kLog2e + logf(l);
+          none ? -INFINITY : (m + kLift) / kLog2e + logf(l * 0x1p-15f);
   }
   __syncthreads();
   const int total = min(Sh::kRows, a.rows - row0) * (kD / 4);

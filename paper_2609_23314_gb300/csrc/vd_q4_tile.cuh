@@ -10,8 +10,9 @@
 //   O += P V    (128 x head_dim, V's rows along the columns)
 // Roles of the warps, which meet only at mbarriers:
 //   0-7   softmax, a row per pair of threads with half the columns each: maximum, weights,
-//         their sum; O is rescaled where the maximum has risen by more than 2^8 (a smaller
-//         rise only makes the weights exceed 1);
+//         their sum.  Weights are relative to a point kTileLift below the maximum (as in the
+//         streaming kernel), and O is rescaled where the maximum has risen kLift above it (a
+//         smaller rise only makes the weights larger);
 //   8-11  K's tiles, a slice of the tokens each: cached codes, which come by bulk copies into
 //         the warp's own ring, to fp16 in the swizzled layout of the products (exact), or
 //         copies of the new tokens' bf16 rows;
@@ -41,6 +42,10 @@
 namespace vd {
 
 constexpr int kTileRows = 128;  // rows of a block
+
+// A rise of the maximum by 2^4 rescales O; the smallest weight that does not become 0 is 2^-36
+// of the largest, 25 nats down.
+constexpr float kTileLift = 11.f, kTileUnlift = 0x1p-11f;
 
 constexpr int kTileThreads = 512;
 constexpr int kSoftWarps = 8, kKeyWarps = 4, kValueWarps = 3, kProductWarp = 15;
@@ -312,7 +317,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
   const int row = row0 + lane_row;
   const uint32_t lanes = tm + ((uint32_t)(warp & 3) << 21);  // their warp's 32 lanes
   const int token = min(row, a.rows - 1) / a.group;
-  float row_max = -INFINITY, row_sum = 0.f;  // in log2 units; the sum: of this half
+  // in log2 units; the reference of the weights, at least kTileLift below the maximum when it
+  // is set; the sum: of this half
+  float row_max = -INFINITY, row_sum = 0.f;
   if (warp < kSoftWarps) {
     constexpr int kHalf = kKeys / 2;
     float* swapped = reinterpret_cast<float*>(smem + Sh::kSwap) + lane_row;
@@ -364,7 +371,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
         tc_fence_before();
         warp_arrive(q_full);
       }
-      bool large = false;  // a maximum of the warp's rows beyond 2^20
+      bool large = false;  // a reference of the warp's rows beyond 2^20
       for (int i = 0; ok && i < count; ++i) {
         const uint32_t s_col = lanes + (i & 1) * kKeys;
         ok = warp_wait(s_done + 8 * (i & 1), (i >> 1) & 1, a.status, a.wait_limit, dead);
@@ -417,9 +424,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
           if (added) tc_fence_after();
           return added;
         };
-        // the weights stay below 2^8, and a row's first scores set its maximum
-        if (__any_sync(kFull, m - row_max > 8.f)) {
-          const float top = fmaxf(row_max, m);
+        // the weights stay below 2^15, and a row's first scores set its reference
+        if (__any_sync(kFull, m - row_max > kLift)) {
+          const float top = fmaxf(row_max, __fadd_ru(m, -kTileLift));
           const float f = top == -INFINITY ? 1.f : exp2_approx(row_max - top);
           row_max = top;
           row_sum *= f;
@@ -456,7 +463,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
         if (large) {
           // Scores are rounded before the maximum is taken off them, like the maximum itself:
           // half a unit of it is 2^-4 at 2^20, but 2^8 at 2^33.  For all rows, this code takes
-          // the chunk of 512 tokens from 350 to 366 us (as a rare one 355)
+          // the chunk of 512 tokens from 353 to 366 us
 #pragma unroll
           for (int j = 0; j < kHalf; j += 2) {
             const float lo = exp2_approx(__fadd_rn(__fmul_rn(__uint_as_float(s[j]), c), shift));
@@ -627,7 +634,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
     row_sum = stat[kTileRows + lane_row] + stat[2 * kTileRows + lane_row];
     const float inv = none ? 0.f : 1.f / row_sum;
     if (a.cluster == 1 && valid && a.lse && half == 0)
-      a.lse[at] = none ? -INFINITY : row_max / kLog2e + logf(row_sum);
+      a.lse[at] = none ? -INFINITY : (row_max + kTileLift) / kLog2e + logf(row_sum * kTileUnlift);
 #pragma unroll 1
     for (int j = half * (kD / 2); j < (half + 1) * (kD / 2); j += 16) {
       uint32_t o[16];
@@ -706,7 +713,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
     sums[r] = none ? 0.f : 1.f / l;  // the first CTA's, which this thread alone has read
     if (a.lse)
       a.lse[(((size_t)seq * a.B + gr / a.group) * a.heads + head) * a.group + gr % a.group] =
-          none ? -INFINITY : m / kLog2e + logf(l);
+          none ? -INFINITY : (m + kTileLift) / kLog2e + logf(l * kTileUnlift);
   }
   __syncthreads();
   for (int i = threadIdx.x; i < mine * (kD / 4); i += kTileThreads) {

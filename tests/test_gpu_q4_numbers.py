@@ -75,3 +75,62 @@ def test_scores_of_any_size(d, B, scale):
                float(v_new.abs().max()))
     near(o, want_o, 2.0 ** -8 * want_o.abs() + 2.0 ** -20 * most, "out")
     near(e, want_l, 2.0 ** -21 * want_l.abs() + 2.0 ** -18, "lse")
+
+
+def tolerance(want_o, want_l, a_old, a_new, a_abs, size, keys, d):
+    """q4_ref.attend_tolerance, but a weight that is subnormal in fp16 is off by 2^-25 of
+    2^-11 of the largest weight: weights are lifted by 2^11 at least before they are rounded."""
+    t_out, t_lse = ref.attend_tolerance(want_o, want_l, a_old, a_new, 0 * a_abs, size, keys, d)
+    return t_out + 2.0 ** -36 * a_abs, t_lse
+
+
+@pytest.mark.parametrize("cluster", [None, "1"])
+@pytest.mark.parametrize("sink", ["cached", "new"])
+@pytest.mark.parametrize("gap", [12.0, 18.0, 20.0, 24.0])
+@pytest.mark.parametrize("value", [0.0, 0.015625])
+def test_weights_far_below_the_largest(gap, value, sink, cluster, monkeypatch):
+    """One key lies `gap` nats above 32768 others, and its own value is small or zero: the
+    others carry the output."""
+    if cluster:
+        monkeypatch.setenv("VD_Q4_CLUSTER", cluster)
+    n, d, G = 32769, 64, 4
+    g = torch.Generator().manual_seed(3)
+    k = torch.zeros(n, d)
+    k[:, 1:] = torch.randn(n, d - 1, generator=g)
+    v = 1.0 + 0.25 * torch.randn(n, d, generator=g)
+    k_new, v_new = torch.zeros(1, d), torch.ones(1, d)
+    if sink == "cached":
+        k[0], v[0] = 0.0, value
+        k[0, 0] = gap
+    else:
+        k_new[0, 0], v_new[0] = gap, value
+    c = vd.Q4Cache.empty(1, 1, 1, n + 7, d)
+    for x, codes, scales in ((k, c.k, c.k_scale), (v, c.v, c.v_scale)):
+        a, b = ref.quantise(x.to(torch.bfloat16))
+        codes[0, 0, 0, :n].copy_(a)
+        scales[0, 0, 0, :n].copy_(b)
+    c.len.fill_(n)
+    q = torch.zeros(1, 1, G, d)
+    q[..., 0] = 1.0
+    new = [x.to(torch.bfloat16).view(1, 1, 1, 1, d).cuda() for x in (k_new, v_new)]
+    qc = q.to(torch.bfloat16).cuda()
+    out, lse = torch.empty_like(qc), torch.empty(1, 1, G, device="cuda")
+    vd.vd_q4_attend(c, qc, out, new[0], new[1], 0, 1.0, lse)
+    ks, vs = (ref.values(x[0, 0, 0, :n].cpu(), y[0, 0, 0, :n].cpu())
+              for x, y in ((c.k, c.k_scale), (c.v, c.v_scale)))
+    # 20 is held as 6 times 3.25, the scale nearest to 20 / 6
+    assert float(ks[:, 0].max()) == ((19.5 if gap == 20.0 else gap) if sink == "cached" else 0.0)
+    got = ref.attend(q[0].double(), ks, vs, *(x[0, 0, 0].cpu().double() for x in new), 1.0)
+    t_out, t_lse = tolerance(*got, n + 1, d)
+    near(out[0].cpu().double(), got[0], t_out, "out")
+    near(lse[0].cpu().double(), got[1], t_lse, "lse")
+
+
+@pytest.mark.parametrize("B", [1, 40])
+def test_new_values_up_to_the_limit(B):
+    """Values of 2^95 and more in the new rows, which sums of lifted weights have to hold."""
+    c, q, k_new, v_new = state([0, 33], 1, 2, 4, 128, B, 40)
+    v_new = v_new.clamp(-1.875, 1.875) * 2.0 ** 95
+    o, e, want_o, want_l = run(c, q, k_new, v_new)
+    # weights in bf16, 2^-8 each, and out's rounding, of values up to 2^96
+    near(o, want_o, torch.full_like(o, 2.0 ** -6 * 2.0 ** 96), "out")
