@@ -123,6 +123,18 @@ __device__ __forceinline__ QueryScale scale_of(uint32_t top) {
   return {((245u - ex) << 7) * 0x00010001u, __uint_as_float((ex + 9u) << 23)};
 }
 
+// What a row's scores are multiplied by for log2 units.  Finite, so that a score of 0 stays one,
+// and not 0, so that a masked score stays masked.  Subnormal factors count: new keys of 2^127
+// make scores of up to 2^128 before it.
+__device__ __forceinline__ float score_factor(float down, float scale) {
+  return fminf(fmaxf(down * scale * kLog2e, 0x1p-149f), 3.40282347e38f);
+}
+
+// The same for cached tokens, whose queries are kTo16 larger.
+__device__ __forceinline__ float cached_factor(float factor) {
+  return fmaxf(factor * kFrom16, 0x1p-149f);
+}
+
 __device__ __forceinline__ uint32_t ld_shared_u8(uint32_t addr) {
   uint32_t r;
   asm volatile("{ .reg .u16 t; ld.shared.u8 t, [%1]; cvt.u32.u16 %0, t; }" : "=r"(r) : "r"(addr));
@@ -348,9 +360,8 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(qf[t][w][e]) : "r"(up));
-    // not 0, which would make a masked score a NaN
-    const float down = fmaxf(f.down * (a.scale * kLog2e), 0x1p-126f);
-    qs[t] = f2_pack(__shfl_sync(kFull, down, 8 * c), __shfl_sync(kFull, down, 8 * c + 4));
+    const float factor = score_factor(f.down, a.scale);
+    qs[t] = f2_pack(__shfl_sync(kFull, factor, 8 * c), __shfl_sync(kFull, factor, 8 * c + 4));
   }
   // the new rows, 16 at a time, in bf16: few, so a warp reads them straight from memory.
   // They go to the cluster's warps from the last one on.
@@ -459,7 +470,7 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
   for (int t = 0; t < NT; ++t) {
     float qs0, qs1;
     f2_unpack(qs[t], qs0, qs1);
-    qs[t] = f2_pack(fmaxf(qs0 * kFrom16, 0x1p-126f), fmaxf(qs1 * kFrom16, 0x1p-126f));
+    qs[t] = f2_pack(cached_factor(qs0), cached_factor(qs1));
 #pragma unroll
     for (int w = 0; w < M; ++w)
 #pragma unroll

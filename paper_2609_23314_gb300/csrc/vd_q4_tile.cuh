@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
     if (count > 0) {
       const uint32_t q_col = lanes + Sh::kColQ + half * 8 * M;
       // Q as in the streaming kernel (scale_of)
-      float unit_scale;
+      float factor;
       bool ok;
       {
         const uint16_t* q = a.q + ((((size_t)seq * a.B + token) * a.heads + head) * a.group +
@@ -356,7 +356,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
         top = (uint32_t)both;
         const QueryScale qs = scale_of(top);
         const uint32_t up = qs.up;
-        unit_scale = qs.down * (a.scale * kLog2e);
+        factor = score_factor(qs.down, a.scale);
 #pragma unroll
         for (int i = 0; i < 8 * M; ++i) {
           asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(w[i]) : "r"(up));
@@ -393,8 +393,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
           warp_arrive(q_full);
         }
         const bool is_new = i < fresh;
-        // not 0, which would make a masked score a NaN
-        const float c = fmaxf(is_new ? unit_scale : unit_scale * kFrom16, 0x1p-126f);
+        const float c = is_new ? factor : cached_factor(factor);
         uint32_t s[kHalf];
         tmem_ld(s_col + half * kHalf, s);
         // tokens behind this row's last one do not count

@@ -134,3 +134,43 @@ def test_new_values_up_to_the_limit(B):
     o, e, want_o, want_l = run(c, q, k_new, v_new)
     # weights in bf16, 2^-8 each, and out's rounding, of values up to 2^96
     near(o, want_o, torch.full_like(o, 2.0 ** -6 * 2.0 ** 96), "out")
+
+
+@pytest.mark.parametrize("scale,size", [(3.3e38, 0.0), (3.3e38, 1e-36), (1e-44, 0.0), (1e-44, 1e36)])
+@pytest.mark.parametrize("B", [1, 40])
+def test_scales_of_any_size(B, scale, size):
+    """Queries of zero, whose scores are zero at any scale, and queries that make up for the
+    scale.  Ordinary tolerances: q4_ref.attend_tolerance."""
+    c, q, k_new, v_new = state([70, 33], 1, 2, 4, 128, B, 72)
+    q = (q.double() * size).to(torch.bfloat16)
+    o, e, want_o, want_l = run(c, q, k_new, v_new, scale=scale)
+    group = q.shape[2] // c.n_kv_head
+    scale = float(torch.tensor(scale, dtype=torch.float32))
+    for s, m in enumerate(c.len.tolist()):
+        for h in range(c.n_kv_head):
+            ks, vs = (ref.values(x[s, 0, h, :m].cpu(), y[s, 0, h, :m].cpu())
+                      for x, y in ((c.k, c.k_scale), (c.v, c.v_scale)))
+            hs = slice(h * group, (h + 1) * group)
+            got = ref.attend(q[s, :, hs].cpu().double(), ks, vs, k_new[s, 0, h].cpu().double(),
+                             v_new[s, 0, h].cpu().double(), scale)
+            t_out, t_lse = tolerance(*got, m + B, 128)
+            near(o[s, :, hs], got[0], t_out, "out")
+            near(e[s, :, hs], got[1], t_lse, "lse")
+
+
+@pytest.mark.parametrize("B", [2, 40])
+def test_factors_below_the_smallest_normal_number(B):
+    """New keys of 2^127 under a scale that brings their scores to 2^-6: what the scores are
+    multiplied by is subnormal.  Its rounding, 2^-17 of itself, is far below the weights'."""
+    d = 256
+    c, q, k_new, v_new = state([0, 0], 1, 2, 4, d, B, 40)
+    q = torch.full_like(q, 2.0 ** -20)
+    sign = torch.where(torch.arange(B, device="cuda") % 2 == 0, 1.0, -1.0)
+    k_new = (sign[:, None].expand(B, d) * 1.5 * 2.0 ** 126).to(torch.bfloat16).expand(
+        k_new.shape).contiguous()
+    o, e, want_o, want_l = run(c, q, k_new, v_new, scale=2.0 ** -121)
+    # weights in bf16, 2^-8, out's rounding, the scores' own 2^-16 of at most 2^-5
+    mean = v_new.double().abs().cpu().cumsum(3) / torch.arange(1, B + 1)[:, None]
+    mean = mean[:, 0].transpose(1, 2).repeat_interleave(4, 2)
+    near(o, want_o, 2.0 ** -8 * want_o.abs() + 2.0 ** -7 * mean, "out")
+    near(e, want_l, torch.full_like(e, 2.0 ** -18) + 2.0 ** -21 * want_l.abs(), "lse")
