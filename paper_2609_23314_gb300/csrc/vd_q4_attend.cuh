@@ -106,10 +106,11 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4],
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// A query row's power of two: its largest magnitude goes to [2^-9, 2^-8) (a query of 2^118
-// and more to at most 1), exact in bf16, so that no finite key row makes a score overflow.
-// For fp16 kTo16 more, which rounds what lies below 2^-19 of the row's largest value to
-// 2^-29 of it.
+// A query row's power of two: its largest magnitude goes to [2^-9, 2^-8), exact in bf16, so
+// that no finite key row makes a score overflow.  The factor is 2^-126 at least: a row whose
+// largest magnitude is 2^118 or more goes to something below 4, and 256 products with new keys
+// below 2^118 stay finite.  For fp16 kTo16 more, at most 2^15, which rounds what lies below
+// 2^-19 of the row's largest value by at most 2^-29 of it (a score's fp32 sum loses more).
 constexpr float kTo16 = 0x1p13f, kFrom16 = 0x1p-13f;
 
 struct QueryScale {

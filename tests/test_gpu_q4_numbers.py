@@ -174,3 +174,29 @@ def test_factors_below_the_smallest_normal_number(B):
     mean = mean[:, 0].transpose(1, 2).repeat_interleave(4, 2)
     near(o, want_o, 2.0 ** -8 * want_o.abs() + 2.0 ** -7 * mean, "out")
     near(e, want_l, torch.full_like(e, 2.0 ** -18) + 2.0 ** -21 * want_l.abs(), "lse")
+
+
+@pytest.mark.parametrize("exponent", [0, 116])
+@pytest.mark.parametrize("B", [1, 40])
+def test_the_largest_queries(B, exponent):
+    """Queries of the largest finite bf16 value, with ordinary new keys and with keys of up to
+    2^117 (whose scores dwarf the cached ones').  Exact products, so that scores only lose what
+    their sums and factor lose; tolerances as everywhere."""
+    top = float(torch.finfo(torch.bfloat16).max)
+    c, q, k_new, v_new = state([70, 33], 1, 2, 4, 128, B, 72)
+    q = torch.where(q > 0, top, -top).to(torch.bfloat16)
+    k_new = (k_new.double().clamp(-1.875, 1.875) * 2.0 ** exponent).to(torch.bfloat16)
+    scale = 2.0 ** -132 if exponent == 0 else 2.0 ** -149
+    o, e, want_o, want_l = run(c, q, k_new, v_new, scale=scale)
+    group = q.shape[2] // c.n_kv_head
+    for s, m in enumerate(c.len.tolist()):
+        for h in range(c.n_kv_head):
+            ks, vs = (ref.values(x[s, 0, h, :m].cpu(), y[s, 0, h, :m].cpu())
+                      for x, y in ((c.k, c.k_scale), (c.v, c.v_scale)))
+            hs = slice(h * group, (h + 1) * group)
+            got = ref.attend(q[s, :, hs].cpu().double(), ks, vs, k_new[s, 0, h].cpu().double(),
+                             v_new[s, 0, h].cpu().double(), scale)
+            t_out, t_lse = tolerance(*got, m + B, 128)
+            assert bool(torch.isfinite(o[s, :, hs]).all())
+            near(o[s, :, hs], got[0], t_out, "out")
+            near(e[s, :, hs], got[1], t_lse, "lse")
