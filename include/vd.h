@@ -342,6 +342,8 @@ vd_status vd_running_sum_init_ex(const vd_cache* c, int32_t of_keys, double* run
  * index): 4.5 bits a value.  What a code stands for is exact in bf16, and
  * storing it again gives the same code (for scales of 2^-14 and more).  A group with
  * a NaN or an infinity reads as NaN (scale byte 255), recorded as VD_ERR_NONFINITE.
+ * Every call refuses (VD_ERR_UNSUPPORTED) a cache of more than 2^30 slots a unit or of more than
+ * (2^31 - 1) / 16 units.
  * ------------------------------------------------------------------------ */
 typedef struct {
   void* k;          /* device, [n_seq][n_layer][n_kv_head][capacity][head_dim / 2] bytes:
@@ -356,7 +358,8 @@ typedef struct {
 } vd_q4_cache;
 
 /* vd_append into a 4-bit cache: B new bf16 rows per unit at slots
- * [len, len + B), len += B.  Arguments and errors as vd_append. */
+ * [len, len + B), len += B.  Arguments and errors as vd_append, B == 0 among them (the
+ * buffers have to be given, and nothing happens). */
 vd_status vd_q4_append(const vd_q4_cache* c, const void* k_new, const void* v_new, int32_t B,
                        vd_stream_t stream);
 
@@ -382,6 +385,9 @@ vd_status vd_q4_unpack(const vd_q4_cache* src, int32_t layer0, const vd_cache* d
  *   q, out        bf16 device [n_seq][B][n_q_head][head_dim], 16-byte aligned; query head h
  *                 reads KV head h / (n_q_head / n_kv_head).
  *   n_q_head      a multiple of n_kv_head.
+ *   B             at least 1.  B * n_q_head / n_kv_head query rows per KV head, at most 2^24, and
+ *                 n_seq * B * n_q_head at most 2^27 - 1 in all (VD_ERR_UNSUPPORTED).
+ *   scale         above 0, at most 3.4e38 (VD_ERR_INVALID_ARG).
  *   k_new, v_new  bf16 device [n_seq][n_layer][n_kv_head][B][head_dim], the buffers of
  *                 vd_q4_append (layer `layer` is read), or both NULL: the tokens see
  *                 the cached rows alone, all of them.
@@ -391,11 +397,12 @@ vd_status vd_q4_unpack(const vd_q4_cache* src, int32_t layer0, const vd_cache* d
  * The cache is not modified; of slots >= len at most the scale bytes up to the next
  * multiple of 8 are read, and ignored.  Scores, softmax statistics and sums are fp32; a weight
  * is rounded to fp16 (bf16 for the new rows) before it multiplies its value, and counts for
- * nothing only where it is less than 2^-36 of the largest.  Sums of the new rows' values times
- * weights of up to 2^15 have to stay finite in fp32: values up to 2^96.  scale times
- * a query row's largest magnitude may be up to 2^117 (beyond, scores come out smaller), and
- * where that magnitude is 2^118 or more, new keys up to 2^117 (beyond, scores overflow).  out must
- * not overlap the inputs.  VD_ERR_TIMEOUT: the outputs are unspecified. */
+ * nothing only where it is less than 2^-36 of the largest.
+ * Range: sums of the new rows' values times weights of up to 2^15 have to stay finite in
+ * fp32 (values up to 2^96); scale times a query row's largest magnitude may be up to 2^117
+ * (beyond, scores come out smaller); where that magnitude is 2^118 or more, new keys up to
+ * 2^117 (beyond, scores overflow).
+ * out must not overlap the inputs.  VD_ERR_TIMEOUT: the outputs are unspecified. */
 vd_status vd_q4_attend(const vd_q4_cache* c, int32_t layer, const void* q, int32_t n_q_head,
                        const void* k_new, const void* v_new, int32_t B, float scale, void* out,
                        float* lse_out, vd_stream_t stream);
@@ -416,7 +423,9 @@ vd_status vd_q4_attend(const vd_q4_cache* c, int32_t layer, const void* q, int32
  *   q_out         bf16 device [n_seq][B][n_q_head][head_dim] (vd_q4_attend's q).
  *   k_new, v_new  bf16 device [n_seq][n_layer][n_kv_head][B][head_dim], the buffers of
  *                 the vd_append* calls; layer `layer` is written.
- * Norms, angles' sines and rotation are fp32, rounded once.  Outputs must not overlap
+ * Norms, angles' sines and rotation are fp32, rounded once: the squares of a head have to stay
+ * finite in their sum (values up to 2^59).  At most 2^31 - 9 tokens and 65536 heads
+ * (VD_ERR_UNSUPPORTED).  Outputs must not overlap
  * the input.  All bf16 buffers 16-byte aligned. */
 vd_status vd_qkv_norm_rope(const void* qkv, int32_t n_seq, int32_t B, int32_t n_q_head,
                            int32_t n_kv_head, int32_t head_dim, const void* q_weight,

@@ -182,6 +182,9 @@ extern "C" vd_status vd_qkv_norm_rope(const void* qkv, int32_t n_seq, int32_t B,
   if (misaligned(qkv) || misaligned(q_weight) || misaligned(k_weight) || misaligned(q_out) ||
       misaligned(k_new) || misaligned(v_new))
     return VD_ERR_ALIGNMENT;
+  const long long tokens = (long long)n_seq * B;
+  if (tokens > INT_MAX - kMaxTokens || (long long)n_q_head + 2LL * n_kv_head > 65536)
+    return VD_ERR_UNSUPPORTED;
   DeviceInfo dev;
   const vd_status r = device_info(&dev);
   if (r != VD_OK) return r;
@@ -194,9 +197,6 @@ extern "C" vd_status vd_qkv_norm_rope(const void* qkv, int32_t n_seq, int32_t B,
   a.q_out = static_cast<uint16_t*>(q_out);
   a.k_new = static_cast<uint16_t*>(k_new);
   a.v_new = static_cast<uint16_t*>(v_new);
-  const long long tokens = (long long)n_seq * B;
-  if (tokens > INT_MAX - kMaxTokens || (long long)n_q_head + 2LL * n_kv_head > 65536)
-    return VD_ERR_UNSUPPORTED;
   a.tokens = (int)tokens;
   a.B = B;
   a.n_q = n_q_head;
