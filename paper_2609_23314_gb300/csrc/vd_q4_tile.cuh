@@ -298,8 +298,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
   grid_dependency_wait();
   grid_launch_dependents();
 
-  const int n = __ldcg(a.len + seq);
-  const bool bad_len = n < 0 || n > a.cap;
+  const int len = __ldcg(a.len + seq);
+  const bool bad_len = len < 0 || len > a.cap;
+  const int n = bad_len ? 0 : len;
   if (bad_len && rank == 0 && tile == 0 && head == 0 && threadIdx.x == 0)
     record_status(a.status, kStDeviceLen);
   const int row0 = tile * kTileRows;
