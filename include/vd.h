@@ -396,8 +396,8 @@ vd_status vd_q4_unpack(const vd_q4_cache* src, int32_t layer0, const vd_cache* d
  * A sequence with len out of [0, capacity] gets no output (VD_ERR_DEVICE_LEN).
  * The cache is not modified; of slots >= len at most the scale bytes up to the next
  * multiple of 8 are read, and ignored.  Scores, softmax statistics and sums are fp32; a weight
- * is rounded to fp16 (bf16 for the new rows) before it multiplies its value, and counts for
- * nothing only where it is less than 2^-36 of the largest.
+ * is rounded to fp16 (2^-16 of itself for the new rows) before it multiplies its value, and
+ * counts for nothing only where it is less than 2^-36 of the largest.
  * Range: sums of the new rows' values times weights of up to 2^15 have to stay finite in
  * fp32 (values up to 2^96); scale times a query row's largest magnitude may be up to 2^117
  * (beyond, scores come out smaller); where that magnitude is 2^118 or more, new keys up to

@@ -17,7 +17,7 @@
 // has 1 to 8 rows (the query heads that share a KV head) per token.  K and V go from
 // codes to fp16 in registers (exact), Q goes to fp16 with each row scaled by a power of
 // two (QueryScale), sums are fp32, and P is rounded to fp16: 2^-11 of a weight, its error
-// averaged over the tokens.  Weights are relative to a point 2^15 below the running maximum
+// averaged over the tokens (for the new rows, in bf16, to two parts).  Weights are relative to a point 2^15 below the running maximum
 // (kLift), so that those far below it keep their bits: the smallest that does not become 0 is
 // 2^-40 of the largest, 27 nats down (17 without the lift).
 // Bound by instruction issue: about 22 warp instructions a token at head_dim 128, 5.3 ns a
@@ -71,6 +71,13 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
+}
+
+// Two weights in bf16, and in `low` what that leaves of them: together within 2^-16 of a weight.
+__device__ __forceinline__ uint32_t split_bf16(float x, float y, uint32_t& low) {
+  const uint32_t high = pack_bf16(x, y);
+  low = pack_bf16(x - __uint_as_float(high << 16), y - __uint_as_float(high & 0xffff0000u));
+  return high;
 }
 
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
@@ -449,19 +456,26 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
         }
         continue;
       }
-      uint32_t p[NT][2];
+      uint32_t p[NT][2], rest[NT][2];
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        p[t][0] = transpose_8x8(pack_bf16(s[0][t][0], s[0][t][1]));
-        p[t][1] = transpose_8x8(pack_bf16(s[0][t][2], s[0][t][3]));
-      }
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          uint32_t low;
+          const uint32_t high = split_bf16(s[0][t][2 * e], s[0][t][2 * e + 1], low);
+          p[t][e] = transpose_8x8(high);
+          rest[t][e] = transpose_8x8(low);
+        }
 #pragma unroll
       for (int i = 0; i < 2 * M; ++i) {
         const uint32_t(&x)[4] = vx[i];
         const uint32_t f[4] = {__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[0], x[1], 0x7632),
                                __byte_perm(x[2], x[3], 0x5410), __byte_perm(x[2], x[3], 0x7632)};
 #pragma unroll
-        for (int t = 0; t < NT; ++t) mma_16816<true>(o[t][i], f, p[t][0], p[t][1]);
+        for (int t = 0; t < NT; ++t) {
+          mma_16816<true>(o[t][i], f, p[t][0], p[t][1]);
+          mma_16816<true>(o[t][i], f, rest[t][0], rest[t][1]);
+        }
       }
     }
   }

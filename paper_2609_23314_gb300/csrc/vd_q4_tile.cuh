@@ -74,7 +74,8 @@ struct TileShape {
   static constexpr int kNeed = kMisc + 16 + 1024;
   static constexpr int kTotal = kNeed > 200 * 1024 ? kNeed : 200 * 1024;
   // columns of tensor memory: two S, P, O, Q (P and Q 16-bit pairs).  At head_dim 256 there
-  // is no room for P, which then takes the lower half of its S
+  // is no room for P, which then takes the lower half of its S.  The low parts of the new rows'
+  // weights take the upper half at any head_dim
   static constexpr bool kAlias = M == 8;
   static constexpr int kColP = 2 * kKeys;
   static constexpr int kColO = kColP + (kAlias ? 0 : kKeys / 2);
@@ -411,11 +412,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
           m4[(j >> 1) & 3] =
               max3(m4[(j >> 1) & 3], __uint_as_float(s[j]), __uint_as_float(s[j + 1]));
         float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * c;
-        // with P over S: both halves have read their scores before either writes weights
-        if (Sh::kAlias) tc_fence_before();
+        // where weights lie over S: both halves have read their scores before either writes some
+        if (Sh::kAlias || is_new) tc_fence_before();
         ok = exchange(m, i + 1);
         if (!ok) break;
-        if (Sh::kAlias) tc_fence_after();
+        if (Sh::kAlias || is_new) tc_fence_after();
         bool added = i == 0;  // the tile before is in O, and P is free
         auto wait_added = [&] {
           if (!added)
@@ -446,9 +447,29 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
           }
         }
         const float shift = row_max == -INFINITY ? 0.f : -row_max;
-        const unsigned long long c2 = f2_pack(c, c), shift2 = f2_pack(shift, shift);
         unsigned long long sum2 = 0;
-        auto weights = [&](auto pack) {
+        if (is_new || large) {
+          // Scores are rounded before the maximum is taken off them, like the maximum itself:
+          // half a unit of it is 2^-4 at 2^20, but 2^8 at 2^33.  For all tiles, that takes the
+          // chunk of 512 tokens from 353 to 366 us.  New rows' weights go into two bf16 parts,
+          // as one would be off by as much as the result's own rounding where a token sees few
+          // rows: the low ones take S's upper half (attend_block of perf/operators.py 18.1 us
+          // with one part, 18.6 with two; a prompt of 8192 tokens over itself 1857, 1968).
+#pragma unroll
+          for (int j0 = 0; j0 < kHalf; j0 += 16) {
+            uint32_t low[8];
+#pragma unroll
+            for (int j = j0; j < j0 + 16; j += 2) {
+              const float lo = exp2_approx(__fadd_rn(__fmul_rn(__uint_as_float(s[j]), c), shift));
+              const float hi = exp2_approx(__fadd_rn(__fmul_rn(__uint_as_float(s[j + 1]), c), shift));
+              sum2 = f2_add(sum2, f2_pack(lo, hi));
+              const uint32_t split = split_bf16(lo, hi, low[(j - j0) / 2]);
+              s[j / 2] = is_new ? split : pack_f16(lo, hi);
+            }
+            if (is_new) tmem_st8(s_col + kKeys / 2 + half * (kHalf / 2) + j0 / 2, low);
+          }
+        } else {
+          const unsigned long long c2 = f2_pack(c, c), shift2 = f2_pack(shift, shift);
 #pragma unroll
           for (int j = 0; j < kHalf; j += 2) {
             float lo, hi;
@@ -457,24 +478,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
             lo = exp2_approx(lo);
             hi = exp2_approx(hi);
             sum2 = f2_add(sum2, f2_pack(lo, hi));
-            s[j / 2] = pack(lo, hi);
+            s[j / 2] = pack_f16(lo, hi);
           }
-        };
-        if (large) {
-          // Scores are rounded before the maximum is taken off them, like the maximum itself:
-          // half a unit of it is 2^-4 at 2^20, but 2^8 at 2^33.  For all rows, this code takes
-          // the chunk of 512 tokens from 353 to 366 us
-#pragma unroll
-          for (int j = 0; j < kHalf; j += 2) {
-            const float lo = exp2_approx(__fadd_rn(__fmul_rn(__uint_as_float(s[j]), c), shift));
-            const float hi = exp2_approx(__fadd_rn(__fmul_rn(__uint_as_float(s[j + 1]), c), shift));
-            sum2 = f2_add(sum2, f2_pack(lo, hi));
-            s[j / 2] = is_new ? pack_bf16(lo, hi) : pack_f16(lo, hi);
-          }
-        } else if (is_new)
-          weights([](float lo, float hi) { return pack_bf16(lo, hi); });
-        else
-          weights([](float lo, float hi) { return pack_f16(lo, hi); });
+        }
         if (!Sh::kAlias) ok = wait_added();
         if (!ok) break;
         const uint32_t p_col =
@@ -594,16 +600,22 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tile_kernel(AttendArgs a) 
         const uint32_t desc = i < fresh ? tc_desc(true, true, kD) : tc_desc(false, true, kD);
         const uint64_t vt = tc_smem(base + (kKeyBufs + i % kValueBufs) * Sh::kTileBytes, kLead);
         const uint32_t p_col = tm + (Sh::kAlias ? (i & 1) * kKeys : Sh::kColP);
+        const uint32_t low_col = tm + (i & 1) * kKeys + kKeys / 2;
 #pragma unroll
         for (int k = 0; k < kKeys / 16; ++k)
           tc_mma(tm + Sh::kColO, p_col + 8 * k, vt + ((2048 * k) >> 4), desc, i > 0 || k > 0);
+        if (i < fresh) {
+#pragma unroll
+          for (int k = 0; k < kKeys / 16; ++k)
+            tc_mma(tm + Sh::kColO, low_col + 8 * k, vt + ((2048 * k) >> 4), desc, true);
+        }
         tc_commit(o_done + 8 * (i % 3));
       };
 #pragma unroll 1
       for (int i = -1; i < count; ++i) {
         operands(i + 1);
-        // S of tile i + 1 takes the place of the weights of tile i - 1
-        if (Sh::kAlias && i > 0) await(o_done + 8 * ((i - 1) % 3), ((i - 1) / 3) & 1);
+        // S of tile i + 1 takes the place of the weights of tile i - 1, or of their low parts
+        if (i > 0 && (Sh::kAlias || i - 1 < fresh)) await(o_done + 8 * ((i - 1) % 3), ((i - 1) / 3) & 1);
         if (i + 1 < count && (i + 1 == 0 || i + 1 == fresh)) await(q_full, i + 1 == 0 ? 0 : 1);
         tc_fence_after();
         if (ok && i + 1 < count) scores(i + 1);

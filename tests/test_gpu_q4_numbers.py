@@ -200,3 +200,24 @@ def test_the_largest_queries(B, exponent):
             assert bool(torch.isfinite(o[s, :, hs]).all())
             near(o[s, :, hs], got[0], t_out, "out")
             near(e[s, :, hs], got[1], t_lse, "lse")
+
+
+@pytest.mark.parametrize("lens", [[0, 3], [200, 70]])
+@pytest.mark.parametrize("d", [64, 96, 128, 256])
+@pytest.mark.parametrize("B", [1, 2, 7, 40, 150])
+def test_weights_of_new_rows(B, d, lens):
+    """A new row's weight is carried in two bf16 parts, 2^-8 of a weight twice over: 2^-16 at
+    most, where q4_ref.attend_tolerance allows for one part."""
+    c, q, k_new, v_new = state(lens, 1, 2, 4, d, B, 208)
+    o, e, want_o, want_l = run(c, q, k_new, v_new)
+    for s, m in enumerate(lens):
+        for h in range(2):
+            ks, vs = (ref.values(x[s, 0, h, :m].cpu(), y[s, 0, h, :m].cpu())
+                      for x, y in ((c.k, c.k_scale), (c.v, c.v_scale)))
+            hs = slice(h * 4, (h + 1) * 4)
+            got = ref.attend(q[s, :, hs].cpu().double(), ks, vs, k_new[s, 0, h].cpu().double(),
+                             v_new[s, 0, h].cpu().double(), d ** -0.5)
+            t_out, t_lse = tolerance(*got, m + B, d)
+            a_new = got[3]
+            near(o[s, :, hs], got[0], t_out - (2.0 ** -8 - 2.0 ** -16) * a_new, "out")
+            near(e[s, :, hs], got[1], t_lse, "lse")
