@@ -85,15 +85,22 @@ vd_status slots_of(const DeviceInfo& dev, int m, const Slots** out) {
   return VD_OK;
 }
 
-// 0, 1: the streaming kernel with tiles of 8 or 16 query rows, 2: the block kernel.  us at
-// 8 KV heads a sequence, 8-row tiles / 16-row tiles / block:
-//   up to 16 rows always stream (8 sequences of 4000 tokens, 16 rows, 22.2 / 19.4 / 33.7;
-//   head_dim 256 38.4 / - / 53.7), more only in one wave (head_dim 256, 8 sequences, 500
-//   tokens, 24 rows 21.2 / - / 18.5) and up to 32 rows (8 sequences of 4000 tokens 37.4 / 31.3 /
-//   34.1) or with little work (one sequence, 500 tokens, 128 rows 9.0 / 9.0 / 13.5, 4000
-//   tokens, 64 rows 15.0 / 13.6 / 16.6, 128 rows 22.9 / 19.6 / 18.8);
-//   8-row tiles, which read the cache once for each, with little work (one sequence of 4000
-//   tokens, 32 rows 11.0 / 13.2, 64 rows 15.0 / 13.6; 32000 tokens, 16 rows 38.1 / 31.9).
+// 0, 1: the streaming kernel with tiles of 8 or 16 query rows, 2: the block kernel.  By the
+// capacity, which the host knows, not by the lengths: a short cache in a large buffer takes the
+// plan of a full one.  us at 8 KV heads a sequence, head_dim 128, 8-row tiles / 16-row tiles / block,
+// full caches:
+//   up to 16 rows always stream (8 sequences of 4000 tokens, 16 rows, 22.4 / 18.7 / 30.5;
+//   head_dim 256 36.6 / - / 52.5), more only in one wave (head_dim 256, 8 sequences, 500
+//   tokens, 24 rows 19.9 / - / 16.7) and up to 32 rows (8 sequences of 4000 tokens 36.3 / 30.8 /
+//   31.2) or with little work (one sequence, 500 tokens, 128 rows 8.3 / 8.5 / 13.1; capacity
+//   4096, 64 rows 14.1 / 12.8 / 15.5, 128 rows 21.5 / 18.7 / 17.5);
+//   8-row tiles, which read the cache once for each, with little work (one sequence, capacity
+//   4096, 32 rows 10.6 / 12.5 / 14.8, 64 rows 14.1 / 12.8 / 15.5; 32000, 16 rows 36.7 / 31.6 /
+//   49.1).
+// Both cuts go by the work alone, and between their measured sides the best kernel also depends
+// on the rows: for one sequence 8-row tiles stay ahead for 32 rows (capacity 4104 10.7, 8192
+// 14.7, 16384 22.3; the rule takes 16-row tiles at 12.5, 18.8, 31.4), and 16-row tiles for 64
+// (4104 12.8, 8192 19.0; the rule takes the block kernel at 15.4, 20.3).
 int choose_kernel(int m, long long rows, long long units, long long capacity, const Slots& slots) {
   const long long tiles8 = (rows + 7) / 8;
   const int kind =
@@ -164,12 +171,12 @@ extern "C" vd_status vd_q4_attend(const vd_q4_cache* c, int32_t layer, const voi
   a.scale = scale;
   a.wait_limit = wait_limit();
   const long long base = units * a.tiles;
-  // The largest cluster that runs in one wave and leaves each CTA enough tokens to pay for
-  // the join; two streaming CTAs run on an SM, and clusters of 16, which do not fill the
-  // GPU's groups of SMs, have to gain more.  us, C = 4, 8, 16: one sequence, 8 KV heads of
-  // 500 tokens 5.6, 5.8, 7.4; 5 sequences, 3 heads, 2500 tokens 7.7, 8.2, 17.8; one
-  // sequence, 8 heads, 4096 tokens 10.0, 7.9, 8.3, 32000 tokens 44, 25, 22.3; two
-  // sequences, 131000 tokens 164, 132, 109.
+  // The largest cluster that runs in one wave and leaves each CTA enough tokens (by the
+  // capacity, as above) to pay for the join; two streaming CTAs run on an SM, and clusters of
+  // 16, which do not fill the GPU's groups of SMs, have to gain more.  us, C = 4, 8, 16, one
+  // token: one sequence, 8 KV heads of 500 tokens 5.1, 5.5, 7.1; 5 sequences, 3 heads, 2500
+  // tokens 7.7, 7.3, 12.5; one sequence, 8 heads, 4096 tokens 9.6, 7.6, 8.2, 32000 tokens 43.5,
+  // 24.7, 21.8 (8 is taken below a capacity of 32768); two sequences, 131000 tokens 162, 127, 107.
   int e = 0;
   const int least[5] = {0, 128, 128, kind == 2 ? 128 : 512, kind == 2 ? 128 : 2048};
   while (e < 4 && slots->at[kind][e + 1] > 0 &&

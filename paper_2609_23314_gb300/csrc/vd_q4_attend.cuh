@@ -20,10 +20,13 @@
 // averaged over the tokens (for the new rows, in bf16, to two parts).  Weights are relative to a point 2^15 below the running maximum
 // (kLift), so that those far below it keep their bits: the smallest that does not become 0 is
 // 2^-40 of the largest, 27 nats down (17 without the lift).
-// Bound by instruction issue: about 22 warp instructions a token at head_dim 128, 5.3 ns a
-// token and SM (its 144 bytes take 3.2 at the copy peak).  us: 512 KV heads around 4096
-// tokens 62.3 (3.7 TB/s), 16 heads of 131000 tokens 107.5 (2.8 TB/s; the copies alone 48),
-// 8 heads of 4096 tokens 8.0.
+// About 21 warp instructions a token at head_dim 128, 128 of them in 16 tokens on half-rate
+// pipes (conversions and fp16 products).  While an SM is active it issues 2.4 instructions a
+// cycle of 4 and the ALU pipe is at 52 %: half-rate pipes and latency bound it, not the issue;
+// 5.3 ns a token and SM (its 144 bytes take 3.2 at the copy peak).  And SMs idle: a quarter of
+// the time where 512 KV heads are 1.7 waves of CTAs.  us: 512 KV heads around 4096 tokens 62.1
+// (3.7 TB/s), 16 heads of 131000 tokens 107.4 (2.8 TB/s; 256 CTAs on 304 places; the copies
+// alone 48), 8 heads of 4096 tokens 7.8.
 #pragma once
 
 #include <cstdint>
@@ -116,8 +119,9 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4],
 // A query row's power of two: its largest magnitude goes to [2^-9, 2^-8), exact in bf16, so
 // that no finite key row makes a score overflow.  The factor is 2^-126 at least: a row whose
 // largest magnitude is 2^118 or more goes to something below 4, and 256 products with new keys
-// below 2^118 stay finite.  For fp16 kTo16 more, at most 2^15, which rounds what lies below
-// 2^-19 of the row's largest value by at most 2^-29 of it (a score's fp32 sum loses more).
+// below 2^118 stay finite.  For fp16 kTo16 more, at most 2^15: the 8 bits of a bf16 value fit
+// down to 2^-17, 2^-21 of the row's largest; what is smaller is off by at most 2^-29 of the
+// largest (the fp32 sum of a score's products is bound by 2^-23 of their magnitudes).
 constexpr float kTo16 = 0x1p13f, kFrom16 = 0x1p-13f;
 
 struct QueryScale {

@@ -24,11 +24,14 @@
 // tiles of a unit and joins the results through distributed shared memory.
 //
 // Per tile of 128 tokens at head_dim 128: the products take 1024 cycles at 4096
-// multiply-adds a cycle, the roles issue 5700 warp instructions, 1425 a scheduler, from code
-// that no longer fits the instruction cache (14 % of the stalls): K and V share theirs (385
-// with one each).  us: 512 new tokens over 32768 cached ones, 8 KV heads of 4 query heads, 343
-// (277 GFLOP, 810 TFLOP/s); without the softmax 280, without the unpacking 263, without the
-// products 330 of a 352 us form; 128 new tokens over 2048 18.0.
+// multiply-adds a cycle, the roles issue 6400 warp instructions (their polls among them), 1600
+// a scheduler, at 2.5 a cycle of 4, and the tensor pipe is at 40 % while an SM is active: the
+// chain from scores to weights to product, its latencies and half-rate conversions bound it.  K
+// and V are unpacked once for every 128 query rows.  K's and V's warps share their code, as the
+// roles' code does not fit the instruction cache (385 us with one each, 343 shared, in one run).
+// us: 512 new tokens over 32768 cached ones, 8 KV heads of 4 query heads, 356 (277 GFLOP, 780
+// TFLOP/s; 128 CTAs on 152 SMs); of a 352 us form, without the softmax 280, without the unpacking
+// 263, without the products 330; 128 new tokens over 2048 18.6; 8192 over themselves 1970.
 #pragma once
 
 #include <cstdint>
