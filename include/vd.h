@@ -424,7 +424,8 @@ vd_status vd_q4_attend(const vd_q4_cache* c, int32_t layer, const void* q, int32
  *   k_new, v_new  bf16 device [n_seq][n_layer][n_kv_head][B][head_dim], the buffers of
  *                 the vd_append* calls; layer `layer` is written.
  * Norms, angles' sines and rotation are fp32, rounded once: the squares of a head have to stay
- * finite in their sum (values up to 2^59).  At most 2^31 - 9 tokens and 65536 heads
+ * finite in their sum (values up to 2^59) and, where eps is 0, normal numbers (a largest value of
+ * at least 2^-59).  At most 2^31 - 9 tokens and 65536 heads
  * (VD_ERR_UNSUPPORTED).  Outputs must not overlap
  * the input.  All bf16 buffers 16-byte aligned. */
 vd_status vd_qkv_norm_rope(const void* qkv, int32_t n_seq, int32_t B, int32_t n_q_head,
