@@ -143,13 +143,16 @@ def hbm_peak():
 
 
 def kernel_source_hash() -> str:
-    """Hash of the CUDA sources' code (comments and white space removed), the
-    key of the committed ncu traffic: a capture stays valid until the code
-    itself changes."""
+    """Hash of the CUDA sources' code (comments and white space removed) that the
+    eviction kernels and their launches are made from, the key of the committed
+    ncu traffic: a capture stays valid until the code itself changes.  The sources
+    of the 4-bit cache are none of them."""
     import re
     h = hashlib.sha256()
     csrc = os.path.join(ROOT, "paper_2609_23314_gb300", "csrc")
     for name in sorted(os.listdir(csrc)):
+        if name.startswith(("vd_q4", "vd_qkv", "vd_tcgen05")):
+            continue
         with open(os.path.join(csrc, name)) as f:
             text = f.read()
         text = re.sub(r"/\*.*?\*/", " ", text, flags=re.S)
