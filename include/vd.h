@@ -399,9 +399,9 @@ vd_status vd_q4_unpack(const vd_q4_cache* src, int32_t layer0, const vd_cache* d
  * is rounded to fp16 (2^-16 of itself for the new rows) before it multiplies its value, and
  * counts for nothing only where it is less than 2^-36 of the largest.
  * Range: sums of the new rows' values times weights of up to 2^15 have to stay finite in
- * fp32 (values up to 2^96); scale times a query row's largest magnitude may be up to 2^117
- * (beyond, scores come out smaller); where that magnitude is 2^118 or more, new keys up to
- * 2^117 (beyond, scores overflow).
+ * fp32 (2^16 rows of values up to 2^96); scale times a query row's largest magnitude may be
+ * up to 2^117 (beyond, scores come out smaller); where that magnitude is 2^118 or more, new
+ * keys up to 2^117 (beyond, scores overflow).
  * out must not overlap the inputs.  VD_ERR_TIMEOUT: the outputs are unspecified. */
 vd_status vd_q4_attend(const vd_q4_cache* c, int32_t layer, const void* q, int32_t n_q_head,
                        const void* k_new, const void* v_new, int32_t B, float scale, void* out,

@@ -84,6 +84,9 @@ __device__ __forceinline__ unsigned long long f2_sub(unsigned long long a, unsig
   return r;
 }
 
+// ptxas may join this with an f2_add of its result into one instruction with one rounding, as
+// tests showed; where the product's own rounding matters, it needs another use as well, or
+// __fmul_rn in its place.
 __device__ __forceinline__ unsigned long long f2_mul(unsigned long long a, unsigned long long b) {
   unsigned long long r;
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));

@@ -17,9 +17,9 @@
 // has 1 to 8 rows (the query heads that share a KV head) per token.  K and V go from
 // codes to fp16 in registers (exact), Q goes to fp16 with each row scaled by a power of
 // two (QueryScale), sums are fp32, and P is rounded to fp16: 2^-11 of a weight, its error
-// averaged over the tokens (for the new rows, in bf16, to two parts).  Weights are relative to a point 2^15 below the running maximum
-// (kLift), so that those far below it keep their bits: the smallest that does not become 0 is
-// 2^-40 of the largest, 27 nats down (17 without the lift).
+// averaged over the tokens (for the new rows, in bf16, to two parts).  Weights are relative to a
+// point 2^15 below the running maximum (kLift), so that those far below it keep their bits: the
+// smallest that does not become 0 is 2^-40 of the largest, 27 nats down (17 without the lift).
 // About 21 warp instructions a token at head_dim 128, 128 of them in 16 tokens on half-rate
 // pipes (conversions and fp16 products).  While an SM is active it issues 2.4 instructions a
 // cycle of 4 and the ALU pipe is at 52 %: half-rate pipes and latency bound it, not the issue;
@@ -292,7 +292,8 @@ __global__ void __launch_bounds__(kThreads, M * NT <= 4 ? 2 : 1) q4_attend_kerne
   // turns them into weights.  The reference mx, the maximum less kLift, is renewed only where
   // a score exceeds it by more.  It is rounded up: no weight exceeds 2^kLift.  Scores
   // are rounded before the maximum is taken off them: a difference of the unrounded product
-  // would be off by half a unit of the maximum, 2^8 at 2^33.
+  // would be off by half a unit of the maximum, 2^8 at 2^33.  (Both the maximum and the
+  // difference use the product, which keeps it rounded.)
   auto soften = [&](auto& s, const unsigned long long (&qs)[NT]) {
     constexpr int kChunks = sizeof(s) / sizeof(s[0]);
     float top[NT][2];
