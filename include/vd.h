@@ -94,8 +94,10 @@ typedef enum {
   VD_ERR_DEVICE_BUDGET = 8, /* device: N_dev[s] out of [1, N], or a decode call found
                                len > N + 1 */
   VD_ERR_NO_DEVICE = 9,   /* no CUDA device, or not an sm_103 device */
-  VD_ERR_INTERNAL = 10    /* device: a kernel's self-check found an inconsistent slot
+  VD_ERR_INTERNAL = 10,   /* device: a kernel's self-check found an inconsistent slot
                              list (never expected); the access was skipped */
+  VD_ERR_DEVICE_PAGE = 11 /* device: a page of a paged cache out of [0, n_page) that a
+                             call would have had to read or write; it was skipped */
 } vd_status;
 
 /* Scoring rules of Sec. 3.2.  Higher scores are kept.
@@ -434,6 +436,122 @@ vd_status vd_qkv_norm_rope(const void* qkv, int32_t n_seq, int32_t B, int32_t n_
                            int32_t rotary_dim, int32_t interleaved, const int32_t* pos_first_new,
                            void* q_out, void* k_new, void* v_new, int32_t layer, int32_t n_layer,
                            vd_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * A paged cache (not in the paper: a storage form of its cache, in which what an
+ * eviction frees can go to other sequences), the pass that fills it, the attention
+ * that reads it, and the way to the contiguous layout of the vd_evict_* calls and back.
+ *
+ * Slot t of sequence s lies in page page_table[s][t / page_size], at t % page_size; the
+ * page of every layer and KV head has the same number.  Places of the table at or behind
+ * ceil((len + the call's new tokens) / page_size) are not read.  Sequences may share pages
+ * that no call writes.
+ *
+ * Types: VD_PAGED_BF16, or VD_PAGED_E4M3: 8-bit floats with 4 exponent and 3 mantissa bits, a
+ * value being the stored one times the scale of its layer and KV head.  Storing divides by
+ * the scale in fp32 and rounds to nearest, ties to even, magnitudes above 448 to 448; a NaN
+ * stays one.  A bf16 value read from such a page and stored again gives the same byte
+ * (scales for which all of these are normal numbers in bf16).
+ *
+ * Every call checks the cache: a null pointer, an extent below 1, a scale with bf16 pages, or a
+ * stride that is smaller than a row (of an extent above 1) is VD_ERR_INVALID_ARG; rows that
+ * are not 16-byte aligned (addresses, strides, head_dim) VD_ERR_ALIGNMENT; head_dim above 256,
+ * more than 2^30 slots a sequence, 2^20 sequences, 65536 KV heads or 2^31 - 1 units (n_seq *
+ * n_layer * n_kv_head) VD_ERR_UNSUPPORTED.
+ * On the device, a sequence whose len, or len and new tokens, lie out of
+ * [0, max_pages * page_size], or whose n_new lies out of [0, B], gets no row and no output
+ * (VD_ERR_DEVICE_LEN).  A page out of [0, n_page) is neither read nor written
+ * (VD_ERR_DEVICE_PAGE); outputs that needed it are unspecified.
+ * ------------------------------------------------------------------------ */
+typedef enum { VD_PAGED_BF16 = 0, VD_PAGED_E4M3 = 1 } vd_paged_type;
+
+typedef struct {
+  void* k;                   /* device: layer 0, page 0, KV head 0, slot 0; rows of head_dim
+                                values lie together */
+  void* v;                   /* the same layout as k */
+  const float* k_scale;      /* VD_PAGED_E4M3: fp32 device [n_layer][n_kv_head], above 0, or
+                                NULL (1); VD_PAGED_BF16: NULL */
+  const float* v_scale;
+  const int32_t* page_table; /* device int32 [n_seq][max_pages] */
+  int32_t* len;              /* device int32 [n_seq], as in vd_cache */
+  int64_t layer_stride;      /* strides of k and v in elements: so heads may hold their slots */
+  int64_t page_stride;       /*   together ([n_page][n_kv_head][page_size][head_dim]) or slots */
+  int64_t head_stride;       /*   their heads ([n_page][page_size][n_kv_head][head_dim]), and */
+  int64_t slot_stride;       /*   k and v may lie in one buffer */
+  int32_t type;              /* vd_paged_type */
+  int32_t n_seq, n_layer, n_kv_head;
+  int32_t head_dim;          /* multiple of 8 (bf16) or 16 (e4m3), at most 256 */
+  int32_t page_size;         /* slots of a page, any number */
+  int32_t n_page;            /* pages of a layer */
+  int32_t max_pages;         /* pages of a sequence at most */
+} vd_paged_cache;
+
+/* The rows of new tokens from their projections into one layer of a paged cache, in one
+ * pass: norms and rotation as in vd_qkv_norm_rope (whose arguments these are), queries to
+ * q_out, keys and values to slots [len, len + n_new).  len stays (vd_paged_advance).
+ *   qkv           bf16 device [n_seq][B][n_q_head + 2 * n_kv_head][head_dim].
+ *   n_new         nullable int32 device [n_seq]: new tokens of each sequence, in [0, B]
+ *                 (NULL: B).  What lies behind them in qkv is padding: its queries are not
+ *                 written.
+ *   pos_first_new nullable int32 device [n_seq]: position of the first new token (after an
+ *                 eviction positions run ahead of slots); NULL: the slot, len.
+ * Numbers and limits as in vd_qkv_norm_rope; keys and values are rounded once, into the page's
+ * type. */
+vd_status vd_paged_append(const vd_paged_cache* c, int32_t layer, const void* qkv, int32_t B,
+                          int32_t n_q_head, const int32_t* n_new, const void* q_weight,
+                          const void* k_weight, float eps, const float* inv_freq,
+                          int32_t rotary_dim, int32_t interleaved, const int32_t* pos_first_new,
+                          void* q_out, vd_stream_t stream);
+
+/* Attention of B new tokens per sequence over one layer of a paged cache:
+ *   s_j = scale * q . k_j,  out = sum_j softmax(s)_j v_j
+ * over slots j < len + i + 1 for token i (causal: the new tokens' rows are in the pages,
+ * vd_paged_append) or, with causal = 0, over slots j < len.
+ *   q, out        bf16 device [n_seq][B][n_q_head][head_dim], 16-byte aligned; query head h
+ *                 reads KV head h / (n_q_head / n_kv_head).
+ *   n_q_head      a multiple of n_kv_head; B * n_q_head / n_kv_head query rows per KV head, at
+ *                 most 2^24, and n_seq * B * n_q_head at most 2^31 - 1 in all
+ *                 (VD_ERR_UNSUPPORTED).
+ *   n_new         as above; what lies behind the new tokens in out and lse_out is left as it was.
+ *   scale         above 0, at most 3.4e38 (VD_ERR_INVALID_ARG).
+ *   lse_out       nullable fp32 device [n_seq][B][n_q_head]: log sum_j exp(s_j).
+ *   workspace     device, 16-byte aligned, of at least vd_paged_attend_workspace bytes
+ *                 (VD_ERR_INVALID_ARG if workspace_bytes is less): the parts of a long
+ *                 sequence are joined there.  Its content means nothing between calls; calls
+ *                 that may run at the same time (on two streams, in two graphs) need one each.
+ * A token that sees no slot, or whose scores are all -infinity, gets out = 0 and lse = -inf.
+ * Values that a token does not see do not reach it, NaN and infinities among them.  Scores,
+ * softmax statistics and sums are fp32; weights are rounded to two bf16 parts (2^-16 of
+ * themselves) for bf16 pages and to fp16 for e4m3 ones, where those below 2^-36 of the largest
+ * count for nothing.
+ * Range: products q . k and sums of values times weights of up to 2^8 have to be finite in fp32;
+ * with e4m3 pages, scale times the scales and a query row's largest magnitude has to lie in
+ * [2^-60, 2^60].
+ * The same inputs give the same bits on the same GPU.  out must not overlap the inputs. */
+vd_status vd_paged_attend(const vd_paged_cache* c, int32_t layer, const void* q, int32_t B,
+                          int32_t n_q_head, const int32_t* n_new, int32_t causal, float scale,
+                          void* out, float* lse_out, void* workspace, size_t workspace_bytes,
+                          vd_stream_t stream);
+
+/* Bytes of workspace that vd_paged_attend takes on the current device for B tokens of
+ * n_q_head heads, whatever the lengths (0 where the arguments are refused). */
+size_t vd_paged_attend_workspace(const vd_paged_cache* c, int32_t n_q_head, int32_t B);
+
+/* len[s] += n_new[s] (NULL: B), at the end of a step, after its last layer. */
+vd_status vd_paged_advance(const vd_paged_cache* c, const int32_t* n_new, int32_t B,
+                           vd_stream_t stream);
+
+/* Rows [0, src->len) of a bf16 cache (an evicted one, say) into layers
+ * [layer0, layer0 + src->n_layer) of dst, and the way back (as bf16), so that every vd_evict_*
+ * call can run on them.  n_seq, n_kv_head and head_dim have to agree (VD_ERR_INVALID_ARG);
+ * a sequence longer than the other side holds is left untouched (VD_ERR_DEVICE_LEN).
+ * vd_paged_pack's call that writes dst's last layer also sets dst->len to src->len; layer by
+ * layer, call it in layer order.  vd_paged_unpack sets dst->len to src->len.  Pages that pack
+ * writes belong to one sequence each. */
+vd_status vd_paged_pack(const vd_paged_cache* dst, int32_t layer0, const vd_cache* src,
+                        vd_stream_t stream);
+vd_status vd_paged_unpack(const vd_paged_cache* src, int32_t layer0, const vd_cache* dst,
+                          vd_stream_t stream);
 
 /* Device scratch the calls need beyond their arguments: always 0 (the fused
  * kernels keep every intermediate on chip). */

@@ -27,11 +27,14 @@ __all__ = [
     "vd_running_sum_init", "vd_running_sum_init_ex", "vd_workspace_size", "vd_status_string",
     "vd_get_device_status",
     "Q4Cache", "vd_q4_append", "vd_q4_pack", "vd_q4_unpack", "vd_q4_attend", "vd_qkv_norm_rope",
+    "VD_PAGED_BF16", "VD_PAGED_E4M3", "PagedCache", "vd_paged_append", "vd_paged_attend",
+    "vd_paged_attend_workspace", "vd_paged_advance", "vd_paged_pack", "vd_paged_unpack",
     "library_path", "load_library",
 ]
 
 VD_SCORE_L2, VD_SCORE_DIR, VD_SCORE_NORM = 0, 1, 2
 VD_MU_RECOMPUTE, VD_MU_RUNNING = 0, 1
+VD_PAGED_BF16, VD_PAGED_E4M3 = 0, 1
 VARIANTS = {"l2": VD_SCORE_L2, "dir": VD_SCORE_DIR, "norm": VD_SCORE_NORM}
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -58,6 +61,18 @@ class _VdQ4Cache(ctypes.Structure):
                 ("v_scale", ctypes.c_void_p), ("len", ctypes.c_void_p), ("n_seq", ctypes.c_int32),
                 ("n_layer", ctypes.c_int32), ("n_kv_head", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("capacity", ctypes.c_int32)]
+
+
+class _VdPagedCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("len", ctypes.c_void_p), ("layer_stride", ctypes.c_int64),
+                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("slot_stride", ctypes.c_int64), ("type", ctypes.c_int32),
+                ("n_seq", ctypes.c_int32), ("n_layer", ctypes.c_int32),
+                ("n_kv_head", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_page", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32)]
 
 
 def library_path() -> str:
@@ -98,6 +113,14 @@ def load_library() -> ctypes.CDLL:
             lib.vd_q4_attend.argtypes = [qp, I32, P, I32, P, P, I32, F, P, P, P]
             lib.vd_qkv_norm_rope.argtypes = [P, I32, I32, I32, I32, I32, P, P, F, P, I32, I32, P,
                                              P, P, P, I32, I32, P]
+            pp, Z = ctypes.POINTER(_VdPagedCache), ctypes.c_size_t
+            lib.vd_paged_append.argtypes = [pp, I32, P, I32, I32, P, P, P, F, P, I32, I32, P, P, P]
+            lib.vd_paged_attend.argtypes = [pp, I32, P, I32, I32, P, I32, F, P, P, P, Z, P]
+            lib.vd_paged_attend_workspace.argtypes = [pp, I32, I32]
+            lib.vd_paged_attend_workspace.restype = Z
+            lib.vd_paged_advance.argtypes = [pp, P, I32, P]
+            lib.vd_paged_pack.argtypes = [pp, I32, cp, P]
+            lib.vd_paged_unpack.argtypes = [pp, I32, cp, P]
             lib.vd_workspace_size.argtypes = [cp]
             lib.vd_workspace_size.restype = ctypes.c_size_t
             lib.vd_status_string.argtypes = [S]
@@ -108,7 +131,8 @@ def load_library() -> ctypes.CDLL:
                       "vd_evict_decode", "vd_evict_block_holefill",
                       "vd_evict_decode_holefill", "vd_append", "vd_running_sum_init",
                       "vd_running_sum_init_ex", "vd_q4_append", "vd_q4_pack", "vd_q4_unpack",
-                      "vd_q4_attend", "vd_qkv_norm_rope",
+                      "vd_q4_attend", "vd_qkv_norm_rope", "vd_paged_append", "vd_paged_attend",
+                      "vd_paged_advance", "vd_paged_pack", "vd_paged_unpack",
                       "vd_get_device_status"):
                 getattr(lib, f).restype = S
             _lib = lib
@@ -264,6 +288,66 @@ class Q4Cache:
 
     def unit_shape(self):
         return self._unit_shape
+
+    def ref(self):
+        """What a call hands to the library; a cache that is not on a GPU is refused."""
+        if not self._gpu:
+            _on_gpu(self.device)
+        return self._ref
+
+
+class PagedCache:
+    """A KV cache in pages (layout: vd_paged_cache in ``include/vd.h``): K and V bf16 or
+    float8_e4m3fn [n_layer, n_page, n_kv_head, page_size, head_dim], of equal strides and with
+    rows that lie together (a transposed [n_layer, n_page, page_size, n_kv_head, head_dim] is
+    one), the page table int32 [n_seq, max_pages], len int32 [n_seq] and, for float8 pages,
+    scales fp32 [n_layer, n_kv_head] (or None: 1); all on one CUDA device.  Holds references to
+    the tensors only."""
+
+    def __init__(self, k, v, page_table, len, k_scale=None, v_scale=None):
+        torch = _torch()
+        if k.dim() != 5 or page_table.dim() != 2:
+            raise ValueError("k must be [n_layer, n_page, n_kv_head, page_size, head_dim], page_table "
+                             "[n_seq, max_pages]")
+        if k.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+            raise TypeError(f"k must be torch.bfloat16 or torch.float8_e4m3fn, got {k.dtype}")
+        self.k, self.v, self.page_table, self.len = k, v, page_table, len
+        self.k_scale, self.v_scale = k_scale, v_scale
+        (self.n_layer, self.n_page, self.n_kv_head, self.page_size,
+         self.head_dim) = (int(x) for x in k.shape)
+        self.n_seq, self.max_pages = (int(x) for x in page_table.shape)
+        self.device = k.device
+        self.type = VD_PAGED_BF16 if k.dtype == torch.bfloat16 else VD_PAGED_E4M3
+        if v.dtype != k.dtype:
+            raise TypeError(f"v must be {k.dtype}, got {v.dtype}")
+        if v.device != k.device:
+            raise ValueError(f"v must live on {k.device}, got {v.device}")
+        if v.shape != k.shape:
+            raise ValueError(f"v must have shape {tuple(k.shape)}, got {tuple(v.shape)}")
+        for d, (n, sk, sv) in enumerate(zip(k.shape, k.stride(), v.stride())):
+            if n > 1 and (sk != sv or (d == 4 and sk != 1)):
+                raise ValueError("k and v must have equal strides, and rows that lie together")
+        _ptr(page_table, torch.int32, page_table.shape, "page_table", self.device)
+        _ptr(len, torch.int32, (self.n_seq,), "len", self.device)
+        scales = (self.n_layer, self.n_kv_head)
+        s = [_ptr(x, torch.float32, scales, name, self.device)
+             for x, name in ((k_scale, "k_scale"), (v_scale, "v_scale"))]
+        self._s = _VdPagedCache(k.data_ptr(), v.data_ptr(), s[0], s[1], page_table.data_ptr(),
+                                len.data_ptr(), *k.stride()[:4], self.type, self.n_seq,
+                                self.n_layer, self.n_kv_head, self.head_dim, self.page_size,
+                                self.n_page, self.max_pages)
+        self._ref = ctypes.byref(self._s)
+        self._gpu = self.device.type == "cuda"
+
+    @classmethod
+    def empty(cls, n_seq, n_layer, n_kv_head, head_dim, n_page, page_size, max_pages, dtype=None,
+              device="cuda"):
+        """A cache of zeros without a page: page_table is all -1."""
+        torch = _torch()
+        shape = (n_layer, n_page, n_kv_head, page_size, head_dim)
+        k, v = (torch.zeros(shape, dtype=dtype or torch.bfloat16, device=device) for _ in range(2))
+        return cls(k, v, torch.full((n_seq, max_pages), -1, dtype=torch.int32, device=device),
+                   torch.zeros(n_seq, dtype=torch.int32, device=device))
 
     def ref(self):
         """What a call hands to the library; a cache that is not on a GPU is refused."""
@@ -531,10 +615,10 @@ def vd_q4_append(cache: Q4Cache, k_new, v_new, B: int, stream=None) -> None:
            "vd_q4_append")
 
 
-def _same_device(q4: Q4Cache, cache: Cache, stream):
-    if q4.device != cache.device:
-        raise ValueError(f"cache must live on {q4.device}, got {cache.device}")
-    return _launch_stream(q4.device, stream)
+def _same_device(stored, cache: Cache, stream):
+    if stored.device != cache.device:
+        raise ValueError(f"cache must live on {stored.device}, got {cache.device}")
+    return _launch_stream(stored.device, stream)
 
 
 def vd_q4_pack(dst: Q4Cache, src: Cache, layer0: int = 0, stream=None) -> None:
@@ -618,6 +702,91 @@ def vd_qkv_norm_rope(qkv, q_out, k_new, v_new, layer: int = 0, q_weight=None, k_
                                            float(eps), args[3], 2 * pairs, int(bool(interleaved)),
                                            args[4], args[5], args[6], args[7], int(layer), n_layer, s),
            "vd_qkv_norm_rope")
+
+
+def vd_paged_append(cache: PagedCache, qkv, q_out, layer: int = 0, q_weight=None, k_weight=None,
+                    eps: float = 1e-6, inv_freq=None, pos_first_new=None,
+                    interleaved: bool = False, n_new=None, stream=None) -> None:
+    """vd_qkv_norm_rope whose keys and values go to slots [len, len + n_new) of one layer of a
+    paged cache (n_new int32 [n_seq], or None: all B); without pos_first_new a token's
+    position is its slot.  len stays until vd_paged_advance."""
+    torch = _torch()
+    if qkv.dim() != 4 or q_out.dim() != 4:
+        raise ValueError("qkv and q_out must have 4 dimensions")
+    dev, n_seq, d = cache.device, cache.n_seq, cache.head_dim
+    s = _launch_stream(dev, stream)
+    _, B, heads, _ = qkv.shape
+    n_q = heads - 2 * cache.n_kv_head
+    pairs = 0 if inv_freq is None else inv_freq.numel()
+    args = (
+        _ptr(qkv, torch.bfloat16, (n_seq, B, heads, d), "qkv", dev),
+        _ptr(n_new, torch.int32, (n_seq,), "n_new", dev),
+        _ptr(q_weight, torch.bfloat16, (d,), "q_weight", dev),
+        _ptr(k_weight, torch.bfloat16, (d,), "k_weight", dev),
+        _ptr(inv_freq, torch.float32, (pairs,), "inv_freq", dev),
+        _ptr(pos_first_new, torch.int32, (n_seq,), "pos_first_new", dev),
+        _ptr(q_out, torch.bfloat16, (n_seq, B, n_q, d), "q_out", dev),
+    )
+    _check(load_library().vd_paged_append(cache.ref(), int(layer), args[0], B, n_q, args[1],
+                                          args[2], args[3], float(eps), args[4], 2 * pairs,
+                                          int(bool(interleaved)), args[5], args[6], s),
+           "vd_paged_append")
+
+
+def vd_paged_attend_workspace(cache: PagedCache, n_q_head: int, B: int) -> int:
+    """Bytes of workspace that vd_paged_attend takes on the current device."""
+    return int(load_library().vd_paged_attend_workspace(cache._ref, int(n_q_head), int(B)))
+
+
+def vd_paged_attend(cache: PagedCache, q, out, workspace, layer: int = 0, causal: bool = True,
+                    scale=None, n_new=None, lse_out=None, stream=None) -> None:
+    """Attention of new tokens over one layer of a paged cache: token i over slots
+    [0, len + i + 1) (causal: its own row is in the pages, vd_paged_append) or over
+    [0, len).  q, out: bf16 [n_seq, B, n_q_head, head_dim]; workspace: uint8, at least
+    vd_paged_attend_workspace bytes, one for each stream and graph that may run at the same
+    time; n_new int32 [n_seq], or None: all B; scale: 1 / sqrt(head_dim) unless given; lse_out:
+    fp32 [n_seq, B, n_q_head]."""
+    torch = _torch()
+    dev = cache.device
+    s = _launch_stream(dev, stream)
+    if q.dim() != 4:
+        raise ValueError("q must be [n_seq, B, n_q_head, head_dim]")
+    _, B, n_q, _ = q.shape
+    shape = (cache.n_seq, B, n_q, cache.head_dim)
+    args = (
+        _ptr(q, torch.bfloat16, shape, "q", dev),
+        _ptr(n_new, torch.int32, (cache.n_seq,), "n_new", dev),
+        _ptr(out, torch.bfloat16, shape, "out", dev),
+        _ptr(lse_out, torch.float32, shape[:3], "lse_out", dev),
+        _ptr(workspace, torch.uint8, (workspace.numel(),), "workspace", dev),
+    )
+    scale = cache.head_dim ** -0.5 if scale is None else float(scale)
+    _check(load_library().vd_paged_attend(cache.ref(), int(layer), args[0], B, n_q, args[1],
+                                          int(bool(causal)), scale, args[2], args[3], args[4],
+                                          workspace.numel(), s),
+           "vd_paged_attend")
+
+
+def vd_paged_advance(cache: PagedCache, B: int = 1, n_new=None, stream=None) -> None:
+    """len += n_new (int32 [n_seq], at most B each; None: B), at the end of a step."""
+    torch = _torch()
+    s = _launch_stream(cache.device, stream)
+    n = _ptr(n_new, torch.int32, (cache.n_seq,), "n_new", cache.device)
+    _check(load_library().vd_paged_advance(cache.ref(), n, int(B), s), "vd_paged_advance")
+
+
+def vd_paged_pack(dst: PagedCache, src: Cache, layer0: int = 0, stream=None) -> None:
+    """Rows [0, src.len) of a bf16 cache into layers [layer0, layer0 + src.n_layer) of a
+    paged one; the call that writes the last layer also sets dst.len."""
+    s = _same_device(dst, src, stream)
+    _check(load_library().vd_paged_pack(dst.ref(), int(layer0), src.ref(), s), "vd_paged_pack")
+
+
+def vd_paged_unpack(src: PagedCache, dst: Cache, layer0: int = 0, stream=None) -> None:
+    """Rows [0, src.len) of layers [layer0, layer0 + dst.n_layer) of a paged cache to bf16
+    in dst, and dst.len = src.len."""
+    s = _same_device(src, dst, stream)
+    _check(load_library().vd_paged_unpack(src.ref(), int(layer0), dst.ref(), s), "vd_paged_unpack")
 
 
 def vd_workspace_size(cache: Cache) -> int:

@@ -1041,6 +1041,7 @@ const char* vd_status_string(vd_status st) {
     case VD_ERR_DEVICE_BUDGET: return "device: budget out of range or decode over budget";
     case VD_ERR_NO_DEVICE: return "no sm_103 CUDA device";
     case VD_ERR_INTERNAL: return "device: inconsistent slot list (internal self-check)";
+    case VD_ERR_DEVICE_PAGE: return "device: page out of range";
     default: return "unknown status";
   }
 }

@@ -1,0 +1,82 @@
+// vd_paged.cuh -- a paged cache (vd_paged_cache in include/vd.h): where its rows lie, what
+// every call checks of it.
+#pragma once
+
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "vd_host.cuh"
+
+namespace vd {
+
+constexpr unsigned kStDevicePage = 11;
+
+// One layer of a paged cache, for kernels.  Offsets and strides are in bytes.
+struct Pages {
+  char *k, *v;
+  const float *k_scale, *v_scale;  // of the layer's heads (nullable)
+  const int32_t* table;
+  const int32_t* len;
+  unsigned* status;
+  long long page_stride, head_stride, slot_stride;
+  int page_size, n_page, max_pages;
+
+  __device__ __forceinline__ int capacity() const { return page_size * max_pages; }
+  // The page that holds a slot, -1 (recorded) if the table names none.
+  __device__ __forceinline__ int page_of(int seq, int slot) const {
+    const int p = __ldcg(table + (size_t)seq * max_pages + slot / page_size);
+    if ((unsigned)p < (unsigned)n_page) return p;
+    record_status(status, kStDevicePage);
+    return -1;
+  }
+  __device__ __forceinline__ long long row(int page, int slot) const {
+    return page * page_stride + (slot % page_size) * slot_stride;
+  }
+};
+
+vd_status validate_paged(const vd_paged_cache* c);
+
+inline Pages pages_of(const vd_paged_cache* c, int layer, unsigned* status) {
+  const int size = c->type == VD_PAGED_E4M3 ? 1 : 2;
+  Pages p;
+  p.k = static_cast<char*>(c->k) + layer * c->layer_stride * size;
+  p.v = static_cast<char*>(c->v) + layer * c->layer_stride * size;
+  p.k_scale = c->k_scale ? c->k_scale + (size_t)layer * c->n_kv_head : nullptr;
+  p.v_scale = c->v_scale ? c->v_scale + (size_t)layer * c->n_kv_head : nullptr;
+  p.table = c->page_table;
+  p.len = c->len;
+  p.status = status;
+  p.page_stride = c->page_stride * size;
+  p.head_stride = c->head_stride * size;
+  p.slot_stride = c->slot_stride * size;
+  p.page_size = c->page_size;
+  p.n_page = c->n_page;
+  p.max_pages = c->max_pages;
+  return p;
+}
+
+// Four fp32 values to e4m3, the first in the lowest byte: to nearest, ties to even,
+// magnitudes above 448 to 448, NaN to NaN.
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
+  uint32_t r;
+  asm("{ .reg .b16 l, h;\n"
+      "cvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n"
+      "cvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n"
+      "mov.b32 %0, {l, h}; }"
+      : "=r"(r)
+      : "f"(a), "f"(b), "f"(c), "f"(d));
+  return r;
+}
+
+// Two e4m3 values (the low or the high half of w) to two fp16 ones, exactly.
+__device__ __forceinline__ uint32_t e4m3_to_h2(uint32_t w, bool high) {
+  uint32_t r;
+  if (high)
+    asm("{ .reg .b16 l, h; mov.b32 {l, h}, %1; cvt.rn.f16x2.e4m3x2 %0, h; }" : "=r"(r) : "r"(w));
+  else
+    asm("{ .reg .b16 l, h; mov.b32 {l, h}, %1; cvt.rn.f16x2.e4m3x2 %0, l; }" : "=r"(r) : "r"(w));
+  return r;
+}
+
+}  // namespace vd
