@@ -21,17 +21,23 @@ struct Pages {
   unsigned* status;
   long long page_stride, head_stride, slot_stride;
   int page_size, n_page, max_pages;
+  uint32_t per_page;  // 2^page_shift / page_size, rounded up
+  int page_shift;
 
+  // Exact for slots below 2^30.
+  __device__ __forceinline__ int place_of(int slot) const {
+    return (int)(((uint64_t)(uint32_t)slot * per_page) >> page_shift);
+  }
   __device__ __forceinline__ int capacity() const { return page_size * max_pages; }
   // The page that holds a slot, -1 (recorded) if the table names none.
   __device__ __forceinline__ int page_of(int seq, int slot) const {
-    const int p = __ldcg(table + (size_t)seq * max_pages + slot / page_size);
+    const int p = __ldcg(table + (size_t)seq * max_pages + place_of(slot));
     if ((unsigned)p < (unsigned)n_page) return p;
     record_status(status, kStDevicePage);
     return -1;
   }
   __device__ __forceinline__ long long row(int page, int slot) const {
-    return page * page_stride + (slot % page_size) * slot_stride;
+    return page * page_stride + (slot - place_of(slot) * page_size) * slot_stride;
   }
 };
 
@@ -53,6 +59,11 @@ inline Pages pages_of(const vd_paged_cache* c, int layer, unsigned* status) {
   p.page_size = c->page_size;
   p.n_page = c->n_page;
   p.max_pages = c->max_pages;
+  // for slots n < 2^30: n / page_size = n per_page >> page_shift, as per_page page_size exceeds
+  // 2^page_shift by less than page_size <= 2^(page_shift - 30)
+  p.page_shift = 30;
+  while ((1LL << (p.page_shift - 30)) < c->page_size) ++p.page_shift;
+  p.per_page = (uint32_t)(((1ull << p.page_shift) + c->page_size - 1) / c->page_size);
   return p;
 }
 

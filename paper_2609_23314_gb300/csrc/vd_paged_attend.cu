@@ -12,145 +12,13 @@
 #include "vd_host.cuh"
 #include "vd_paged.cuh"
 #include "vd_paged_attend.cuh"
+#include "vd_paged_stream.cuh"
 
 namespace vd {
 
 namespace {
 
-constexpr int kTileRows = 4;
 constexpr int kMaxDim = 256;
-
-struct Row8 {
-  float x[8];
-};
-
-template <bool E4M3>
-__device__ __forceinline__ Row8 load8(const char* p, float scale) {
-  Row8 r;
-  if (E4M3) {
-    const uint2 w = __ldcg(reinterpret_cast<const uint2*>(p));
-    const uint32_t h[4] = {e4m3_to_h2(w.x, false), e4m3_to_h2(w.x, true), e4m3_to_h2(w.y, false),
-                           e4m3_to_h2(w.y, true)};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      asm("{ .reg .b16 a, b; mov.b32 {a, b}, %2; cvt.f32.f16 %0, a; cvt.f32.f16 %1, b; }"
-          : "=f"(r.x[2 * i]), "=f"(r.x[2 * i + 1])
-          : "r"(h[i]));
-      r.x[2 * i] *= scale;
-      r.x[2 * i + 1] *= scale;
-    }
-  } else {
-    unpack8(ld_cg16(p), r.x);
-  }
-  return r;
-}
-
-// A lane has 8 of the head's values (head_dim 256 fills a warp), a warp a token at a time.
-template <bool E4M3>
-__global__ void __launch_bounds__(kThreads, 1) paged_attend_kernel(PagedAttendArgs a) {
-  __shared__ long long sh[kWarps + 1 + kThreads];
-  __shared__ float part[kWarps][kTileRows][kMaxDim / 8][8];
-  __shared__ float stat[kWarps][kTileRows][2];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  grid_dependency_wait();
-  grid_launch_dependents();
-  write_empty(a);
-  Walk walk(a, sh, kWarps);
-  if (threadIdx.x == 0) a.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
-  const bool on = lane < a.d / 8;
-  const Row8 zero = {};
-  Share s;
-  while (walk.next(s)) {
-    Row8 q[kTileRows], o[kTileRows];
-    float m[kTileRows], l[kTileRows];
-    int sees[kTileRows];
-#pragma unroll
-    for (int i = 0; i < kTileRows; ++i) {
-      const long long row = out_row(a, s, i);
-      q[i] = on && row >= 0 ? load8<false>(reinterpret_cast<const char*>(a.q + row * a.d + lane * 8), 1.f)
-                            : zero;
-      o[i] = zero;
-      m[i] = -INFINITY;
-      l[i] = 0.f;
-      sees[i] = a.causal ? s.w.len + (s.tile * kTileRows + i) / a.group + 1 : s.w.len;
-    }
-    const float ks = a.pages.k_scale ? a.pages.k_scale[s.head] : 1.f;
-    const float vs = a.pages.v_scale ? a.pages.v_scale[s.head] : 1.f;
-    const long long in = s.head * a.pages.head_stride + lane * (E4M3 ? 8 : 16);
-    for (int stage = s.s0 + warp; stage < s.s1; stage += kWarps) {
-      const int last = min(s.w.total, (stage + 1) * kStageKeys);
-      for (int t = stage * kStageKeys; t < last; ++t) {
-        const int page = a.pages.page_of(s.seq, t);
-        if (page < 0) continue;
-        const long long at = a.pages.row(page, t) + in;
-        const Row8 k = on ? load8<E4M3>(a.pages.k + at, ks) : zero;
-        const Row8 v = on ? load8<E4M3>(a.pages.v + at, vs) : zero;
-#pragma unroll
-        for (int i = 0; i < kTileRows; ++i) {
-          float x = 0.f;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x = fmaf(q[i].x[e], k.x[e], x);
-#pragma unroll
-          for (int off = 16; off > 0; off >>= 1) x += __shfl_xor_sync(kFull, x, off);
-          x *= a.scale;
-          x = x * kLog2e;
-          if (t >= sees[i] || x == -INFINITY) continue;
-          const float top = fmaxf(m[i], x), f = exp2f(m[i] - top), p = exp2f(x - top);
-          m[i] = top;
-          l[i] = l[i] * f + p;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) o[i].x[e] = o[i].x[e] * f + p * v.x[e];
-        }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < kTileRows; ++i) {
-      if (l[i] != l[i] && m[i] == -INFINITY) m[i] = 0.f;  // all scores NaN: so is the output
-      if (on)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) part[warp][i][lane][e] = o[i].x[e];
-      if (lane == 0) {
-        stat[warp][i][0] = m[i];
-        stat[warp][i][1] = l[i];
-      }
-    }
-    __syncthreads();
-    // warp i joins row i
-    if (warp < kTileRows) {
-    float top = -INFINITY, sum = 0.f;
-    Row8 y = zero;
-    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, stat[w][warp][0]);
-    for (int w = 0; w < kWarps; ++w) {
-      const float f = stat[w][warp][0] == -INFINITY ? 0.f : exp2f(stat[w][warp][0] - top);
-      if (f == 0.f) continue;
-      sum += f * stat[w][warp][1];
-      if (on)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y.x[e] += f * part[w][warp][lane][e];
-    }
-    const long long row = out_row(a, s, warp);
-    if (s.whole) {
-      if (row >= 0) {
-        const float r = top == -INFINITY ? 0.f : 1.f / sum;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y.x[e] *= r;
-        if (on) st16(a.out + row * a.d + lane * 8, pack8(y.x));
-        if (a.lse && lane == 0) a.lse[row] = (top + log2f(sum)) * kLn2;
-      }
-    } else {
-      const size_t at = (size_t)s.slot * kTileRows + warp;
-      if (on) {
-        float4* dst = reinterpret_cast<float4*>(a.parts + at * a.d + lane * 8);
-        dst[0] = make_float4(y.x[0], y.x[1], y.x[2], y.x[3]);
-        dst[1] = make_float4(y.x[4], y.x[5], y.x[6], y.x[7]);
-      }
-      if (lane == 0) a.stats[at] = make_float2(top, sum);
-      if (threadIdx.x == 0 && s.s0 == 0) a.split[blockIdx.x] = walk.split_of(s);
-    }
-    }
-    __syncthreads();
-  }
-}
 
 // A CTA puts together one row of the unit that CTA `first` of the kernel before begins and
 // does not end.
@@ -167,7 +35,8 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(PagedAttendArgs a)
   s.seq = unit.x;
   s.head = unit.y;
   s.tile = unit.z;
-  s.w = seq_work(a, s.seq, false);
+  const int2 size = seq_size(a, s.seq, false);
+  s.w = seq_work(a, size.x, size.y);
   const long long row = out_row(a, s, i);
   if (row < 0) return;
   const int n = unit.w - first + 1;
@@ -215,6 +84,7 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(PagedAttendArgs a)
 }
 
 struct Plan {
+  const PagedKernel* kernel;
   int rows, ctas;
   size_t split, stats, parts;  // bytes of the workspace's three parts
 };
@@ -230,8 +100,10 @@ vd_status plan_of(const vd_paged_cache* c, int n_q_head, int B, Plan* plan) {
   DeviceInfo dev;
   r = device_info(&dev);
   if (r != VD_OK) return r;
-  plan->rows = kTileRows;
-  plan->ctas = 2 * dev.sms;
+  const auto& kernels = c->type == VD_PAGED_E4M3 ? kPagedE4m3 : kPagedBf16;
+  plan->kernel = &kernels[(c->head_dim + 31) / 32 - 1][rows > 8];
+  plan->rows = plan->kernel->rows;
+  plan->ctas = dev.sms;
   const size_t parts = 2 * (size_t)plan->ctas * plan->rows;
   plan->split = (size_t)plan->ctas * sizeof(int4);
   plan->stats = parts * sizeof(float2);
@@ -287,10 +159,13 @@ vd_status vd_paged_attend(const vd_paged_cache* c, int32_t layer, const void* q,
   a.causal = causal != 0;
   a.scale = scale;
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  r = launch_dependent((unsigned)p.ctas, s,
-                       c->type == VD_PAGED_E4M3 ? paged_attend_kernel<true>
-                                                : paged_attend_kernel<false>,
-                       a);
+  const PagedKernel& k = *p.kernel;
+  if (cudaFuncSetAttribute(k.kern, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem) !=
+      cudaSuccess) {
+    cudaGetLastError();
+    return VD_ERR_CUDA;
+  }
+  r = launch_clusters((unsigned)p.ctas, (unsigned)k.threads, 1, k.smem, s, k.kern, a);
   if (r != VD_OK) return r;
   return launch_dependent((unsigned)(p.ctas * p.rows), s, paged_join_kernel, a);
 }

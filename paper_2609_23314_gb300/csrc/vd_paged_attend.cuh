@@ -13,6 +13,7 @@
 #include <cstdint>
 #include <cuda_runtime.h>
 
+#include "vd_attend.cuh"
 #include "vd_device.cuh"
 #include "vd_paged.cuh"
 
@@ -35,7 +36,7 @@ struct PagedAttendArgs {
   float scale;
 };
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
+constexpr float kLn2 = 0.69314718055994531f;
 
 // What a sequence has to do.
 struct SeqWork {
@@ -44,32 +45,23 @@ struct SeqWork {
   long long work;              // stages of all its units
 };
 
-__device__ __forceinline__ SeqWork seq_work(const PagedAttendArgs& a, int seq, bool report) {
-  SeqWork w;
-  w.len = __ldcg(a.pages.len + seq);
-  w.add = a.n_new ? __ldcg(a.n_new + seq) : a.B;
-  if (w.add < 0 || w.add > a.B || w.len < 0 || w.len > a.pages.capacity() - (a.causal ? w.add : 0)) {
-    if (report) record_status(a.pages.status, kStDeviceLen);
-    w.len = w.add = 0;
-  }
-  w.total = w.add == 0 ? 0 : w.len + (a.causal ? w.add : 0);
-  w.tiles = (w.add * a.group + a.rows - 1) / a.rows;
+__device__ __forceinline__ SeqWork seq_work(const PagedAttendArgs& a, int len, int add) {
+  SeqWork w = {len, add, 0, 0, 0, 0};
+  w.total = add == 0 ? 0 : len + (a.causal ? add : 0);
+  w.tiles = (add * a.group + a.rows - 1) / a.rows;
   w.stages = (w.total + kStageKeys - 1) / kStageKeys;
   w.work = (long long)w.stages * w.tiles * a.heads;
   return w;
 }
 
-__device__ __forceinline__ long long block_sum_i64(long long v, long long* sh) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(kFull, v, off);
-  if (lane == 0) sh[warp] = v;
-  __syncthreads();
-  long long t = 0;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) t += sh[w];
-  __syncthreads();
-  return t;
+// Length and new tokens of a sequence, none of which where they are out of range.
+__device__ __forceinline__ int2 seq_size(const PagedAttendArgs& a, int seq, bool report) {
+  const int len = __ldcg(a.pages.len + seq), add = a.n_new ? __ldcg(a.n_new + seq) : a.B;
+  if (add < 0 || add > a.B || len < 0 || len > a.pages.capacity() - (a.causal ? add : 0)) {
+    if (report) record_status(a.pages.status, kStDeviceLen);
+    return make_int2(0, 0);
+  }
+  return make_int2(len, add);
 }
 
 // The line cut into `ctas` pieces: the first `more` have one stage more.
@@ -91,22 +83,42 @@ struct Share {
   SeqWork w;
   bool whole;
   int slot;  // of the part
+  int last;  // the last CTA that has a part of the unit, where this share begins it
+};
+
+constexpr int kChunk = 64;  // sequences that a walk looks at together
+
+struct WalkMem {
+  long long end[kChunk];  // where each ends on the line
+  int2 size[kChunk];
+  long long sum[32];
 };
 
 // Walks over a CTA's piece of the line.  All threads of the CTA make the same calls.
 struct Walk {
   const PagedAttendArgs& a;
-  long long* sh;  // kWarps + 1 + kThreads entries
+  WalkMem& m;
   Cut cut;
   long long at, end, seq_begin;  // line positions: the next stage, the piece's end, seq's first
-  int seq, chunk;                // chunk: first sequence of those whose ends are in sh
+  int seq, chunk;                // chunk: the first of the sequences in m
 
-  __device__ Walk(const PagedAttendArgs& args, long long* shared, int least)
-      : a(args), sh(shared), at(0), end(0), seq_begin(0), seq(0), chunk(0) {
-    long long mine = 0;
-    for (int s = threadIdx.x; s < a.n_seq; s += kThreads)
-      mine += seq_work(a, s, blockIdx.x == 0).work;
-    const long long all = block_sum_i64(mine, sh);
+  // Pieces of `least` stages at least.
+  __device__ Walk(const PagedAttendArgs& args, WalkMem& mem, int least)
+      : a(args), m(mem), at(0), end(0), seq_begin(0), seq(0), chunk(0) {
+    load(0, blockIdx.x == 0);
+    long long all = m.end[kChunk - 1];
+    if (a.n_seq > kChunk) {
+      long long mine = 0;
+      for (int s = kChunk + threadIdx.x; s < a.n_seq; s += blockDim.x) {
+        const int2 n = seq_size(a, s, blockIdx.x == 0);
+        mine += seq_work(a, n.x, n.y).work;
+      }
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1) mine += __shfl_xor_sync(kFull, mine, off);
+      if ((threadIdx.x & 31) == 0) m.sum[threadIdx.x >> 5] = mine;
+      __syncthreads();
+      for (int w = 0; w < (int)blockDim.x / 32; ++w) all += m.sum[w];
+    }
     const long long most = all / least;
     cut.ctas = most >= (long long)gridDim.x ? (int)gridDim.x : most > 1 ? (int)most : 1;
     cut.per = all / cut.ctas;
@@ -114,39 +126,43 @@ struct Walk {
     if ((int)blockIdx.x >= cut.ctas) return;
     at = cut.begin(blockIdx.x);
     end = cut.begin(blockIdx.x + 1);
-    load(0);
   }
-  // sh[kWarps + 1 + i]: where sequence chunk + i ends on the line
-  __device__ void load(long long begin) {
-    const int s = chunk + threadIdx.x;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    long long x = s < a.n_seq ? seq_work(a, s, false).work : 0;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const long long y = __shfl_up_sync(kFull, x, off);
-      if (lane >= off) x += y;
-    }
+  // The ends of the chunk's sequences, the first of which begins at `begin`; by the first warp.
+  __device__ void load(long long begin, bool report) {
     __syncthreads();  // the last chunk's readers
-    if (lane == 31) sh[warp] = x;
-    __syncthreads();
-    for (int w = 0; w < warp; ++w) begin += sh[w];
-    sh[kWarps + 1 + threadIdx.x] = begin + x;
+    if (threadIdx.x < 32) {
+      const int lane = threadIdx.x;
+#pragma unroll
+      for (int i = 0; i < kChunk; i += 32) {
+        const int s = chunk + i + lane;
+        const int2 n = s < a.n_seq ? seq_size(a, s, report) : make_int2(0, 0);
+        long long x = seq_work(a, n.x, n.y).work;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+          const long long y = __shfl_up_sync(kFull, x, off);
+          if (lane >= off) x += y;
+        }
+        m.end[i + lane] = begin + x;
+        m.size[i + lane] = n;
+        begin += __shfl_sync(kFull, x, 31);
+      }
+    }
     __syncthreads();
   }
   // The next share, if there is one.
   __device__ bool next(Share& s) {
     if (at >= end) return false;
     long long stop;
-    while ((stop = sh[kWarps + 1 + seq - chunk]) <= at) {  // a sequence that is done, or empty
+    while ((stop = m.end[seq - chunk]) <= at) {  // a sequence that is done, or empty
       seq_begin = stop;
       ++seq;
-      if (seq == chunk + kThreads) {
+      if (seq == chunk + kChunk) {
         chunk = seq;
-        load(stop);
+        load(stop, false);
       }
     }
     s.seq = seq;
-    s.w = seq_work(a, seq, false);
+    s.w = seq_work(a, m.size[seq - chunk].x, m.size[seq - chunk].y);
     const long long in = at - seq_begin;
     const int unit = (int)(in / s.w.stages);
     s.s0 = (int)(in - (long long)unit * s.w.stages);
@@ -158,13 +174,8 @@ struct Walk {
     // a CTA's first share may begin inside a unit, its last one may end there
     s.slot = 2 * blockIdx.x + (s.s0 == 0 ? 1 : 0);
     at += s.s1 - s.s0;
+    s.last = s.whole || s.s0 > 0 ? 0 : cut.holder(at + (s.w.stages - s.s1) - 1);
     return true;
-  }
-  // What the join has to know of a share that begins a unit and does not end it: the unit and
-  // the last CTA that has a part of it.
-  __device__ int4 split_of(const Share& s) const {
-    const long long unit_end = at + (s.w.stages - s.s1);
-    return make_int4(s.seq, s.head, s.tile, cut.holder(unit_end - 1));
   }
 };
 
@@ -178,15 +189,16 @@ __device__ __forceinline__ long long out_row(const PagedAttendArgs& a, const Sha
 // Outputs of tokens that see no slot: zeros and -infinity.
 __device__ __forceinline__ void write_empty(const PagedAttendArgs& a) {
   for (int s = blockIdx.x; s < a.n_seq; s += gridDim.x) {
-    const SeqWork w = seq_work(a, s, false);
+    const int2 n = seq_size(a, s, false);
+    const SeqWork w = seq_work(a, n.x, n.y);
     if (w.add == 0 || w.total > 0) continue;
     const long long row0 = (long long)s * a.B * a.heads * a.group;
     const long long rows = (long long)w.add * a.heads * a.group;
     const int chunks = a.d / 8;
-    for (long long i = threadIdx.x; i < rows * chunks; i += kThreads)
+    for (long long i = threadIdx.x; i < rows * chunks; i += blockDim.x)
       st16(a.out + row0 * a.d + i * 8, make_uint4(0, 0, 0, 0));
     if (a.lse)
-      for (long long i = threadIdx.x; i < rows; i += kThreads) a.lse[row0 + i] = -INFINITY;
+      for (long long i = threadIdx.x; i < rows; i += blockDim.x) a.lse[row0 + i] = -INFINITY;
   }
 }
 

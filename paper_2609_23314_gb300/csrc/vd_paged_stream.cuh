@@ -1,0 +1,490 @@
+// vd_paged_stream.cuh -- attention over one layer of a paged cache (vd_paged_attend in
+// include/vd.h): the streaming kernel, for few query rows per KV head.
+//
+//   s_ij = scale * q_i . k_j,  o_i = sum_j exp(s_ij - m_i) v_j / sum_j exp(s_ij - m_i)
+//
+// in one pass over the slots with a running maximum and sum.  A CTA takes its piece of the line
+// (vd_paged_attend.cuh); its warps take a share's stages of 16 slots in turn, each with its own
+// ring of asynchronous copies and its own running state, so that warps wait for nothing but their
+// copies, and meet at the end of the share.
+//
+// Per stage a warp computes  S^T = K Q^T  and  O^T += V^T P^T  with slots and head dims on the
+// 16-row side of m16n8k16, so that 8 query rows fill a tile.  bf16 pages are multiplied as
+// they are, weights in two bf16 parts (2^-16 of a weight); e4m3 ones go to fp16 (exact), Q too
+// with each row scaled by a power of two (QueryScale), weights are rounded to fp16.  Sums are
+// fp32.
+#pragma once
+
+#include <cstdint>
+#include <cuda_runtime.h>
+
+#include "vd_attend.cuh"
+#include "vd_device.cuh"
+#include "vd_paged.cuh"
+#include "vd_paged_attend.cuh"
+
+namespace vd {
+
+// 16 bytes to shared memory, or zeros.
+__device__ __forceinline__ void cp_async16_or_zero(uint32_t smem, const void* p, bool real) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(p),
+               "r"(real ? 16 : 0)
+               : "memory");
+}
+
+__device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+
+template <int M, int NT, bool E4M3>
+struct StreamShape {
+  static constexpr int kD = 32 * M;  // head_dim, rounded up
+  static constexpr int kRows = 8 * NT;
+  static constexpr int kRowBytes = kD * (E4M3 ? 1 : 2);
+  static constexpr int kChunks = kRowBytes / 16;
+  static constexpr int kTileBytes = kStageKeys * kRowBytes;  // of K or V
+  static constexpr int kStageBytes = 2 * kTileBytes;
+  static constexpr int kStreamWarps = M <= 4 ? 8 : 4;
+  static constexpr int kStreamThreads = 32 * kStreamWarps;
+  static constexpr int kStages = E4M3 ? (M == 2 ? 8 : M == 3 || M == 6 ? 6 : 5)
+                                      : (M == 2 ? 6 : M == 3 || M == 6 ? 4 : 3);
+  static constexpr int kRing = kStreamWarps * kStages * kStageBytes;
+  static constexpr int kPart = kD + 4;  // floats of a partial row
+  static constexpr int kParts = kRing;  // [warp][8 rows]
+  static constexpr int kStats = kParts + kStreamWarps * 8 * kPart * 4;  // [warp][8 rows] max, sum
+  static constexpr int kWalk = kStats + kStreamWarps * 8 * 8;
+  static constexpr int kTotal = kWalk + (int)sizeof(WalkMem);
+  static_assert(kTotal <= 232448, "shared memory");
+};
+
+// The chunk (16 bytes) of a row at which chunk c lies, so that the same chunk of 8 rows falls on
+// different banks.
+template <int kChunks>
+__device__ __forceinline__ int swizzle(int row, int c) {
+  if (kChunks % 8 == 0) return c ^ (row & 7);
+  if (kChunks % 4 == 0) return c ^ ((row >> 1) & 3);
+  return c ^ ((row >> 2) & 1);
+}
+
+// The running maximum less this is the point that weights are relative to: fp16 weights far
+// below the largest keep their bits, and the point moves only where the maximum rises by more.
+template <bool E4M3>
+constexpr float kPagedLift = E4M3 ? 15.f : 8.f;
+
+// Whether one of two values has an exponent of ones.
+template <bool E4M3>
+__device__ __forceinline__ bool odd_pair(uint32_t w) {
+  const uint32_t lo = E4M3 ? 0x7c00u : 0x7f80u, hi = lo << 16;
+  return (w & lo) == lo || (w & hi) == hi;
+}
+
+// Two weights in bf16, and in `low` what that leaves of them: together within 2^-16 of a weight.
+// Both parts of a weight above 0 are above 0, so that an infinite value stays one.
+__device__ __forceinline__ uint32_t split_weights(float x, float y, uint32_t& low) {
+  uint32_t high;
+  asm("cvt.rz.bf16x2.f32 %0, %1, %2;" : "=r"(high) : "f"(y), "f"(x));
+  low = pack_bf16(fmaxf(x - __uint_as_float(high << 16), x * 0x1p-30f),
+                  fmaxf(y - __uint_as_float(high & 0xffff0000u), y * 0x1p-30f));
+  return high;
+}
+
+template <int M, int NT, bool E4M3>
+__global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
+    paged_stream_kernel(PagedAttendArgs a) {
+  using Sh = StreamShape<M, NT, E4M3>;
+  constexpr int kW = Sh::kStreamWarps, kS = Sh::kStages;
+  extern __shared__ __align__(128) unsigned char smem[];
+  const uint32_t base = smem_addr(smem);
+  float* parts = reinterpret_cast<float*>(smem + Sh::kParts);
+  float2* stats = reinterpret_cast<float2*>(smem + Sh::kStats);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int r = lane >> 2, c = lane & 3;
+  const int chunks = a.d * (E4M3 ? 1 : 2) / 16;  // of a row in the pages
+  const uint32_t ring = base + warp * kS * Sh::kStageBytes;
+  // what copies do not write: the chunks behind head_dim
+  if (chunks < Sh::kChunks)
+    for (int i = lane; i < kS * 2 * kStageKeys * Sh::kChunks; i += 32)
+      st_shared16(ring + 16 * i, make_uint4(0, 0, 0, 0));
+  grid_dependency_wait();
+  grid_launch_dependents();
+  Walk walk(a, *reinterpret_cast<WalkMem*>(smem + Sh::kWalk), kW);
+  if (threadIdx.x == 0) a.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
+
+  // A stage's rows: lanes 0 .. 15 and 16 .. 31 look up its 16 slots
+  auto lookup = [&](const Share& s, int stage, int& slot) {
+    slot = stage * kStageKeys + (lane & 15);
+    if (stage >= s.s1 || slot >= s.w.total) return -1;
+    const int p = __ldcg(a.pages.table + (size_t)s.seq * a.pages.max_pages + a.pages.place_of(slot));
+    return p;
+  };
+  auto fetch = [&](const Share& s, int stage, int at, int page, int slot) {
+    if (stage >= s.s1) return;
+    const bool there = slot < s.w.total;
+    if (there && (unsigned)page >= (unsigned)a.pages.n_page)
+      record_status(a.pages.status, kStDevicePage);
+    const bool real = there && (unsigned)page < (unsigned)a.pages.n_page;
+    const long long row = real ? a.pages.row(page, slot) + s.head * a.pages.head_stride : -1;
+    const uint32_t dst = ring + at * Sh::kStageBytes;
+    int t = lane / chunks, ch = lane - t * chunks;
+    const int dt = 32 / chunks, dch = 32 - dt * chunks;
+    for (int i = 0; i < kStageKeys * chunks; i += 32) {
+      const long long from = __shfl_sync(kFull, row, t & 15);
+      if (t < kStageKeys) {
+        const long long in = from < 0 ? 0 : from + ch * 16;
+        const uint32_t to = dst + t * Sh::kRowBytes + (swizzle<Sh::kChunks>(t, ch) << 4);
+        cp_async16_or_zero(to, a.pages.k + in, from >= 0);
+        cp_async16_or_zero(to + Sh::kTileBytes, a.pages.v + in, from >= 0);
+      }
+      t += dt;
+      ch += dch;
+      if (ch >= chunks) {
+        ch -= chunks;
+        ++t;
+      }
+    }
+  };
+  // The first stages of a share; the page and slot of the next one to fetch
+  int next_page, next_slot;
+  auto begin = [&](const Share& s) {
+    int page[kS - 1], slot[kS - 1];
+#pragma unroll
+    for (int i = 0; i < kS - 1; ++i) page[i] = lookup(s, s.s0 + warp + i * kW, slot[i]);
+    next_page = lookup(s, s.s0 + warp + (kS - 1) * kW, next_slot);
+#pragma unroll
+    for (int i = 0; i < kS - 1; ++i) {
+      fetch(s, s.s0 + warp + i * kW, i, page[i], slot[i]);
+      cp_async_commit();
+    }
+  };
+
+  Share s;
+  bool more = walk.next(s);
+  if (more) begin(s);
+  while (more) {
+    // Q: lane (r, c) holds row r of each n-tile
+    uint32_t qf[NT][2 * M][2];
+    int sees[NT][2];  // slots that columns 2 c and 2 c + 1 see
+    float qs[NT][2];  // what their scores are multiplied by for log2 units
+    int all_see = a.causal ? s.w.len + (s.tile * Sh::kRows) / a.group + 1 : s.w.len;
+    const float ks = E4M3 && a.pages.k_scale ? __ldg(a.pages.k_scale + s.head) : 1.f;
+    const float vs = E4M3 && a.pages.v_scale ? __ldg(a.pages.v_scale + s.head) : 1.f;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const long long row = out_row(a, s, 8 * t + r);
+#pragma unroll
+      for (int j = 0; j < 2 * M; ++j) {
+        // e4m3: chunk j's dims 4 c .. 4 c + 3; bf16: chunks 2 j and 2 j + 1, dims 2 c, 2 c + 1
+        const int d0 = 16 * j + (E4M3 ? 4 : 2) * c, d1 = E4M3 ? d0 + 2 : d0 + 8;
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(a.q + (row < 0 ? 0 : row) * a.d);
+        qf[t][j][0] = row >= 0 && d0 < a.d ? __ldcg(src + d0 / 2) : 0u;
+        qf[t][j][1] = row >= 0 && d1 < a.d ? __ldcg(src + d1 / 2) : 0u;
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        sees[t][e] = a.causal
+                         ? s.w.len + (s.tile * Sh::kRows + 8 * t + 2 * c + e) / a.group + 1
+                         : s.w.len;
+      if (!E4M3) {
+        qs[t][0] = qs[t][1] = a.scale * kLog2e;
+      } else {
+        uint32_t top = 0;  // largest magnitude of the row, as bits
+#pragma unroll
+        for (int j = 0; j < 2 * M; ++j)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t x = qf[t][j][e];
+            top = max(top, max(x & 0x7fffu, (x >> 16) & 0x7fffu));
+          }
+        top = max(top, __shfl_xor_sync(kFull, top, 1));
+        top = max(top, __shfl_xor_sync(kFull, top, 2));
+        const QueryScale f = scale_of(top);
+#pragma unroll
+        for (int j = 0; j < 2 * M; ++j)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            uint32_t x = qf[t][j][e];
+            asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(x) : "r"(f.up));
+            qf[t][j][e] = pack_f16(__uint_as_float(x << 16) * kTo16,
+                                   __uint_as_float(x & 0xffff0000u) * kTo16);
+          }
+        const float factor = score_factor(f.down, a.scale * ks) * kFrom16;
+        qs[t][0] = __shfl_sync(kFull, factor, 8 * c);
+        qs[t][1] = __shfl_sync(kFull, factor, 8 * c + 4);
+      }
+    }
+    float o[NT][2 * M][4];
+    float mx[NT][2], sum[NT][2];  // references and sums of columns 2 c and 2 c + 1
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      mx[t][0] = mx[t][1] = -INFINITY;
+      sum[t][0] = sum[t][1] = 0.f;
+#pragma unroll
+      for (int i = 0; i < 2 * M; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[t][i][e] = 0.f;
+    }
+
+    int at = 0;  // the ring's place of the stage
+    for (int stage = s.s0 + warp; stage < s.s1; stage += kW) {
+      cp_async_wait<kS - 2>();
+      __syncwarp();
+      {
+        const int ahead = stage + (kS - 1) * kW, page = next_page, slot = next_slot;
+        next_page = lookup(s, ahead + kW, next_slot);
+        fetch(s, ahead, at == 0 ? kS - 1 : at - 1, page, slot);
+        cp_async_commit();
+      }
+      const uint32_t tile_k = ring + at * Sh::kStageBytes, tile_v = tile_k + Sh::kTileBytes;
+      at = at + 1 == kS ? 0 : at + 1;
+      const int key0 = stage * kStageKeys;
+      float x[NT][4];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[t][e] = 0.f;
+      const int kt = (lane & 7) + 8 * ((lane >> 3) & 1), kc = lane >> 4;
+      if (E4M3) {
+#pragma unroll
+        for (int j = 0; j < M; ++j) {  // two chunks of 16 dims
+          uint32_t w[4];
+          ldmatrix4(tile_k + kt * Sh::kRowBytes + (swizzle<Sh::kChunks>(kt, 2 * j + kc) << 4), w);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t f[4] = {e4m3_to_h2(w[2 * h], false), e4m3_to_h2(w[2 * h + 1], false),
+                                   e4m3_to_h2(w[2 * h], true), e4m3_to_h2(w[2 * h + 1], true)};
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+              mma_16816<false>(x[t], f, qf[t][2 * j + h][0], qf[t][2 * j + h][1]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 2 * M; ++j) {
+          uint32_t f[4];
+          ldmatrix4(tile_k + kt * Sh::kRowBytes + (swizzle<Sh::kChunks>(kt, 2 * j + kc) << 4), f);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) mma_16816<true>(x[t], f, qf[t][j][0], qf[t][j][1]);
+        }
+      }
+      // Scores, rounded before the maximum is taken off them (a difference of the unrounded
+      // product would be off by half a unit of the maximum), into the running state
+      const bool hides = key0 + kStageKeys > all_see;
+      bool above = false;
+      float top[NT][2];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          x[t][e] = __fmul_rn(x[t][e], qs[t][e]);
+          x[t][e + 2] = __fmul_rn(x[t][e + 2], qs[t][e]);
+          if (hides) {
+            if (key0 + r >= sees[t][e]) x[t][e] = -INFINITY;
+            if (key0 + r + 8 >= sees[t][e]) x[t][e + 2] = -INFINITY;
+          }
+          top[t][e] = __fadd_ru(fmaxf(x[t][e], x[t][e + 2]), -kPagedLift<E4M3>);
+          above |= top[t][e] > mx[t][e];
+        }
+      if (__any_sync(kFull, above)) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float m = fmaxf(mx[t][e], top[t][e]);
+#pragma unroll
+            for (int off = 4; off < 32; off <<= 1) m = fmaxf(m, __shfl_xor_sync(kFull, m, off));
+            const float f = m == -INFINITY ? 1.f : exp2_approx(mx[t][e] - m);
+            mx[t][e] = m;
+            sum[t][e] *= f;
+#pragma unroll
+            for (int i = 0; i < 2 * M; ++i) {
+              o[t][i][e] *= f;
+              o[t][i][e + 2] *= f;
+            }
+          }
+      }
+      uint32_t ph[NT][2], pl[NT][2];  // weights of slots 2 c, 2 c + 1 (and + 8) for row r
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float m = mx[t][e] == -INFINITY ? 0.f : mx[t][e];
+          x[t][e] = exp2_approx(__fadd_rn(x[t][e], -m));
+          x[t][e + 2] = exp2_approx(__fadd_rn(x[t][e + 2], -m));
+          sum[t][e] += x[t][e] + x[t][e + 2];
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (E4M3) {
+            ph[t][h] = transpose_8x8(pack_f16(x[t][2 * h], x[t][2 * h + 1]));
+          } else {
+            uint32_t low;
+            ph[t][h] = transpose_8x8(split_weights(x[t][2 * h], x[t][2 * h + 1], low));
+            pl[t][h] = transpose_8x8(low);
+          }
+        }
+      }
+      auto product = [&](float (&y)[4], const uint32_t (&f)[4], int t) {
+        mma_16816<!E4M3>(y, f, ph[t][0], ph[t][1]);
+        if (!E4M3) mma_16816<true>(y, f, pl[t][0], pl[t][1]);
+      };
+      // V's dims 16 i .. 16 i + 15.  A value that is not finite must not reach the tokens that do
+      // not see its slot, whose weight for it is 0: then the slots go one by one, to those
+      // that do.
+      auto take = [&](int i, const uint32_t (&f)[4]) {
+        if (hides && __any_sync(kFull, odd_pair<E4M3>(f[0]) || odd_pair<E4M3>(f[1]) ||
+                                           odd_pair<E4M3>(f[2]) || odd_pair<E4M3>(f[3]))) {
+#pragma unroll 1
+          for (int slot = 0; slot < kStageKeys; ++slot) {
+            const uint32_t keep = (slot & 7) >> 1 != c ? 0u : slot & 1 ? 0xffff0000u : 0xffffu;
+            const uint32_t g[4] = {slot < 8 ? f[0] & keep : 0u, slot < 8 ? f[1] & keep : 0u,
+                                   slot < 8 ? 0u : f[2] & keep, slot < 8 ? 0u : f[3] & keep};
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+              float y[4] = {0.f, 0.f, 0.f, 0.f};
+              product(y, g, t);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (key0 + slot < sees[t][e & 1]) o[t][i][e] += y[e];
+            }
+          }
+        } else {
+#pragma unroll
+          for (int t = 0; t < NT; ++t) product(o[t][i], f, t);
+        }
+      };
+      if (E4M3) {
+        const int vt = (lane & 7) + 8 * ((lane >> 3) & 1), vc = lane >> 4;
+#pragma unroll
+        for (int j = 0; j < M; ++j) {
+          uint32_t w[4];
+          ldmatrix4_trans(tile_v + vt * Sh::kRowBytes + (swizzle<Sh::kChunks>(vt, 2 * j + vc) << 4),
+                          w);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            // a word: dims 2 r, 2 r + 1 of slot 2 c, then of 2 c + 1; rows r and r + 8 of the
+            // product are dims 2 r and 2 r + 1
+            const uint32_t lo = __byte_perm(w[2 * h], 0, 0x3120),
+                           hi = __byte_perm(w[2 * h + 1], 0, 0x3120);
+            const uint32_t f[4] = {e4m3_to_h2(lo, false), e4m3_to_h2(lo, true),
+                                   e4m3_to_h2(hi, false), e4m3_to_h2(hi, true)};
+            take(2 * j + h, f);
+          }
+        }
+      } else {
+        const int vt = (lane & 7) + 8 * (lane >> 4), vc = (lane >> 3) & 1;
+#pragma unroll
+        for (int j = 0; j < 2 * M; ++j) {
+          uint32_t f[4];
+          ldmatrix4_trans(tile_v + vt * Sh::kRowBytes + (swizzle<Sh::kChunks>(vt, 2 * j + vc) << 4),
+                          f);
+          take(j, f);
+        }
+      }
+      __syncwarp();
+    }
+
+    // the next share's first stages come while this one's warps meet
+    cp_async_wait<0>();
+    __syncwarp();
+    Share next;
+    more = walk.next(next);
+    if (more) begin(next);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) sum[t][e] += __shfl_xor_sync(kFull, sum[t][e], off);
+        // all scores NaN: so is the result
+        if (sum[t][e] != sum[t][e] && mx[t][e] == -INFINITY) mx[t][e] = 0.f;
+      }
+      float* mine = parts + warp * 8 * Sh::kPart;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float* row = mine + (2 * c + e) * Sh::kPart;
+#pragma unroll
+        for (int i = 0; i < 2 * M; ++i) {
+          if (E4M3) {
+            *reinterpret_cast<float2*>(row + 16 * i + 2 * r) = make_float2(o[t][i][e], o[t][i][e + 2]);
+          } else {
+            row[16 * i + r] = o[t][i][e];
+            row[16 * i + 8 + r] = o[t][i][e + 2];
+          }
+        }
+        if (r == 0) stats[warp * 8 + 2 * c + e] = make_float2(mx[t][e], sum[t][e]);
+      }
+      __syncthreads();
+#pragma unroll 1
+      for (int q = warp; q < 8; q += kW) {
+        const long long row = out_row(a, s, 8 * t + q);
+        if (row < 0) continue;
+        float top = -INFINITY, total = 0.f, f[kW];
+#pragma unroll
+        for (int w = 0; w < kW; ++w) top = fmaxf(top, stats[w * 8 + q].x);
+#pragma unroll
+        for (int w = 0; w < kW; ++w) {
+          const float2 st = stats[w * 8 + q];
+          f[w] = st.x == -INFINITY ? 0.f : exp2_approx(st.x - top);
+          total += st.x == -INFINITY ? 0.f : f[w] * st.y;
+        }
+        const float scale = s.whole ? (top == -INFINITY ? 0.f : vs / total) : vs;
+        const size_t part = (size_t)s.slot * Sh::kRows + 8 * t + q;
+        for (int d = 4 * lane; d < a.d; d += 128) {
+          float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int w = 0; w < kW; ++w) {
+            const float4 z = *reinterpret_cast<const float4*>(parts + (w * 8 + q) * Sh::kPart + d);
+            if (stats[w * 8 + q].x == -INFINITY) continue;
+            y.x += f[w] * z.x;
+            y.y += f[w] * z.y;
+            y.z += f[w] * z.z;
+            y.w += f[w] * z.w;
+          }
+          y = make_float4(y.x * scale, y.y * scale, y.z * scale, y.w * scale);
+          if (s.whole)
+            *reinterpret_cast<uint2*>(a.out + row * a.d + d) =
+                make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
+          else
+            *reinterpret_cast<float4*>(a.parts + part * a.d + d) = y;
+        }
+        if (lane == 0) {
+          if (!s.whole)
+            a.stats[part] = make_float2(top, total);
+          else if (a.lse)
+            a.lse[row] = (top + log2f(total)) * kLn2;
+        }
+      }
+      __syncthreads();
+    }
+    if (threadIdx.x == 0 && !s.whole && s.s0 == 0)
+      a.split[blockIdx.x] = make_int4(s.seq, s.head, s.tile, s.last);
+    s = next;
+  }
+  write_empty(a);
+}
+
+struct PagedKernel {
+  void (*kern)(PagedAttendArgs);
+  int smem, rows, threads;
+};
+
+template <int M, int NT, bool E4M3>
+constexpr PagedKernel paged_stream() {
+  using Sh = StreamShape<M, NT, E4M3>;
+  return {paged_stream_kernel<M, NT, E4M3>, Sh::kTotal, Sh::kRows, Sh::kStreamThreads};
+}
+
+// [(head_dim + 31) / 32 - 1][tiles of 8 or 16 rows]
+extern const PagedKernel kPagedBf16[8][2], kPagedE4m3[8][2];
+
+}  // namespace vd
