@@ -21,58 +21,69 @@ namespace {
 constexpr int kMaxDim = 256;
 
 // A CTA puts together one row of the unit that CTA `first` of the kernel before begins and
-// does not end.
+// does not end: its warps take parts in turn, a lane 4 values, or 8.
 __global__ void __launch_bounds__(kThreads) paged_join_kernel(PagedAttendArgs a) {
-  __shared__ float part[kWarps][kMaxDim];
-  __shared__ float stat[kWarps][2];
+  __shared__ float4 part[kWarps][kMaxDim / 4];
+  __shared__ float2 stat[kWarps];
   grid_dependency_wait();
   grid_launch_dependents();
   const int first = blockIdx.x / a.rows, i = blockIdx.x % a.rows;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int4 unit = __ldcg(a.split + first);
-  if (unit.x < 0) return;
-  Share s;
-  s.seq = unit.x;
-  s.head = unit.y;
-  s.tile = unit.z;
-  const int2 size = seq_size(a, s.seq, false);
-  s.w = seq_work(a, size.x, size.y);
-  const long long row = out_row(a, s, i);
-  if (row < 0) return;
+  if (unit.x < 0 || i >= unit.z) return;
+  const int tok = (unit.y + i) / a.group, g = unit.y + i - tok * a.group;
+  const long long row = unit.x + (long long)tok * a.heads * a.group + g;
   const int n = unit.w - first + 1;
-  auto at = [&](int p) { return (size_t)(2 * (first + p) + (p == 0 ? 1 : 0)) * a.rows + i; };
-  float top = -INFINITY, sum = 0.f, y[kMaxDim / 32];
+  float2 total = make_float2(-INFINITY, 0.f);
+  float y[8];
 #pragma unroll
-  for (int e = 0; e < kMaxDim / 32; ++e) y[e] = 0.f;
-  for (int p = warp; p < n; p += kWarps) {
-    const float2 st = __ldcg(a.stats + at(p));
-    const float m = fmaxf(top, st.x);
-    const float f = top == -INFINITY ? 0.f : exp2f(top - m), g = st.x == -INFINITY ? 0.f : exp2f(st.x - m);
-    top = m;
-    sum = sum * f + (g == 0.f ? 0.f : g * st.y);
+  for (int e = 0; e < 8; ++e) y[e] = 0.f;
+  for (int p0 = warp; p0 < n; p0 += 2 * kWarps) {
+    float2 st[2];
+    float4 v[2][2];
 #pragma unroll
-    for (int e = 0; e < kMaxDim / 32; ++e)
-      if (e * 32 + lane < a.d) {
-        const float v = __ldcg(a.parts + at(p) * a.d + e * 32 + lane);
-        y[e] = y[e] * f + (g == 0.f ? 0.f : g * v);
+    for (int j = 0; j < 2; ++j) {  // loads of two parts together
+      const int p = p0 + j * kWarps;
+      const size_t at = (size_t)(2 * (first + p) + (p == 0 ? 1 : 0)) * a.rows + i;
+      st[j] = make_float2(-INFINITY, 0.f);
+      if (p < n) {
+        st[j] = __ldcg(a.stats + at);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          if (128 * h + 4 * lane < a.d)
+            v[j][h] = __ldcg(reinterpret_cast<const float4*>(a.parts + at * a.d + 128 * h + 4 * lane));
       }
-  }
+    }
 #pragma unroll
-  for (int e = 0; e < kMaxDim / 32; ++e) part[warp][e * 32 + lane] = y[e];
-  if (lane == 0) {
-    stat[warp][0] = top;
-    stat[warp][1] = sum;
+    for (int j = 0; j < 2; ++j) {
+      if (st[j].x == -INFINITY) continue;  // nothing seen
+      const float m = fmaxf(total.x, st[j].x);
+      const float f = total.x == -INFINITY ? 0.f : exp2_approx(total.x - m);
+      const float w = exp2_approx(st[j].x - m);
+      total = make_float2(m, total.y * f + w * st[j].y);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (128 * h + 4 * lane < a.d) {
+          y[4 * h] = y[4 * h] * f + w * v[j][h].x;
+          y[4 * h + 1] = y[4 * h + 1] * f + w * v[j][h].y;
+          y[4 * h + 2] = y[4 * h + 2] * f + w * v[j][h].z;
+          y[4 * h + 3] = y[4 * h + 3] * f + w * v[j][h].w;
+        }
+    }
   }
+  part[warp][lane] = make_float4(y[0], y[1], y[2], y[3]);
+  part[warp][32 + lane] = make_float4(y[4], y[5], y[6], y[7]);
+  if (lane == 0) stat[warp] = total;
   __syncthreads();
-  top = -INFINITY;
-  sum = 0.f;
-  for (int w = 0; w < kWarps; ++w) top = fmaxf(top, stat[w][0]);
-  float z = 0.f;
+  float top = -INFINITY, sum = 0.f, z = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) top = fmaxf(top, stat[w].x);
+#pragma unroll
   for (int w = 0; w < kWarps; ++w) {
-    const float f = stat[w][0] == -INFINITY ? 0.f : exp2f(stat[w][0] - top);
-    if (f == 0.f) continue;
-    sum += f * stat[w][1];
-    z += f * part[w][threadIdx.x];
+    const float f = stat[w].x == -INFINITY ? 0.f : exp2_approx(stat[w].x - top);
+    if (stat[w].x == -INFINITY) continue;
+    sum += f * stat[w].y;
+    z += f * reinterpret_cast<const float*>(part[w])[threadIdx.x];
   }
   if (threadIdx.x < a.d) {
     z = top == -INFINITY ? 0.f : z / sum;
@@ -156,6 +167,7 @@ vd_status vd_paged_attend(const vd_paged_cache* c, int32_t layer, const void* q,
   a.B = B;
   a.d = c->head_dim;
   a.rows = p.rows;
+  a.stage_keys = p.kernel->stage_keys;
   a.causal = causal != 0;
   a.scale = scale;
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);

@@ -2,7 +2,7 @@
 // include/vd.h): how the work is divided and its parts are joined.
 //
 // A unit is a sequence's KV head and a tile of `rows` query rows; it takes ceil(slots /
-// kStageKeys) stages.  The units' stages, sequence after sequence, make one line that is cut
+// stage_keys) stages.  The units' stages, sequence after sequence, make one line that is cut
 // into equal pieces, one for each CTA, whatever the lengths are: the lengths are on the device,
 // and a cut by them needs no plan on the host and leaves no CTA idle beside a long sequence.
 // A CTA that holds all stages of a unit writes its output.  Of the others it writes a part (sums
@@ -19,19 +19,20 @@
 
 namespace vd {
 
-constexpr int kStageKeys = 16;
-
 struct PagedAttendArgs {
   Pages pages;
   const uint16_t* q;
   uint16_t* out;
   float* lse;            // nullable
   const int32_t* n_new;  // nullable
-  int4* split;           // workspace: of each CTA (see split_of), ...
+  int4* split;           // workspace: of each CTA the unit that it begins and does not end: the row
+                         // of out of its KV head's first one, the tile's first row and the
+                         // number of its rows, the last CTA with a part; or -1
   float2* stats;         // ... [2 CTAs][rows] references and sums of weights,
   float* parts;          // ... [2 CTAs][rows][d] sums
   int n_seq, heads, group, B, d;
   int rows;              // of a tile
+  int stage_keys;        // slots of a stage
   int causal;
   float scale;
 };
@@ -49,7 +50,7 @@ __device__ __forceinline__ SeqWork seq_work(const PagedAttendArgs& a, int len, i
   SeqWork w = {len, add, 0, 0, 0, 0};
   w.total = add == 0 ? 0 : len + (a.causal ? add : 0);
   w.tiles = (add * a.group + a.rows - 1) / a.rows;
-  w.stages = (w.total + kStageKeys - 1) / kStageKeys;
+  w.stages = (w.total + a.stage_keys - 1) / a.stage_keys;
   w.work = (long long)w.stages * w.tiles * a.heads;
   return w;
 }
@@ -64,6 +65,11 @@ __device__ __forceinline__ int2 seq_size(const PagedAttendArgs& a, int seq, bool
   return make_int2(len, add);
 }
 
+// Quotients, of which most fit 32 bits.
+__device__ __forceinline__ long long divide(long long n, long long d) {
+  return (unsigned long long)(n | d) >> 32 ? n / d : (long long)((uint32_t)n / (uint32_t)d);
+}
+
 // The line cut into `ctas` pieces: the first `more` have one stage more.
 struct Cut {
   long long per;
@@ -73,20 +79,19 @@ struct Cut {
   }
   __device__ __forceinline__ int holder(long long at) const {
     const long long head = (per + 1) * more;
-    return at < head ? (int)(at / (per + 1)) : more + (int)((at - head) / per);
+    return at < head ? (int)divide(at, per + 1) : more + (int)divide(at - head, per);
   }
 };
 
-// A CTA's share of a unit: stages [s0, s1) of `stages`.
+// A CTA's share of a unit: stages [s0, s1).
 struct Share {
   int seq, head, tile, s0, s1;
-  SeqWork w;
-  bool whole;
-  int slot;  // of the part
+  int len, add, total;  // of the sequence, as in SeqWork
+  int slot;  // of the part; -1: the whole unit
   int last;  // the last CTA that has a part of the unit, where this share begins it
 };
 
-constexpr int kChunk = 64;  // sequences that a walk looks at together
+constexpr int kChunk = 64;  // sequences that are looked at together
 
 struct WalkMem {
   long long end[kChunk];  // where each ends on the line
@@ -94,18 +99,18 @@ struct WalkMem {
   long long sum[32];
 };
 
-// Walks over a CTA's piece of the line.  All threads of the CTA make the same calls.
+// Walks over a CTA's piece of the line.  All threads of the CTA construct it together; then each
+// warp may go its own way.
 struct Walk {
-  const PagedAttendArgs& a;
-  WalkMem& m;
   Cut cut;
-  long long at, end, seq_begin;  // line positions: the next stage, the piece's end, seq's first
-  int seq, chunk;                // chunk: the first of the sequences in m
+  long long at, end;  // line positions: the next stage, the piece's end
+  int chunk, seq, head, tile, stage;
+  SeqWork w;          // of seq
 
   // Pieces of `least` stages at least.
-  __device__ Walk(const PagedAttendArgs& args, WalkMem& mem, int least)
-      : a(args), m(mem), at(0), end(0), seq_begin(0), seq(0), chunk(0) {
-    load(0, blockIdx.x == 0);
+  __device__ Walk(const PagedAttendArgs& a, WalkMem& m, int least)
+      : at(0), end(0), chunk(0), seq(0), head(0), tile(0), stage(0), w() {
+    load(a, m, 0, blockIdx.x == 0);
     long long all = m.end[kChunk - 1];
     if (a.n_seq > kChunk) {
       long long mine = 0;
@@ -117,18 +122,38 @@ struct Walk {
       for (int off = 16; off > 0; off >>= 1) mine += __shfl_xor_sync(kFull, mine, off);
       if ((threadIdx.x & 31) == 0) m.sum[threadIdx.x >> 5] = mine;
       __syncthreads();
-      for (int w = 0; w < (int)blockDim.x / 32; ++w) all += m.sum[w];
+      for (int i = 0; i < (int)blockDim.x / 32; ++i) all += m.sum[i];
     }
-    const long long most = all / least;
+    const long long most = divide(all, least);
     cut.ctas = most >= (long long)gridDim.x ? (int)gridDim.x : most > 1 ? (int)most : 1;
-    cut.per = all / cut.ctas;
+    cut.per = divide(all, cut.ctas);
     cut.more = (int)(all - cut.per * cut.ctas);
     if ((int)blockIdx.x >= cut.ctas) return;
     at = cut.begin(blockIdx.x);
     end = cut.begin(blockIdx.x + 1);
+    if (at >= end) return;
+    // the first sequence and the place in it
+    long long begin = 0, stop;
+    while ((stop = m.end[kChunk - 1]) <= at) {
+      begin = stop;
+      chunk += kChunk;
+      load(a, m, stop, false);
+    }
+    const int lane = threadIdx.x & 31;
+    int done = 0;
+#pragma unroll
+    for (int i = 0; i < kChunk; i += 32)
+      done += __popc(__ballot_sync(kFull, m.end[i + lane] <= at));
+    if (done > 0) begin = m.end[done - 1];
+    seq = chunk + done;
+    w = seq_work(a, m.size[done].x, m.size[done].y);
+    const int unit = (int)divide(at - begin, w.stages);
+    stage = (int)(at - begin - (long long)unit * w.stages);
+    head = unit / w.tiles;
+    tile = unit - head * w.tiles;
   }
   // The ends of the chunk's sequences, the first of which begins at `begin`; by the first warp.
-  __device__ void load(long long begin, bool report) {
+  __device__ void load(const PagedAttendArgs& a, WalkMem& m, long long begin, bool report) {
     __syncthreads();  // the last chunk's readers
     if (threadIdx.x < 32) {
       const int lane = threadIdx.x;
@@ -150,39 +175,50 @@ struct Walk {
     __syncthreads();
   }
   // The next share, if there is one.
-  __device__ bool next(Share& s) {
+  __device__ bool next(const PagedAttendArgs& a, const WalkMem& m, Share& s) {
     if (at >= end) return false;
-    long long stop;
-    while ((stop = m.end[seq - chunk]) <= at) {  // a sequence that is done, or empty
-      seq_begin = stop;
-      ++seq;
-      if (seq == chunk + kChunk) {
-        chunk = seq;
-        load(stop, false);
+    s.seq = seq;
+    s.head = head;
+    s.tile = tile;
+    s.len = w.len;
+    s.add = w.add;
+    s.total = w.total;
+    const int n = end - at < w.stages - stage ? (int)(end - at) : w.stages - stage;
+    s.s0 = stage;
+    s.s1 = stage += n;
+    at += n;
+    // a CTA's first share may begin inside a unit, its last one may end there
+    s.slot = n == w.stages ? -1 : 2 * (int)blockIdx.x + (s.s0 == 0 ? 1 : 0);
+    s.last = s.slot < 0 || s.s0 > 0 ? 0 : cut.holder(at + (w.stages - stage) - 1);
+    if (stage == w.stages) {
+      stage = 0;
+      if (++tile == w.tiles) {
+        tile = 0;
+        if (++head == a.heads) {
+          head = 0;
+          if (at < end) do {
+              ++seq;
+              const int2 n = seq - chunk < kChunk ? m.size[seq - chunk] : seq_size(a, seq, false);
+              w = seq_work(a, n.x, n.y);
+            } while (w.work == 0);
+        }
       }
     }
-    s.seq = seq;
-    s.w = seq_work(a, m.size[seq - chunk].x, m.size[seq - chunk].y);
-    const long long in = at - seq_begin;
-    const int unit = (int)(in / s.w.stages);
-    s.s0 = (int)(in - (long long)unit * s.w.stages);
-    s.head = unit / s.w.tiles;
-    s.tile = unit - s.head * s.w.tiles;
-    const long long left = end - at;
-    s.s1 = s.w.stages - s.s0 <= left ? s.w.stages : s.s0 + (int)left;
-    s.whole = s.s0 == 0 && s.s1 == s.w.stages;
-    // a CTA's first share may begin inside a unit, its last one may end there
-    s.slot = 2 * blockIdx.x + (s.s0 == 0 ? 1 : 0);
-    at += s.s1 - s.s0;
-    s.last = s.whole || s.s0 > 0 ? 0 : cut.holder(at + (s.w.stages - s.s1) - 1);
     return true;
   }
 };
 
+// What the join has to know of such a unit.
+__device__ __forceinline__ int4 split_of(const PagedAttendArgs& a, const Share& s) {
+  const int row0 = s.tile * a.rows;
+  return make_int4((s.seq * a.B * a.heads + s.head) * a.group, row0,
+                   min(a.rows, s.add * a.group - row0), s.last);
+}
+
 // Where a tile's row lies: out and q at row * d, lse at row.  -1: no such row.
 __device__ __forceinline__ long long out_row(const PagedAttendArgs& a, const Share& s, int row) {
   const int at = s.tile * a.rows + row, tok = at / a.group;
-  if (tok >= s.w.add) return -1;
+  if (tok >= s.add) return -1;
   return (((long long)s.seq * a.B + tok) * a.heads + s.head) * a.group + (at - tok * a.group);
 }
 

@@ -4,11 +4,11 @@
 //   s_ij = scale * q_i . k_j,  o_i = sum_j exp(s_ij - m_i) v_j / sum_j exp(s_ij - m_i)
 //
 // in one pass over the slots with a running maximum and sum.  A CTA takes its piece of the line
-// (vd_paged_attend.cuh); its warps take a share's stages of 16 slots in turn, each with its own
+// (vd_paged_attend.cuh); its warps take a share's stages in turn, each with its own
 // ring of asynchronous copies and its own running state, so that warps wait for nothing but their
-// copies, and meet at the end of the share.
+// copies, and meet at the end of the share.  The copies run ahead into the next shares.
 //
-// Per stage a warp computes  S^T = K Q^T  and  O^T += V^T P^T  with slots and head dims on the
+// Per 16 slots a warp computes  S^T = K Q^T  and  O^T += V^T P^T  with slots and head dims on the
 // 16-row side of m16n8k16, so that 8 query rows fill a tile.  bf16 pages are multiplied as
 // they are, weights in two bf16 parts (2^-16 of a weight); e4m3 ones go to fp16 (exact), Q too
 // with each row scaled by a power of two (QueryScale), weights are rounded to fp16.  Sums are
@@ -24,6 +24,14 @@
 #include "vd_paged_attend.cuh"
 
 namespace vd {
+
+// Where the CTA's warps are: they take a share together, while each one's copies run ahead.
+struct StreamMem {
+  WalkMem walk;
+  Walk at;
+  Share share[2];
+  int more[2];
+};
 
 // 16 bytes to shared memory, or zeros.
 __device__ __forceinline__ void cp_async16_or_zero(uint32_t smem, const void* p, bool real) {
@@ -52,18 +60,20 @@ struct StreamShape {
   static constexpr int kRows = 8 * NT;
   static constexpr int kRowBytes = kD * (E4M3 ? 1 : 2);
   static constexpr int kChunks = kRowBytes / 16;
-  static constexpr int kTileBytes = kStageKeys * kRowBytes;  // of K or V
+  static constexpr int kGroups = (E4M3 && M <= 4) || M <= 2 ? 2 : 1;  // of 16 slots, in a stage
+  static constexpr int kKeys = 16 * kGroups;
+  static constexpr int kTileBytes = kKeys * kRowBytes;  // of K or V
   static constexpr int kStageBytes = 2 * kTileBytes;
   static constexpr int kStreamWarps = M <= 4 ? 8 : 4;
   static constexpr int kStreamThreads = 32 * kStreamWarps;
-  static constexpr int kStages = E4M3 ? (M == 2 ? 8 : M == 3 || M == 6 ? 6 : 5)
-                                      : (M == 2 ? 6 : M == 3 || M == 6 ? 4 : 3);
+  static constexpr int kStages =
+      E4M3 ? (M == 2 || M == 8 ? 5 : M == 3 ? 4 : M == 4 ? 3 : 6) : (M == 3 || M == 6 ? 4 : 3);
   static constexpr int kRing = kStreamWarps * kStages * kStageBytes;
   static constexpr int kPart = kD + 4;  // floats of a partial row
   static constexpr int kParts = kRing;  // [warp][8 rows]
   static constexpr int kStats = kParts + kStreamWarps * 8 * kPart * 4;  // [warp][8 rows] max, sum
-  static constexpr int kWalk = kStats + kStreamWarps * 8 * 8;
-  static constexpr int kTotal = kWalk + (int)sizeof(WalkMem);
+  static constexpr int kMem = kStats + kStreamWarps * 8 * 8;
+  static constexpr int kTotal = kMem + (int)sizeof(StreamMem);
   static_assert(kTotal <= 232448, "shared memory");
 };
 
@@ -81,11 +91,11 @@ __device__ __forceinline__ int swizzle(int row, int c) {
 template <bool E4M3>
 constexpr float kPagedLift = E4M3 ? 15.f : 8.f;
 
-// Whether one of two values has an exponent of ones.
+// Whether one of a word's values is not finite.
 template <bool E4M3>
-__device__ __forceinline__ bool odd_pair(uint32_t w) {
-  const uint32_t lo = E4M3 ? 0x7c00u : 0x7f80u, hi = lo << 16;
-  return (w & lo) == lo || (w & hi) == hi;
+__device__ __forceinline__ bool not_finite(uint32_t w) {
+  if (E4M3) return __vcmpeq4(w & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0;
+  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
 }
 
 // Two weights in bf16, and in `low` what that leaves of them: together within 2^-16 of a weight.
@@ -102,7 +112,7 @@ template <int M, int NT, bool E4M3>
 __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
     paged_stream_kernel(PagedAttendArgs a) {
   using Sh = StreamShape<M, NT, E4M3>;
-  constexpr int kW = Sh::kStreamWarps, kS = Sh::kStages;
+  constexpr int kW = Sh::kStreamWarps, kS = Sh::kStages, kG = Sh::kGroups;
   extern __shared__ __align__(128) unsigned char smem[];
   const uint32_t base = smem_addr(smem);
   float* parts = reinterpret_cast<float*>(smem + Sh::kParts);
@@ -113,69 +123,108 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
   const uint32_t ring = base + warp * kS * Sh::kStageBytes;
   // what copies do not write: the chunks behind head_dim
   if (chunks < Sh::kChunks)
-    for (int i = lane; i < kS * 2 * kStageKeys * Sh::kChunks; i += 32)
+    for (int i = lane; i < kS * Sh::kStageBytes / 16; i += 32)
       st_shared16(ring + 16 * i, make_uint4(0, 0, 0, 0));
   grid_dependency_wait();
   grid_launch_dependents();
-  Walk walk(a, *reinterpret_cast<WalkMem*>(smem + Sh::kWalk), kW);
-  if (threadIdx.x == 0) a.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
+  StreamMem& mem = *reinterpret_cast<StreamMem*>(smem + Sh::kMem);
+  Walk ahead(a, mem.walk, kW);
+  if (threadIdx.x == 0) {
+    a.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    mem.at = ahead;
+    mem.more[0] = mem.at.next(a, mem.walk, mem.share[0]);
+  }
+  __syncthreads();
 
-  // A stage's rows: lanes 0 .. 15 and 16 .. 31 look up its 16 slots
-  auto lookup = [&](const Share& s, int stage, int& slot) {
-    slot = stage * kStageKeys + (lane & 15);
-    if (stage >= s.s1 || slot >= s.w.total) return -1;
-    const int p = __ldcg(a.pages.table + (size_t)s.seq * a.pages.max_pages + a.pages.place_of(slot));
-    return p;
+  // Copies: a stage's slots, one for each lane, and their pages are looked up one stage before
+  // the copies are issued
+  struct Fetch {
+    int page, slot;      // slot -1: none
+    long long head;
   };
-  auto fetch = [&](const Share& s, int stage, int at, int page, int slot) {
-    if (stage >= s.s1) return;
-    const bool there = slot < s.w.total;
-    if (there && (unsigned)page >= (unsigned)a.pages.n_page)
-      record_status(a.pages.status, kStDevicePage);
-    const bool real = there && (unsigned)page < (unsigned)a.pages.n_page;
-    const long long row = real ? a.pages.row(page, slot) + s.head * a.pages.head_stride : -1;
-    const uint32_t dst = ring + at * Sh::kStageBytes;
-    int t = lane / chunks, ch = lane - t * chunks;
-    const int dt = 32 / chunks, dch = 32 - dt * chunks;
-    for (int i = 0; i < kStageKeys * chunks; i += 32) {
-      const long long from = __shfl_sync(kFull, row, t & 15);
-      if (t < kStageKeys) {
-        const long long in = from < 0 ? 0 : from + ch * 16;
+  Share fs;
+  int fetched = 0;  // the next stage of fs to look up
+  bool any = ahead.next(a, mem.walk, fs);
+  if (any) fetched = fs.s0 + warp;
+  auto lookup = [&](Fetch& f) {
+    while (any && fetched >= fs.s1) {
+      any = ahead.next(a, mem.walk, fs);
+      if (any) fetched = fs.s0 + warp;
+    }
+    f.slot = -2;
+    if (!any) return;
+    f.slot = fetched * Sh::kKeys + (lane & (Sh::kKeys - 1));
+    f.page = -1;
+    if (f.slot < fs.total)
+      f.page = __ldcg(a.pages.table + (size_t)fs.seq * a.pages.max_pages + a.pages.place_of(f.slot));
+    else
+      f.slot = -1;
+    f.head = fs.head * a.pages.head_stride;
+    fetched += kW;
+  };
+  const long long v_from_k = a.pages.v - a.pages.k;
+  auto fetch = [&](const Fetch& f, int at) {
+    if (f.slot != -2) {
+      bool real = f.slot >= 0;
+      if (real && (unsigned)f.page >= (unsigned)a.pages.n_page) {
+        record_status(a.pages.status, kStDevicePage);
+        real = false;
+      }
+      const char* row = real ? a.pages.k + a.pages.row(f.page, f.slot) + f.head : nullptr;
+      const uint32_t dst = ring + at * Sh::kStageBytes;
+      auto copy = [&](int t, int ch) {
+        const char* from = reinterpret_cast<const char*>(
+            __shfl_sync(kFull, reinterpret_cast<unsigned long long>(row), t));
+        const bool there = from != nullptr;
+        from = there ? from + ch * 16 : a.pages.k;
         const uint32_t to = dst + t * Sh::kRowBytes + (swizzle<Sh::kChunks>(t, ch) << 4);
-        cp_async16_or_zero(to, a.pages.k + in, from >= 0);
-        cp_async16_or_zero(to + Sh::kTileBytes, a.pages.v + in, from >= 0);
-      }
-      t += dt;
-      ch += dch;
-      if (ch >= chunks) {
-        ch -= chunks;
-        ++t;
+        cp_async16_or_zero(to, from, there);
+        cp_async16_or_zero(to + Sh::kTileBytes, from + v_from_k, there);
+      };
+      if (chunks == Sh::kChunks) {
+#pragma unroll
+        for (int i = 0; i < Sh::kKeys * Sh::kChunks / 32; ++i) {
+          const int at = 32 * i + lane;
+          copy(at / Sh::kChunks, at % Sh::kChunks);
+        }
+      } else {
+        // whole rows: a warp takes 32 / chunks of them at a time
+        const int rows = 32 / chunks, t0 = lane / chunks, ch = lane - t0 * chunks;
+        for (int t = t0; t - t0 < Sh::kKeys; t += rows) {
+          const bool on = t0 < rows && t < Sh::kKeys;
+          const char* from = reinterpret_cast<const char*>(__shfl_sync(
+              kFull, reinterpret_cast<unsigned long long>(row), t & (Sh::kKeys - 1)));
+          const bool there = from != nullptr;
+          from = there ? from + ch * 16 : a.pages.k;
+          const uint32_t to = dst + t * Sh::kRowBytes + (swizzle<Sh::kChunks>(t, ch) << 4);
+          if (on) {
+            cp_async16_or_zero(to, from, there);
+            cp_async16_or_zero(to + Sh::kTileBytes, from + v_from_k, there);
+          }
+        }
       }
     }
+    cp_async_commit();
   };
-  // The first stages of a share; the page and slot of the next one to fetch
-  int next_page, next_slot;
-  auto begin = [&](const Share& s) {
-    int page[kS - 1], slot[kS - 1];
+  Fetch pending;
+  {
+    Fetch f[kS - 1];
 #pragma unroll
-    for (int i = 0; i < kS - 1; ++i) page[i] = lookup(s, s.s0 + warp + i * kW, slot[i]);
-    next_page = lookup(s, s.s0 + warp + (kS - 1) * kW, next_slot);
+    for (int i = 0; i < kS - 1; ++i) lookup(f[i]);
+    lookup(pending);
 #pragma unroll
-    for (int i = 0; i < kS - 1; ++i) {
-      fetch(s, s.s0 + warp + i * kW, i, page[i], slot[i]);
-      cp_async_commit();
-    }
-  };
+    for (int i = 0; i < kS - 1; ++i) fetch(f[i], i);
+  }
 
-  Share s;
-  bool more = walk.next(s);
-  if (more) begin(s);
-  while (more) {
+  int at = 0;  // the ring's place of the next stage
+  for (int turn = 0; mem.more[turn & 1]; ++turn) {
+    const Share& s = mem.share[turn & 1];
+    const int s1 = s.s1, len = s.len;
     // Q: lane (r, c) holds row r of each n-tile
     uint32_t qf[NT][2 * M][2];
     int sees[NT][2];  // slots that columns 2 c and 2 c + 1 see
     float qs[NT][2];  // what their scores are multiplied by for log2 units
-    int all_see = a.causal ? s.w.len + (s.tile * Sh::kRows) / a.group + 1 : s.w.len;
+    const int all_see = a.causal ? len + (s.tile * Sh::kRows) / a.group + 1 : len;
     const float ks = E4M3 && a.pages.k_scale ? __ldg(a.pages.k_scale + s.head) : 1.f;
     const float vs = E4M3 && a.pages.v_scale ? __ldg(a.pages.v_scale + s.head) : 1.f;
 #pragma unroll
@@ -192,8 +241,8 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
 #pragma unroll
       for (int e = 0; e < 2; ++e)
         sees[t][e] = a.causal
-                         ? s.w.len + (s.tile * Sh::kRows + 8 * t + 2 * c + e) / a.group + 1
-                         : s.w.len;
+                         ? len + (s.tile * Sh::kRows + 8 * t + 2 * c + e) / a.group + 1
+                         : len;
       if (!E4M3) {
         qs[t][0] = qs[t][1] = a.scale * kLog2e;
       } else {
@@ -234,64 +283,64 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
         for (int e = 0; e < 4; ++e) o[t][i][e] = 0.f;
     }
 
-    int at = 0;  // the ring's place of the stage
-    for (int stage = s.s0 + warp; stage < s.s1; stage += kW) {
+    for (int stage = s.s0 + warp; stage < s1; stage += kW) {
       cp_async_wait<kS - 2>();
       __syncwarp();
       {
-        const int ahead = stage + (kS - 1) * kW, page = next_page, slot = next_slot;
-        next_page = lookup(s, ahead + kW, next_slot);
-        fetch(s, ahead, at == 0 ? kS - 1 : at - 1, page, slot);
-        cp_async_commit();
+        const Fetch f = pending;
+        lookup(pending);
+        fetch(f, at == 0 ? kS - 1 : at - 1);
       }
       const uint32_t tile_k = ring + at * Sh::kStageBytes, tile_v = tile_k + Sh::kTileBytes;
       at = at + 1 == kS ? 0 : at + 1;
-      const int key0 = stage * kStageKeys;
-      float x[NT][4];
+      const int key0 = stage * Sh::kKeys;
+      float x[kG][NT][4];
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+      for (int g = 0; g < kG; ++g) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[t][e] = 0.f;
-      const int kt = (lane & 7) + 8 * ((lane >> 3) & 1), kc = lane >> 4;
-      if (E4M3) {
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int j = 0; j < M; ++j) {  // two chunks of 16 dims
+          for (int e = 0; e < 4; ++e) x[g][t][e] = 0.f;
+        const int kt = 16 * g + (lane & 7) + 8 * ((lane >> 3) & 1), kc = lane >> 4;
+#pragma unroll
+        for (int j = 0; j < (E4M3 ? M : 2 * M); ++j) {
           uint32_t w[4];
           ldmatrix4(tile_k + kt * Sh::kRowBytes + (swizzle<Sh::kChunks>(kt, 2 * j + kc) << 4), w);
+          if (E4M3) {  // two chunks of 16 dims
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t f[4] = {e4m3_to_h2(w[2 * h], false), e4m3_to_h2(w[2 * h + 1], false),
-                                   e4m3_to_h2(w[2 * h], true), e4m3_to_h2(w[2 * h + 1], true)};
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t f[4] = {e4m3_to_h2(w[2 * h], false), e4m3_to_h2(w[2 * h + 1], false),
+                                     e4m3_to_h2(w[2 * h], true), e4m3_to_h2(w[2 * h + 1], true)};
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-              mma_16816<false>(x[t], f, qf[t][2 * j + h][0], qf[t][2 * j + h][1]);
+              for (int t = 0; t < NT; ++t)
+                mma_16816<false>(x[g][t], f, qf[t][2 * j + h][0], qf[t][2 * j + h][1]);
+            }
+          } else {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) mma_16816<true>(x[g][t], w, qf[t][j][0], qf[t][j][1]);
           }
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 2 * M; ++j) {
-          uint32_t f[4];
-          ldmatrix4(tile_k + kt * Sh::kRowBytes + (swizzle<Sh::kChunks>(kt, 2 * j + kc) << 4), f);
-#pragma unroll
-          for (int t = 0; t < NT; ++t) mma_16816<true>(x[t], f, qf[t][j][0], qf[t][j][1]);
         }
       }
       // Scores, rounded before the maximum is taken off them (a difference of the unrounded
       // product would be off by half a unit of the maximum), into the running state
-      const bool hides = key0 + kStageKeys > all_see;
+      const bool hides = key0 + Sh::kKeys > all_see;
       bool above = false;
       float top[NT][2];
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          x[t][e] = __fmul_rn(x[t][e], qs[t][e]);
-          x[t][e + 2] = __fmul_rn(x[t][e + 2], qs[t][e]);
-          if (hides) {
-            if (key0 + r >= sees[t][e]) x[t][e] = -INFINITY;
-            if (key0 + r + 8 >= sees[t][e]) x[t][e + 2] = -INFINITY;
-          }
-          top[t][e] = __fadd_ru(fmaxf(x[t][e], x[t][e + 2]), -kPagedLift<E4M3>);
+          float m = -INFINITY;
+#pragma unroll
+          for (int g = 0; g < kG; ++g)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              float& y = x[g][t][e + 2 * h];
+              y = __fmul_rn(y, qs[t][e]);
+              if (hides && key0 + 16 * g + 8 * h + r >= sees[t][e]) y = -INFINITY;
+              m = fmaxf(m, y);
+            }
+          top[t][e] = __fadd_ru(m, -kPagedLift<E4M3>);
           above |= top[t][e] > mx[t][e];
         }
       if (__any_sync(kFull, above)) {
@@ -312,93 +361,110 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
             }
           }
       }
-      uint32_t ph[NT][2], pl[NT][2];  // weights of slots 2 c, 2 c + 1 (and + 8) for row r
+      uint32_t ph[kG][NT][2], pl[kG][NT][2];  // weights of slots 2 c, 2 c + 1 (and + 8) for row r
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const float m = mx[t][e] == -INFINITY ? 0.f : mx[t][e];
-          x[t][e] = exp2_approx(__fadd_rn(x[t][e], -m));
-          x[t][e + 2] = exp2_approx(__fadd_rn(x[t][e + 2], -m));
-          sum[t][e] += x[t][e] + x[t][e + 2];
-        }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (E4M3) {
-            ph[t][h] = transpose_8x8(pack_f16(x[t][2 * h], x[t][2 * h + 1]));
-          } else {
-            uint32_t low;
-            ph[t][h] = transpose_8x8(split_weights(x[t][2 * h], x[t][2 * h + 1], low));
-            pl[t][h] = transpose_8x8(low);
+          for (int g = 0; g < kG; ++g) {
+            x[g][t][e] = exp2_approx(__fadd_rn(x[g][t][e], -m));
+            x[g][t][e + 2] = exp2_approx(__fadd_rn(x[g][t][e + 2], -m));
+            sum[t][e] += x[g][t][e] + x[g][t][e + 2];
           }
         }
-      }
-      auto product = [&](float (&y)[4], const uint32_t (&f)[4], int t) {
-        mma_16816<!E4M3>(y, f, ph[t][0], ph[t][1]);
-        if (!E4M3) mma_16816<true>(y, f, pl[t][0], pl[t][1]);
-      };
-      // V's dims 16 i .. 16 i + 15.  A value that is not finite must not reach the tokens that do
-      // not see its slot, whose weight for it is 0: then the slots go one by one, to those
-      // that do.
-      auto take = [&](int i, const uint32_t (&f)[4]) {
-        if (hides && __any_sync(kFull, odd_pair<E4M3>(f[0]) || odd_pair<E4M3>(f[1]) ||
-                                           odd_pair<E4M3>(f[2]) || odd_pair<E4M3>(f[3]))) {
-#pragma unroll 1
-          for (int slot = 0; slot < kStageKeys; ++slot) {
-            const uint32_t keep = (slot & 7) >> 1 != c ? 0u : slot & 1 ? 0xffff0000u : 0xffffu;
-            const uint32_t g[4] = {slot < 8 ? f[0] & keep : 0u, slot < 8 ? f[1] & keep : 0u,
-                                   slot < 8 ? 0u : f[2] & keep, slot < 8 ? 0u : f[3] & keep};
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-              float y[4] = {0.f, 0.f, 0.f, 0.f};
-              product(y, g, t);
+        for (int g = 0; g < kG; ++g)
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (key0 + slot < sees[t][e & 1]) o[t][i][e] += y[e];
+          for (int h = 0; h < 2; ++h) {
+            if (E4M3) {
+              ph[g][t][h] = transpose_8x8(pack_f16(x[g][t][2 * h], x[g][t][2 * h + 1]));
+            } else {
+              uint32_t low;
+              ph[g][t][h] = transpose_8x8(split_weights(x[g][t][2 * h], x[g][t][2 * h + 1], low));
+              pl[g][t][h] = transpose_8x8(low);
             }
           }
-        } else {
+      }
+      // Calls use(i, f) with V's dims 16 i .. 16 i + 15 of a group of slots.  Rows of f: dims in
+      // order (bf16), or dims 2 r for row r and 2 r + 1 for row r + 8
+      auto values = [&](int g, auto&& use) {
+        const int vt = 16 * g + (lane & 7) + 8 * (E4M3 ? (lane >> 3) & 1 : lane >> 4),
+                  vc = E4M3 ? lane >> 4 : (lane >> 3) & 1;
 #pragma unroll
-          for (int t = 0; t < NT; ++t) product(o[t][i], f, t);
-        }
-      };
-      if (E4M3) {
-        const int vt = (lane & 7) + 8 * ((lane >> 3) & 1), vc = lane >> 4;
-#pragma unroll
-        for (int j = 0; j < M; ++j) {
+        for (int j = 0; j < (E4M3 ? M : 2 * M); ++j) {
           uint32_t w[4];
           ldmatrix4_trans(tile_v + vt * Sh::kRowBytes + (swizzle<Sh::kChunks>(vt, 2 * j + vc) << 4),
                           w);
+          if (E4M3) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            // a word: dims 2 r, 2 r + 1 of slot 2 c, then of 2 c + 1; rows r and r + 8 of the
-            // product are dims 2 r and 2 r + 1
-            const uint32_t lo = __byte_perm(w[2 * h], 0, 0x3120),
-                           hi = __byte_perm(w[2 * h + 1], 0, 0x3120);
-            const uint32_t f[4] = {e4m3_to_h2(lo, false), e4m3_to_h2(lo, true),
-                                   e4m3_to_h2(hi, false), e4m3_to_h2(hi, true)};
-            take(2 * j + h, f);
+            for (int h = 0; h < 2; ++h) {
+              // a word: dims 2 r, 2 r + 1 of slot 2 c, then of slot 2 c + 1
+              const uint32_t lo = __byte_perm(w[2 * h], 0, 0x3120),
+                             hi = __byte_perm(w[2 * h + 1], 0, 0x3120);
+              const uint32_t f[4] = {e4m3_to_h2(lo, false), e4m3_to_h2(lo, true),
+                                     e4m3_to_h2(hi, false), e4m3_to_h2(hi, true)};
+              use(2 * j + h, f);
+            }
+          } else {
+            use(j, w);
           }
         }
-      } else {
-        const int vt = (lane & 7) + 8 * (lane >> 4), vc = (lane >> 3) & 1;
+      };
+      auto product = [&](float (&y)[4], const uint32_t (&f)[4], int g, int t) {
+        mma_16816<!E4M3>(y, f, ph[g][t][0], ph[g][t][1]);
+        if (!E4M3) mma_16816<true>(y, f, pl[g][t][0], pl[g][t][1]);
+      };
+      // A value that is not finite must not reach the tokens that do not see its slot, whose
+      // weight for it is 0: then the slots go one by one, to those that do.
+      bool odd = false;
+      if (hides) {
+        for (int i = lane; i < Sh::kTileBytes / 16; i += 32) {
+          const uint4 w = ld_shared16(tile_v + 16 * i);
+          odd |= not_finite<E4M3>(w.x) || not_finite<E4M3>(w.y) || not_finite<E4M3>(w.z) ||
+                 not_finite<E4M3>(w.w);
+        }
+        odd = __any_sync(kFull, odd);
+      }
+      if (!odd) {
 #pragma unroll
-        for (int j = 0; j < 2 * M; ++j) {
-          uint32_t f[4];
-          ldmatrix4_trans(tile_v + vt * Sh::kRowBytes + (swizzle<Sh::kChunks>(vt, 2 * j + vc) << 4),
-                          f);
-          take(j, f);
+        for (int g = 0; g < kG; ++g)
+          values(g, [&](int i, const uint32_t (&f)[4]) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) product(o[t][i], f, g, t);
+          });
+      } else {
+#pragma unroll
+        for (int g = 0; g < kG; ++g) {
+#pragma unroll 1
+          for (int slot = 0; slot < 16; ++slot) {
+            const uint32_t keep = (slot & 7) >> 1 != c ? 0u : slot & 1 ? 0xffff0000u : 0xffffu;
+            const uint32_t first = slot < 8 ? keep : 0u, second = slot < 8 ? 0u : keep;
+            values(g, [&](int i, const uint32_t (&f)[4]) {
+              const uint32_t one[4] = {f[0] & first, f[1] & first, f[2] & second, f[3] & second};
+#pragma unroll
+              for (int t = 0; t < NT; ++t) {
+                float y[4] = {0.f, 0.f, 0.f, 0.f};
+                product(y, one, g, t);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  if (key0 + 16 * g + slot < sees[t][e & 1]) o[t][i][e] += y[e];
+              }
+            });
+          }
         }
       }
       __syncwarp();
     }
 
-    // the next share's first stages come while this one's warps meet
-    cp_async_wait<0>();
-    __syncwarp();
-    Share next;
-    more = walk.next(next);
-    if (more) begin(next);
+    // The warps meet
+    if (threadIdx.x == 32 * (kW - 1)) {
+      const int i = (turn + 1) & 1;
+      mem.more[i] = mem.at.next(a, mem.walk, mem.share[i]);
+      if (s.slot >= 0 && s.s0 == 0) a.split[blockIdx.x] = split_of(a, s);
+    }
+    const bool whole = s.slot < 0;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
 #pragma unroll
@@ -437,7 +503,7 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
           f[w] = st.x == -INFINITY ? 0.f : exp2_approx(st.x - top);
           total += st.x == -INFINITY ? 0.f : f[w] * st.y;
         }
-        const float scale = s.whole ? (top == -INFINITY ? 0.f : vs / total) : vs;
+        const float scale = whole ? (top == -INFINITY ? 0.f : vs / total) : vs;
         const size_t part = (size_t)s.slot * Sh::kRows + 8 * t + q;
         for (int d = 4 * lane; d < a.d; d += 128) {
           float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -451,14 +517,14 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
             y.w += f[w] * z.w;
           }
           y = make_float4(y.x * scale, y.y * scale, y.z * scale, y.w * scale);
-          if (s.whole)
+          if (whole)
             *reinterpret_cast<uint2*>(a.out + row * a.d + d) =
                 make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
           else
             *reinterpret_cast<float4*>(a.parts + part * a.d + d) = y;
         }
         if (lane == 0) {
-          if (!s.whole)
+          if (!whole)
             a.stats[part] = make_float2(top, total);
           else if (a.lse)
             a.lse[row] = (top + log2f(total)) * kLn2;
@@ -466,22 +532,20 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
       }
       __syncthreads();
     }
-    if (threadIdx.x == 0 && !s.whole && s.s0 == 0)
-      a.split[blockIdx.x] = make_int4(s.seq, s.head, s.tile, s.last);
-    s = next;
   }
   write_empty(a);
 }
 
 struct PagedKernel {
   void (*kern)(PagedAttendArgs);
-  int smem, rows, threads;
+  int smem, rows, threads, stage_keys;
 };
 
 template <int M, int NT, bool E4M3>
 constexpr PagedKernel paged_stream() {
   using Sh = StreamShape<M, NT, E4M3>;
-  return {paged_stream_kernel<M, NT, E4M3>, Sh::kTotal, Sh::kRows, Sh::kStreamThreads};
+  return {paged_stream_kernel<M, NT, E4M3>, Sh::kTotal, Sh::kRows, Sh::kStreamThreads,
+          Sh::kKeys};
 }
 
 // [(head_dim + 31) / 32 - 1][tiles of 8 or 16 rows]
