@@ -8,6 +8,7 @@
 
 #include <climits>
 #include <cstdint>
+#include <mutex>
 
 #include "vd_host.cuh"
 #include "vd_paged.cuh"
@@ -94,10 +95,53 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(PagedAttendArgs a)
   if (threadIdx.x == 0 && a.lse) a.lse[row] = (top + log2f(sum)) * kLn2;
 }
 
+// CTAs of a kernel that run at once on a device, in clusters of 1, 2, 4, 8, 16 (0: such a
+// cluster does not fit); asked for once per device and kernel.
+struct Slots {
+  bool ready;
+  int at[5];
+};
+std::mutex g_slots_mu;
+Slots g_slots[64][2][8][2];
+
+vd_status slots_of(const DeviceInfo& dev, const PagedKernel& k, Slots& s) {
+  std::lock_guard<std::mutex> lk(g_slots_mu);
+  if (s.ready) return VD_OK;
+  if (cudaFuncSetAttribute(k.kern, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem) !=
+          cudaSuccess ||
+      cudaFuncSetAttribute(k.kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) !=
+          cudaSuccess) {
+    cudaGetLastError();
+    return VD_ERR_CUDA;
+  }
+  for (int e = 0; e < 5; ++e) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(16 * dev.sms);
+    cfg.blockDim = dim3(k.threads);
+    cfg.dynamicSmemBytes = k.smem;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 1u << e;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, k.kern, &cfg) != cudaSuccess) {
+      cudaGetLastError();
+      n = 0;
+    }
+    s.at[e] = n << e;
+  }
+  if (s.at[0] < 1) return VD_ERR_CUDA;
+  s.ready = true;
+  return VD_OK;
+}
+
 struct Plan {
   const PagedKernel* kernel;
-  int rows, ctas;
+  int rows, tiles, cluster, ctas;
   size_t split, stats, parts;  // bytes of the workspace's three parts
+  unsigned* status;
 };
 
 // Refuses what the call refuses of its sizes.
@@ -111,12 +155,28 @@ vd_status plan_of(const vd_paged_cache* c, int n_q_head, int B, Plan* plan) {
   DeviceInfo dev;
   r = device_info(&dev);
   if (r != VD_OK) return r;
-  const auto& kernels = c->type == VD_PAGED_E4M3 ? kPagedE4m3 : kPagedBf16;
-  plan->kernel = &kernels[(c->head_dim + 31) / 32 - 1][rows > 8];
-  plan->rows = plan->kernel->rows;
-  plan->ctas = dev.sms;
-  const size_t parts = 2 * (size_t)plan->ctas * plan->rows;
-  plan->split = (size_t)plan->ctas * sizeof(int4);
+  const bool e4m3 = c->type == VD_PAGED_E4M3;
+  const int m = (c->head_dim + 31) / 32 - 1, nt = rows > 8;
+  const PagedKernel& k = (e4m3 ? kPagedE4m3 : kPagedBf16)[m][nt];
+  Slots& slots = g_slots[dev.id][e4m3][m][nt];
+  r = slots_of(dev, k, slots);
+  if (r != VD_OK) return r;
+  plan->kernel = &k;
+  plan->status = dev.status;
+  plan->rows = k.rows;
+  plan->tiles = (int)((rows + k.rows - 1) / k.rows);
+  // A cluster for each unit: the largest with which they run at once
+  const long long units = (long long)c->n_seq * c->n_kv_head * plan->tiles;
+  const long long capacity = (long long)c->page_size * c->max_pages;
+  int e = 4;
+  while (e > 0 && (units << e > slots.at[e] || capacity < 128 << e)) --e;
+  if (capacity > 1024 << e) e = 0;
+  const int want = env_int("VD_PAGED_CLUSTER", -1);
+  if (want == 1) e = 0;
+  plan->cluster = 1 << e;
+  plan->ctas = e > 0 ? (int)(units << e) : slots.at[0];
+  const size_t parts = e > 0 ? 0 : 2 * (size_t)plan->ctas * plan->rows;
+  plan->split = e > 0 ? 0 : (size_t)plan->ctas * sizeof(int4);
   plan->stats = parts * sizeof(float2);
   plan->parts = parts * c->head_dim * sizeof(float);
   return VD_OK;
@@ -130,7 +190,8 @@ extern "C" {
 
 size_t vd_paged_attend_workspace(const vd_paged_cache* c, int32_t n_q_head, int32_t B) {
   vd::Plan p;
-  return vd::plan_of(c, n_q_head, B, &p) == VD_OK ? p.split + p.stats + p.parts : 0;
+  // at least one unit of 16 bytes: a workspace is never empty
+  return vd::plan_of(c, n_q_head, B, &p) == VD_OK ? 16 + p.split + p.stats + p.parts : 0;
 }
 
 vd_status vd_paged_attend(const vd_paged_cache* c, int32_t layer, const void* q, int32_t B,
@@ -147,12 +208,9 @@ vd_status vd_paged_attend(const vd_paged_cache* c, int32_t layer, const void* q,
   Plan p;
   r = plan_of(c, n_q_head, B, &p);
   if (r != VD_OK) return r;
-  if (workspace_bytes < p.split + p.stats + p.parts) return VD_ERR_INVALID_ARG;
-  DeviceInfo dev;
-  r = device_info(&dev);
-  if (r != VD_OK) return r;
+  if (workspace_bytes < 16 + p.split + p.stats + p.parts) return VD_ERR_INVALID_ARG;
   PagedAttendArgs a;
-  a.pages = pages_of(c, layer, dev.status);
+  a.pages = pages_of(c, layer, p.status);
   a.q = static_cast<const uint16_t*>(q);
   a.out = static_cast<uint16_t*>(out);
   a.lse = lse_out;
@@ -171,14 +229,12 @@ vd_status vd_paged_attend(const vd_paged_cache* c, int32_t layer, const void* q,
   a.causal = causal != 0;
   a.scale = scale;
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  a.tiles = p.tiles;
+  a.cluster = p.cluster;
   const PagedKernel& k = *p.kernel;
-  if (cudaFuncSetAttribute(k.kern, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem) !=
-      cudaSuccess) {
-    cudaGetLastError();
-    return VD_ERR_CUDA;
-  }
-  r = launch_clusters((unsigned)p.ctas, (unsigned)k.threads, 1, k.smem, s, k.kern, a);
-  if (r != VD_OK) return r;
+  r = launch_clusters((unsigned)p.ctas, (unsigned)k.threads, (unsigned)p.cluster, k.smem, s, k.kern,
+                      a);
+  if (r != VD_OK || p.cluster > 1) return r;
   return launch_dependent((unsigned)(p.ctas * p.rows), s, paged_join_kernel, a);
 }
 

@@ -8,6 +8,10 @@
 // A CTA that holds all stages of a unit writes its output.  Of the others it writes a part (sums
 // relative to a reference, the reference, the sum of weights), and paged_join_kernel puts
 // the parts of a unit together, in order: the same bits every time.
+//
+// Where the units are so few that several CTAs can take each, a cluster takes a unit instead and
+// joins its CTAs' parts through distributed shared memory: one launch, and no look at the other
+// sequences.
 #pragma once
 
 #include <cstdint>
@@ -32,6 +36,8 @@ struct PagedAttendArgs {
   float* parts;          // ... [2 CTAs][rows][d] sums
   int n_seq, heads, group, B, d;
   int rows;              // of a tile
+  int tiles;             // of B tokens
+  int cluster;           // CTAs that share a unit, or 1: pieces of the line
   int stage_keys;        // slots of a stage
   int causal;
   float scale;
@@ -42,16 +48,17 @@ constexpr float kLn2 = 0.69314718055994531f;
 // What a sequence has to do.
 struct SeqWork {
   int len, add, total, tiles;  // slots, new tokens, slots that the last of them sees
-  int stages;
-  long long work;              // stages of all its units
+  int stages;                  // of a unit
+  __device__ __forceinline__ long long all(int heads) const {
+    return (long long)stages * tiles * heads;
+  }
 };
 
 __device__ __forceinline__ SeqWork seq_work(const PagedAttendArgs& a, int len, int add) {
-  SeqWork w = {len, add, 0, 0, 0, 0};
+  SeqWork w = {len, add, 0, 0, 0};
   w.total = add == 0 ? 0 : len + (a.causal ? add : 0);
   w.tiles = (add * a.group + a.rows - 1) / a.rows;
   w.stages = (w.total + a.stage_keys - 1) / a.stage_keys;
-  w.work = (long long)w.stages * w.tiles * a.heads;
   return w;
 }
 
@@ -84,16 +91,18 @@ struct Cut {
 };
 
 // A CTA's share of a unit: stages [s0, s1).
+constexpr int kWhole = -1, kOfCluster = -2;
+
 struct Share {
   int seq, head, tile, s0, s1;
   int len, add, total;  // of the sequence, as in SeqWork
-  int slot;  // of the part; -1: the whole unit
-  int last;  // the last CTA that has a part of the unit, where this share begins it
+  int slot;  // of the part; kWhole: the whole unit, kOfCluster: a part of the cluster's unit
 };
 
 constexpr int kChunk = 64;  // sequences that are looked at together
 
 struct WalkMem {
+  Cut cut;
   long long end[kChunk];  // where each ends on the line
   int2 size[kChunk];
   long long sum[32];
@@ -102,11 +111,11 @@ struct WalkMem {
 // Walks over a CTA's piece of the line.  All threads of the CTA construct it together; then each
 // warp may go its own way.
 struct Walk {
-  Cut cut;
   long long at, end;  // line positions: the next stage, the piece's end
   int chunk, seq, head, tile, stage;
   SeqWork w;          // of seq
 
+  __device__ Walk() : at(0), end(0) {}
   // Pieces of `least` stages at least.
   __device__ Walk(const PagedAttendArgs& a, WalkMem& m, int least)
       : at(0), end(0), chunk(0), seq(0), head(0), tile(0), stage(0), w() {
@@ -116,7 +125,7 @@ struct Walk {
       long long mine = 0;
       for (int s = kChunk + threadIdx.x; s < a.n_seq; s += blockDim.x) {
         const int2 n = seq_size(a, s, blockIdx.x == 0);
-        mine += seq_work(a, n.x, n.y).work;
+        mine += seq_work(a, n.x, n.y).all(a.heads);
       }
 #pragma unroll
       for (int off = 16; off > 0; off >>= 1) mine += __shfl_xor_sync(kFull, mine, off);
@@ -124,10 +133,12 @@ struct Walk {
       __syncthreads();
       for (int i = 0; i < (int)blockDim.x / 32; ++i) all += m.sum[i];
     }
+    Cut cut;
     const long long most = divide(all, least);
     cut.ctas = most >= (long long)gridDim.x ? (int)gridDim.x : most > 1 ? (int)most : 1;
     cut.per = divide(all, cut.ctas);
     cut.more = (int)(all - cut.per * cut.ctas);
+    if (threadIdx.x == 0) m.cut = cut;
     if ((int)blockIdx.x >= cut.ctas) return;
     at = cut.begin(blockIdx.x);
     end = cut.begin(blockIdx.x + 1);
@@ -156,21 +167,22 @@ struct Walk {
   __device__ void load(const PagedAttendArgs& a, WalkMem& m, long long begin, bool report) {
     __syncthreads();  // the last chunk's readers
     if (threadIdx.x < 32) {
-      const int lane = threadIdx.x;
+      static_assert(kChunk == 64, "two sequences a lane");
+      const int i = 2 * threadIdx.x, s = chunk + i;
+      const int2 none = make_int2(0, 0), n0 = s < a.n_seq ? seq_size(a, s, report) : none,
+                 n1 = s + 1 < a.n_seq ? seq_size(a, s + 1, report) : none;
+      const long long x0 = seq_work(a, n0.x, n0.y).all(a.heads),
+                      x1 = seq_work(a, n1.x, n1.y).all(a.heads);
+      long long x = x0 + x1;
 #pragma unroll
-      for (int i = 0; i < kChunk; i += 32) {
-        const int s = chunk + i + lane;
-        const int2 n = s < a.n_seq ? seq_size(a, s, report) : make_int2(0, 0);
-        long long x = seq_work(a, n.x, n.y).work;
-#pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-          const long long y = __shfl_up_sync(kFull, x, off);
-          if (lane >= off) x += y;
-        }
-        m.end[i + lane] = begin + x;
-        m.size[i + lane] = n;
-        begin += __shfl_sync(kFull, x, 31);
+      for (int off = 1; off < 32; off <<= 1) {
+        const long long y = __shfl_up_sync(kFull, x, off);
+        if ((int)threadIdx.x >= off) x += y;
       }
+      m.end[i] = begin + x - x1;
+      m.end[i + 1] = begin + x;
+      m.size[i] = n0;
+      m.size[i + 1] = n1;
     }
     __syncthreads();
   }
@@ -188,8 +200,7 @@ struct Walk {
     s.s1 = stage += n;
     at += n;
     // a CTA's first share may begin inside a unit, its last one may end there
-    s.slot = n == w.stages ? -1 : 2 * (int)blockIdx.x + (s.s0 == 0 ? 1 : 0);
-    s.last = s.slot < 0 || s.s0 > 0 ? 0 : cut.holder(at + (w.stages - stage) - 1);
+    s.slot = n == w.stages ? kWhole : 2 * (int)blockIdx.x + (s.s0 == 0 ? 1 : 0);
     if (stage == w.stages) {
       stage = 0;
       if (++tile == w.tiles) {
@@ -200,7 +211,7 @@ struct Walk {
               ++seq;
               const int2 n = seq - chunk < kChunk ? m.size[seq - chunk] : seq_size(a, seq, false);
               w = seq_work(a, n.x, n.y);
-            } while (w.work == 0);
+            } while (w.all(a.heads) == 0);
         }
       }
     }
@@ -208,11 +219,31 @@ struct Walk {
   }
 };
 
-// What the join has to know of such a unit.
-__device__ __forceinline__ int4 split_of(const PagedAttendArgs& a, const Share& s) {
+// The share of a CTA of a cluster, with no stage where there are fewer than CTAs; false: the unit
+// has nothing to do.
+__device__ __forceinline__ bool cluster_share(const PagedAttendArgs& a, Share& s) {
+  const int rank = blockIdx.x % a.cluster, unit = blockIdx.x / a.cluster;
+  s.tile = unit % a.tiles;
+  s.head = unit / a.tiles % a.heads;
+  s.seq = unit / a.tiles / a.heads;
+  const int2 n = seq_size(a, s.seq, rank == 0 && s.tile == 0 && s.head == 0);
+  const SeqWork w = seq_work(a, n.x, n.y);
+  s.len = w.len;
+  s.add = w.add;
+  s.total = w.total;
+  s.s0 = (int)((long long)w.stages * rank / a.cluster);
+  s.s1 = (int)((long long)w.stages * (rank + 1) / a.cluster);
+  s.slot = kOfCluster;
+  return s.tile < w.tiles && w.total > 0;
+}
+
+// What the join has to know of such a unit; `at`: the line's position behind the share.
+__device__ __forceinline__ int4 split_of(const PagedAttendArgs& a, const Cut& cut, const Share& s,
+                                         long long at) {
   const int row0 = s.tile * a.rows;
+  const int left = seq_work(a, s.len, s.add).stages - s.s1;
   return make_int4((s.seq * a.B * a.heads + s.head) * a.group, row0,
-                   min(a.rows, s.add * a.group - row0), s.last);
+                   min(a.rows, s.add * a.group - row0), cut.holder(at + left - 1));
 }
 
 // Where a tile's row lies: out and q at row * d, lse at row.  -1: no such row.

@@ -67,7 +67,7 @@ struct StreamShape {
   static constexpr int kStreamWarps = M <= 4 ? 8 : 4;
   static constexpr int kStreamThreads = 32 * kStreamWarps;
   static constexpr int kStages =
-      E4M3 ? (M == 2 || M == 8 ? 5 : M == 3 ? 4 : M == 4 ? 3 : 6) : (M == 3 || M == 6 ? 4 : 3);
+      E4M3 ? (M == 2 ? 5 : M == 3 || M == 8 ? 4 : M == 4 ? 3 : 6) : (M == 3 || M == 6 ? 4 : 3);
   static constexpr int kRing = kStreamWarps * kStages * kStageBytes;
   static constexpr int kPart = kD + 4;  // floats of a partial row
   static constexpr int kParts = kRing;  // [warp][8 rows]
@@ -77,14 +77,19 @@ struct StreamShape {
   static_assert(kTotal <= 232448, "shared memory");
 };
 
-// The chunk (16 bytes) of a row at which chunk c lies, so that the same chunk of 8 rows falls on
+// Chunk c (16 bytes) of a row lies at c ^ turn(row), so that the same chunk of 8 rows falls on
 // different banks.
 template <int kChunks>
-__device__ __forceinline__ int swizzle(int row, int c) {
-  if (kChunks % 8 == 0) return c ^ (row & 7);
-  if (kChunks % 4 == 0) return c ^ ((row >> 1) & 3);
-  return c ^ ((row >> 2) & 1);
-}
+struct Swizzle {
+  static constexpr int kMask = kChunks % 8 == 0 ? 7 : kChunks % 4 == 0 ? 3 : 1;
+  static __device__ __forceinline__ int turn(int row) {
+    return (kMask == 7 ? row : kMask == 3 ? row >> 1 : row >> 2) & kMask;
+  }
+  // From the address of chunk 0 or 1 of a row to the chunk `even` further.
+  static __device__ __forceinline__ uint32_t step(uint32_t addr, int even) {
+    return (addr ^ ((even & kMask) << 4)) + ((even & ~kMask) << 4);
+  }
+};
 
 // The running maximum less this is the point that weights are relative to: fp16 weights far
 // below the largest keep their bits, and the point moves only where the maximum rises by more.
@@ -112,6 +117,7 @@ template <int M, int NT, bool E4M3>
 __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
     paged_stream_kernel(PagedAttendArgs a) {
   using Sh = StreamShape<M, NT, E4M3>;
+  using Sw = Swizzle<Sh::kChunks>;
   constexpr int kW = Sh::kStreamWarps, kS = Sh::kStages, kG = Sh::kGroups;
   extern __shared__ __align__(128) unsigned char smem[];
   const uint32_t base = smem_addr(smem);
@@ -128,30 +134,55 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
   grid_dependency_wait();
   grid_launch_dependents();
   StreamMem& mem = *reinterpret_cast<StreamMem*>(smem + Sh::kMem);
-  Walk ahead(a, mem.walk, kW);
-  if (threadIdx.x == 0) {
-    a.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
-    mem.at = ahead;
-    mem.more[0] = mem.at.next(a, mem.walk, mem.share[0]);
+  Walk ahead;
+  Share fs;  // the share whose stages are being fetched
+  bool any;
+  if (a.cluster > 1) {
+    any = cluster_share(a, fs);
+  } else {
+    ahead = Walk(a, mem.walk, kW);
+    any = ahead.next(a, mem.walk, fs);
   }
+  if (threadIdx.x == 0) {
+    if (a.cluster == 1) a.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    mem.at = ahead;
+    mem.more[0] = any;
+    mem.share[0] = fs;
+  }
+  int fetched = fs.s0 + warp;  // the next stage of fs to look up
+
+  // Q: lane (r, c) holds row r of each n-tile
+  uint32_t qf[NT][2 * M][2];
+  auto load_queries = [&](const Share& s) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const long long row = out_row(a, s, 8 * t + r);
+      const uint32_t* src = reinterpret_cast<const uint32_t*>(a.q + (row < 0 ? 0 : row) * a.d);
+#pragma unroll
+      for (int j = 0; j < 2 * M; ++j) {
+        // e4m3: chunk j's dims 4 c .. 4 c + 3; bf16: chunks 2 j and 2 j + 1, dims 2 c, 2 c + 1
+        const int d0 = 16 * j + (E4M3 ? 4 : 2) * c, d1 = E4M3 ? d0 + 2 : d0 + 8;
+        qf[t][j][0] = row >= 0 && d0 < a.d ? __ldcg(src + d0 / 2) : 0u;
+        qf[t][j][1] = row >= 0 && d1 < a.d ? __ldcg(src + d1 / 2) : 0u;
+      }
+    }
+  };
+  if (any) load_queries(fs);  // ahead of the copies, behind which they would wait
   __syncthreads();
 
   // Copies: a stage's slots, one for each lane, and their pages are looked up one stage before
   // the copies are issued
+  constexpr int kNoStage = -2;
   struct Fetch {
-    int page, slot;      // slot -1: none
+    int page, slot;  // slot -1: none, kNoStage: no copies at all
     long long head;
   };
-  Share fs;
-  int fetched = 0;  // the next stage of fs to look up
-  bool any = ahead.next(a, mem.walk, fs);
-  if (any) fetched = fs.s0 + warp;
   auto lookup = [&](Fetch& f) {
     while (any && fetched >= fs.s1) {
       any = ahead.next(a, mem.walk, fs);
       if (any) fetched = fs.s0 + warp;
     }
-    f.slot = -2;
+    f.slot = kNoStage;
     if (!any) return;
     f.slot = fetched * Sh::kKeys + (lane & (Sh::kKeys - 1));
     f.page = -1;
@@ -164,7 +195,7 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
   };
   const long long v_from_k = a.pages.v - a.pages.k;
   auto fetch = [&](const Fetch& f, int at) {
-    if (f.slot != -2) {
+    if (f.slot != kNoStage) {
       bool real = f.slot >= 0;
       if (real && (unsigned)f.page >= (unsigned)a.pages.n_page) {
         record_status(a.pages.status, kStDevicePage);
@@ -177,7 +208,7 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
             __shfl_sync(kFull, reinterpret_cast<unsigned long long>(row), t));
         const bool there = from != nullptr;
         from = there ? from + ch * 16 : a.pages.k;
-        const uint32_t to = dst + t * Sh::kRowBytes + (swizzle<Sh::kChunks>(t, ch) << 4);
+        const uint32_t to = dst + t * Sh::kRowBytes + ((ch ^ Sw::turn(t)) << 4);
         cp_async16_or_zero(to, from, there);
         cp_async16_or_zero(to + Sh::kTileBytes, from + v_from_k, there);
       };
@@ -196,7 +227,7 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
               kFull, reinterpret_cast<unsigned long long>(row), t & (Sh::kKeys - 1)));
           const bool there = from != nullptr;
           from = there ? from + ch * 16 : a.pages.k;
-          const uint32_t to = dst + t * Sh::kRowBytes + (swizzle<Sh::kChunks>(t, ch) << 4);
+          const uint32_t to = dst + t * Sh::kRowBytes + ((ch ^ Sw::turn(t)) << 4);
           if (on) {
             cp_async16_or_zero(to, from, there);
             cp_async16_or_zero(to + Sh::kTileBytes, from + v_from_k, there);
@@ -216,28 +247,23 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
     for (int i = 0; i < kS - 1; ++i) fetch(f[i], i);
   }
 
+  // Where a lane's row of the four 8 x 8 blocks of a matrix load lies in a tile: blocks of K are
+  // slots 0-7, 8-15 of a chunk, then of the next one; of V in bf16, chunks go first
+  const int slots8 = lane & 7, b3 = (lane >> 3) & 1, b4 = lane >> 4;
+  const int k_slot = slots8 + 8 * b3, v_slot = slots8 + 8 * (E4M3 ? b3 : b4);
+  const uint32_t k_lane = k_slot * Sh::kRowBytes + ((b4 ^ Sw::turn(k_slot)) << 4);
+  const uint32_t v_lane = v_slot * Sh::kRowBytes + (((E4M3 ? b4 : b3) ^ Sw::turn(v_slot)) << 4);
   int at = 0;  // the ring's place of the next stage
   for (int turn = 0; mem.more[turn & 1]; ++turn) {
     const Share& s = mem.share[turn & 1];
     const int s1 = s.s1, len = s.len;
-    // Q: lane (r, c) holds row r of each n-tile
-    uint32_t qf[NT][2 * M][2];
     int sees[NT][2];  // slots that columns 2 c and 2 c + 1 see
     float qs[NT][2];  // what their scores are multiplied by for log2 units
     const int all_see = a.causal ? len + (s.tile * Sh::kRows) / a.group + 1 : len;
-    const float ks = E4M3 && a.pages.k_scale ? __ldg(a.pages.k_scale + s.head) : 1.f;
-    const float vs = E4M3 && a.pages.v_scale ? __ldg(a.pages.v_scale + s.head) : 1.f;
+    const float ks = E4M3 && a.pages.k_scale ? __ldcg(a.pages.k_scale + s.head) : 1.f;
+    const float vs = E4M3 && a.pages.v_scale ? __ldcg(a.pages.v_scale + s.head) : 1.f;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const long long row = out_row(a, s, 8 * t + r);
-#pragma unroll
-      for (int j = 0; j < 2 * M; ++j) {
-        // e4m3: chunk j's dims 4 c .. 4 c + 3; bf16: chunks 2 j and 2 j + 1, dims 2 c, 2 c + 1
-        const int d0 = 16 * j + (E4M3 ? 4 : 2) * c, d1 = E4M3 ? d0 + 2 : d0 + 8;
-        const uint32_t* src = reinterpret_cast<const uint32_t*>(a.q + (row < 0 ? 0 : row) * a.d);
-        qf[t][j][0] = row >= 0 && d0 < a.d ? __ldcg(src + d0 / 2) : 0u;
-        qf[t][j][1] = row >= 0 && d1 < a.d ? __ldcg(src + d1 / 2) : 0u;
-      }
 #pragma unroll
       for (int e = 0; e < 2; ++e)
         sees[t][e] = a.causal
@@ -301,11 +327,10 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
         for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int e = 0; e < 4; ++e) x[g][t][e] = 0.f;
-        const int kt = 16 * g + (lane & 7) + 8 * ((lane >> 3) & 1), kc = lane >> 4;
 #pragma unroll
         for (int j = 0; j < (E4M3 ? M : 2 * M); ++j) {
           uint32_t w[4];
-          ldmatrix4(tile_k + kt * Sh::kRowBytes + (swizzle<Sh::kChunks>(kt, 2 * j + kc) << 4), w);
+          ldmatrix4(Sw::step(tile_k + k_lane, 2 * j) + 16 * g * Sh::kRowBytes, w);
           if (E4M3) {  // two chunks of 16 dims
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -390,13 +415,10 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
       // Calls use(i, f) with V's dims 16 i .. 16 i + 15 of a group of slots.  Rows of f: dims in
       // order (bf16), or dims 2 r for row r and 2 r + 1 for row r + 8
       auto values = [&](int g, auto&& use) {
-        const int vt = 16 * g + (lane & 7) + 8 * (E4M3 ? (lane >> 3) & 1 : lane >> 4),
-                  vc = E4M3 ? lane >> 4 : (lane >> 3) & 1;
 #pragma unroll
         for (int j = 0; j < (E4M3 ? M : 2 * M); ++j) {
           uint32_t w[4];
-          ldmatrix4_trans(tile_v + vt * Sh::kRowBytes + (swizzle<Sh::kChunks>(vt, 2 * j + vc) << 4),
-                          w);
+          ldmatrix4_trans(Sw::step(tile_v + v_lane, 2 * j) + 16 * g * Sh::kRowBytes, w);
           if (E4M3) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -461,10 +483,13 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
     // The warps meet
     if (threadIdx.x == 32 * (kW - 1)) {
       const int i = (turn + 1) & 1;
+      if (s.slot >= 0 && s.s0 == 0)
+        a.split[blockIdx.x] = split_of(a, mem.walk.cut, s, mem.at.at);
       mem.more[i] = mem.at.next(a, mem.walk, mem.share[i]);
-      if (s.slot >= 0 && s.s0 == 0) a.split[blockIdx.x] = split_of(a, s);
     }
-    const bool whole = s.slot < 0;
+    const bool whole = s.slot == kWhole;
+    float* joint = reinterpret_cast<float*>(smem);  // of a cluster: [row][kD], [row] max, sum
+    float2* joint_stats = reinterpret_cast<float2*>(joint + Sh::kRows * Sh::kD);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
 #pragma unroll
@@ -490,6 +515,7 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
         if (r == 0) stats[warp * 8 + 2 * c + e] = make_float2(mx[t][e], sum[t][e]);
       }
       __syncthreads();
+      if (t == 0 && mem.more[(turn + 1) & 1]) load_queries(mem.share[(turn + 1) & 1]);
 #pragma unroll 1
       for (int q = warp; q < 8; q += kW) {
         const long long row = out_row(a, s, 8 * t + q);
@@ -521,16 +547,66 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
             *reinterpret_cast<uint2*>(a.out + row * a.d + d) =
                 make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
           else
-            *reinterpret_cast<float4*>(a.parts + part * a.d + d) = y;
+            *reinterpret_cast<float4*>(s.slot == kOfCluster ? joint + (8 * t + q) * Sh::kD + d
+                                                            : a.parts + part * a.d + d) = y;
         }
         if (lane == 0) {
           if (!whole)
-            a.stats[part] = make_float2(top, total);
+            *(s.slot == kOfCluster ? joint_stats + 8 * t + q : a.stats + part) =
+                make_float2(top, total);
           else if (a.lse)
             a.lse[row] = (top + log2f(total)) * kLn2;
         }
       }
       __syncthreads();
+    }
+    if (s.slot == kOfCluster) {
+      cluster_sync();
+      for (int q = blockIdx.x % a.cluster + a.cluster * warp; q < Sh::kRows; q += a.cluster * kW) {
+        const long long row = out_row(a, s, q);
+        if (row < 0) continue;
+        float2 mine = make_float2(-INFINITY, 0.f);
+        if (lane < a.cluster) {
+          const uint64_t w = ld_cluster_u64(mapa(smem_addr(joint_stats + q), lane));
+          mine = make_float2(__uint_as_float((uint32_t)w), __uint_as_float((uint32_t)(w >> 32)));
+        }
+        float top = mine.x;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, off));
+        const float f = mine.x == -INFINITY ? 0.f : exp2_approx(mine.x - top);
+        float total = mine.x == -INFINITY ? 0.f : f * mine.y;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) total += __shfl_xor_sync(kFull, total, off);
+        const float inverse = top == -INFINITY ? 0.f : 1.f / total;
+        const unsigned seen = __ballot_sync(kFull, mine.x != -INFINITY);
+        for (int d0 = 0; d0 < a.d; d0 += 128) {
+          const int d = d0 + 4 * lane;
+          float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int k0 = 0; k0 < a.cluster; k0 += 8) {
+            float4 z[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              if (d < a.d && (seen >> (k0 + k) & 1))
+                z[k] = ld_cluster_f32x4(mapa(smem_addr(joint + q * Sh::kD + d), k0 + k));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const float g = __shfl_sync(kFull, f, k0 + k);
+              if (d < a.d && (seen >> (k0 + k) & 1)) {
+                y.x += g * z[k].x;
+                y.y += g * z[k].y;
+                y.z += g * z[k].z;
+                y.w += g * z[k].w;
+              }
+            }
+          }
+          if (d < a.d)
+            *reinterpret_cast<uint2*>(a.out + row * a.d + d) =
+                make_uint2(pack_bf16(y.x * inverse, y.y * inverse),
+                           pack_bf16(y.z * inverse, y.w * inverse));
+        }
+        if (lane == 0 && a.lse) a.lse[row] = (top + log2f(total)) * kLn2;
+      }
+      cluster_sync();  // no CTA leaves while its results are read
     }
   }
   write_empty(a);

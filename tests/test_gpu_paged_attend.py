@@ -12,7 +12,7 @@ import paper_2609_23314_gb300 as vd
 from paged_ref import FILL, FP8, check_attend, raw
 from paper_2609_23314_gb300 import build
 
-pytestmark = pytest.mark.gpu
+pytestmark = [pytest.mark.gpu, pytest.mark.usefixtures("route")]
 BF = torch.bfloat16
 
 
@@ -24,6 +24,14 @@ def _lib():
     vd.vd_get_device_status()
     yield
     assert vd.vd_get_device_status() == 0
+
+
+@pytest.fixture(params=["automatic", "pieces"])
+def route(request, monkeypatch):
+    """The plan that the library takes, which for few units is a cluster for each, and again with
+    pieces of the line and the join."""
+    if request.param == "pieces":
+        monkeypatch.setenv("VD_PAGED_CLUSTER", "1")
 
 
 def queries(n, B, n_q, d, seed=0, size=1.0):
