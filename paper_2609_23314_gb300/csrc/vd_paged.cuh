@@ -36,6 +36,7 @@ struct Pages {
     record_status(status, kStDevicePage);
     return -1;
   }
+  // Offset of a slot's row of the first KV head.
   __device__ __forceinline__ long long row(int page, int slot) const {
     return page * page_stride + (slot - place_of(slot) * page_size) * slot_stride;
   }

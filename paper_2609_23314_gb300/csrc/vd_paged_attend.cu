@@ -225,7 +225,14 @@ vd_status vd_paged_attend(const vd_paged_cache* c, int32_t layer, const void* q,
   a.B = B;
   a.d = c->head_dim;
   a.rows = p.rows;
-  a.stage_keys = p.kernel->stage_keys;
+  auto log2 = [](int x) {
+    int e = 0;
+    while (1 << e < x) ++e;
+    return e;
+  };
+  a.row_shift = log2(p.rows);
+  a.stage_shift = log2(p.kernel->stage_keys);
+  a.cluster_shift = log2(p.cluster);
   a.causal = causal != 0;
   a.scale = scale;
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);

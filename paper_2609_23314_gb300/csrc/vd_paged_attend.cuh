@@ -2,7 +2,7 @@
 // include/vd.h): how the work is divided and its parts are joined.
 //
 // A unit is a sequence's KV head and a tile of `rows` query rows; it takes ceil(slots /
-// stage_keys) stages.  The units' stages, sequence after sequence, make one line that is cut
+// slots of a stage) stages.  The units' stages, sequence after sequence, make one line that is cut
 // into equal pieces, one for each CTA, whatever the lengths are: the lengths are on the device,
 // and a cut by them needs no plan on the host and leaves no CTA idle beside a long sequence.
 // A CTA that holds all stages of a unit writes its output.  Of the others it writes a part (sums
@@ -35,10 +35,10 @@ struct PagedAttendArgs {
   float2* stats;         // ... [2 CTAs][rows] references and sums of weights,
   float* parts;          // ... [2 CTAs][rows][d] sums
   int n_seq, heads, group, B, d;
-  int rows;              // of a tile
+  int rows;              // of a tile, a power of two
   int tiles;             // of B tokens
-  int cluster;           // CTAs that share a unit, or 1: pieces of the line
-  int stage_keys;        // slots of a stage
+  int cluster;           // CTAs that share a unit, a power of two, or 1: pieces of the line
+  int row_shift, stage_shift, cluster_shift;  // log2 of rows, of a stage's slots, of cluster
   int causal;
   float scale;
 };
@@ -57,8 +57,8 @@ struct SeqWork {
 __device__ __forceinline__ SeqWork seq_work(const PagedAttendArgs& a, int len, int add) {
   SeqWork w = {len, add, 0, 0, 0};
   w.total = add == 0 ? 0 : len + (a.causal ? add : 0);
-  w.tiles = (add * a.group + a.rows - 1) / a.rows;
-  w.stages = (w.total + a.stage_keys - 1) / a.stage_keys;
+  w.tiles = (add * a.group + a.rows - 1) >> a.row_shift;
+  w.stages = (w.total + (1 << a.stage_shift) - 1) >> a.stage_shift;
   return w;
 }
 
@@ -222,17 +222,18 @@ struct Walk {
 // The share of a CTA of a cluster, with no stage where there are fewer than CTAs; false: the unit
 // has nothing to do.
 __device__ __forceinline__ bool cluster_share(const PagedAttendArgs& a, Share& s) {
-  const int rank = blockIdx.x % a.cluster, unit = blockIdx.x / a.cluster;
-  s.tile = unit % a.tiles;
-  s.head = unit / a.tiles % a.heads;
-  s.seq = unit / a.tiles / a.heads;
+  const int rank = blockIdx.x & (a.cluster - 1), unit = blockIdx.x >> a.cluster_shift;
+  const int head = unit / a.tiles;
+  s.tile = unit - head * a.tiles;
+  s.seq = head / a.heads;
+  s.head = head - s.seq * a.heads;
   const int2 n = seq_size(a, s.seq, rank == 0 && s.tile == 0 && s.head == 0);
   const SeqWork w = seq_work(a, n.x, n.y);
   s.len = w.len;
   s.add = w.add;
   s.total = w.total;
-  s.s0 = (int)((long long)w.stages * rank / a.cluster);
-  s.s1 = (int)((long long)w.stages * (rank + 1) / a.cluster);
+  s.s0 = (int)((uint32_t)(w.stages * rank) >> a.cluster_shift);  // below 2^26 stages, 17 ranks
+  s.s1 = (int)((uint32_t)(w.stages * (rank + 1)) >> a.cluster_shift);
   s.slot = kOfCluster;
   return s.tile < w.tiles && w.total > 0;
 }

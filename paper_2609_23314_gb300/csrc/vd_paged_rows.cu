@@ -31,6 +31,10 @@ vd_status validate_paged(const vd_paged_cache* c) {
     if (extent[i] > 1 && stride[i] % unit != 0) aligned = false;
   }
   if (!aligned) return VD_ERR_ALIGNMENT;
+  // where a layer's rows lie is counted in 32 bits, 16 bytes each
+  double span = 0;
+  for (int i = 1; i < 4; ++i) span += (double)(extent[i] - 1) * (double)stride[i];
+  if (span / unit >= 4294967040.0) return VD_ERR_UNSUPPORTED;
   if (c->head_dim > 256 || (long long)c->page_size * c->max_pages > (1LL << 30) ||
       c->n_seq > (1 << 20) || c->n_kv_head > 65536 ||
       (long long)c->n_seq * c->n_kv_head > INT_MAX / c->n_layer)

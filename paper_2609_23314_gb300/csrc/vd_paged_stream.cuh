@@ -54,6 +54,28 @@ __device__ __forceinline__ void ldmatrix4_trans(uint32_t addr, uint32_t (&r)[4])
                : "memory");
 }
 
+// c += a b, 16 x 8 x 16; not volatile, so that products and loads are free to overlap.
+template <bool BF16>
+__device__ __forceinline__ void product16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0,
+                                          uint32_t b1) {
+  if (BF16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+        "{%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+        "{%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+
 template <int M, int NT, bool E4M3>
 struct StreamShape {
   static constexpr int kD = 32 * M;  // head_dim, rounded up
@@ -170,68 +192,66 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
   if (any) load_queries(fs);  // ahead of the copies, behind which they would wait
   __syncthreads();
 
-  // Copies: a stage's slots, one for each lane, and their pages are looked up one stage before
-  // the copies are issued
-  constexpr int kNoStage = -2;
+  // Copies.  A stage's slots, one for each lane, and their pages are looked up one stage before
+  // its copies are issued
+  constexpr int kNone = -2;
   struct Fetch {
-    int page, slot;  // slot -1: none, kNoStage: no copies at all
-    long long head;
+    int page;   // of the lane's slot; kNone: nothing there
+    int stage;  // kNone: no more
+    int head;
   };
   auto lookup = [&](Fetch& f) {
     while (any && fetched >= fs.s1) {
       any = ahead.next(a, mem.walk, fs);
-      if (any) fetched = fs.s0 + warp;
+      fetched = fs.s0 + warp;
     }
-    f.slot = kNoStage;
+    f.stage = kNone;
     if (!any) return;
-    f.slot = fetched * Sh::kKeys + (lane & (Sh::kKeys - 1));
-    f.page = -1;
-    if (f.slot < fs.total)
-      f.page = __ldcg(a.pages.table + (size_t)fs.seq * a.pages.max_pages + a.pages.place_of(f.slot));
-    else
-      f.slot = -1;
-    f.head = fs.head * a.pages.head_stride;
+    f.stage = fetched;
+    f.head = fs.head;
+    const int slot = fetched * Sh::kKeys + (lane & (Sh::kKeys - 1));
+    f.page = kNone;
+    if (slot < fs.total)
+      f.page = __ldcg(a.pages.table + (size_t)fs.seq * a.pages.max_pages + a.pages.place_of(slot));
     fetched += kW;
   };
-  const long long v_from_k = a.pages.v - a.pages.k;
+  constexpr uint32_t kNoRow = 0xffffffffu;
+  auto copy = [&](uint32_t dst, uint32_t row, int t, int ch) {
+    const bool real = row != kNoRow;
+    const size_t from = (size_t)(real ? row + ch : 0u) * 16;
+    const uint32_t to = dst + t * Sh::kRowBytes + ((ch ^ Sw::turn(t)) << 4);
+    cp_async16_or_zero(to, a.pages.k + from, real);
+    cp_async16_or_zero(to + Sh::kTileBytes, a.pages.v + from, real);
+  };
   auto fetch = [&](const Fetch& f, int at) {
-    if (f.slot != kNoStage) {
-      bool real = f.slot >= 0;
+    if (f.stage != kNone) {
+      bool real = f.page != kNone;
       if (real && (unsigned)f.page >= (unsigned)a.pages.n_page) {
         record_status(a.pages.status, kStDevicePage);
         real = false;
       }
-      const char* row = real ? a.pages.k + a.pages.row(f.page, f.slot) + f.head : nullptr;
+      const int slot = f.stage * Sh::kKeys + (lane & (Sh::kKeys - 1));
+      // where the lane's row lies, in 16 bytes
+      const uint32_t mine =
+          real ? (uint32_t)((a.pages.row(f.page, slot) + f.head * a.pages.head_stride) >> 4) : kNoRow;
       const uint32_t dst = ring + at * Sh::kStageBytes;
-      auto copy = [&](int t, int ch) {
-        const char* from = reinterpret_cast<const char*>(
-            __shfl_sync(kFull, reinterpret_cast<unsigned long long>(row), t));
-        const bool there = from != nullptr;
-        from = there ? from + ch * 16 : a.pages.k;
-        const uint32_t to = dst + t * Sh::kRowBytes + ((ch ^ Sw::turn(t)) << 4);
-        cp_async16_or_zero(to, from, there);
-        cp_async16_or_zero(to + Sh::kTileBytes, from + v_from_k, there);
-      };
       if (chunks == Sh::kChunks) {
+        constexpr int kCopies = Sh::kKeys * Sh::kChunks / 32;  // of K, and of V
+        uint32_t row[kCopies];
 #pragma unroll
-        for (int i = 0; i < Sh::kKeys * Sh::kChunks / 32; ++i) {
+        for (int i = 0; i < kCopies; ++i)
+          row[i] = __shfl_sync(kFull, mine, (32 * i + lane) / Sh::kChunks);
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
           const int at = 32 * i + lane;
-          copy(at / Sh::kChunks, at % Sh::kChunks);
+          copy(dst, row[i], at / Sh::kChunks, at % Sh::kChunks);
         }
       } else {
         // whole rows: a warp takes 32 / chunks of them at a time
         const int rows = 32 / chunks, t0 = lane / chunks, ch = lane - t0 * chunks;
         for (int t = t0; t - t0 < Sh::kKeys; t += rows) {
-          const bool on = t0 < rows && t < Sh::kKeys;
-          const char* from = reinterpret_cast<const char*>(__shfl_sync(
-              kFull, reinterpret_cast<unsigned long long>(row), t & (Sh::kKeys - 1)));
-          const bool there = from != nullptr;
-          from = there ? from + ch * 16 : a.pages.k;
-          const uint32_t to = dst + t * Sh::kRowBytes + ((ch ^ Sw::turn(t)) << 4);
-          if (on) {
-            cp_async16_or_zero(to, from, there);
-            cp_async16_or_zero(to + Sh::kTileBytes, from + v_from_k, there);
-          }
+          const uint32_t row = __shfl_sync(kFull, mine, t & (Sh::kKeys - 1));
+          if (t0 < rows && t < Sh::kKeys) copy(dst, row, t, ch);
         }
       }
     }
@@ -320,32 +340,46 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
       const uint32_t tile_k = ring + at * Sh::kStageBytes, tile_v = tile_k + Sh::kTileBytes;
       at = at + 1 == kS ? 0 : at + 1;
       const int key0 = stage * Sh::kKeys;
-      float x[kG][NT][4];
+      // Matrix loads go kBatch at a time ahead of their products; a query tile alone has two chains
+      // of sums, so that products wait less for one another
+      constexpr int kLoads = E4M3 ? M : 2 * M, kBatch = kLoads % 4 == 0 ? 4 : kLoads % 3 == 0 ? 3 : 2;
+      constexpr int kChains = NT == 1 ? 2 : 1;
+      float x[kG][NT][4], xs[kChains][kG][NT][4] = {};
 #pragma unroll
-      for (int g = 0; g < kG; ++g) {
+      for (int g = 0; g < kG; ++g)
+#pragma unroll
+        for (int j0 = 0; j0 < kLoads; j0 += kBatch) {
+          uint32_t w[kBatch][4];
+#pragma unroll
+          for (int j = 0; j < kBatch; ++j)
+            ldmatrix4(Sw::step(tile_k + k_lane, 2 * (j0 + j)) + 16 * g * Sh::kRowBytes, w[j]);
+#pragma unroll
+          for (int j = 0; j < kBatch; ++j) {
+            if (E4M3) {  // two chunks of 16 dims
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const uint32_t f[4] = {
+                    e4m3_to_h2(w[j][2 * h], false), e4m3_to_h2(w[j][2 * h + 1], false),
+                    e4m3_to_h2(w[j][2 * h], true), e4m3_to_h2(w[j][2 * h + 1], true)};
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+                  product16<false>(xs[h % kChains][g][t], f, qf[t][2 * (j0 + j) + h][0],
+                                   qf[t][2 * (j0 + j) + h][1]);
+              }
+            } else {
+#pragma unroll
+              for (int t = 0; t < NT; ++t)
+                product16<true>(xs[j % kChains][g][t], w[j], qf[t][j0 + j][0], qf[t][j0 + j][1]);
+            }
+          }
+        }
+#pragma unroll
+      for (int g = 0; g < kG; ++g)
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[g][t][e] = 0.f;
-#pragma unroll
-        for (int j = 0; j < (E4M3 ? M : 2 * M); ++j) {
-          uint32_t w[4];
-          ldmatrix4(Sw::step(tile_k + k_lane, 2 * j) + 16 * g * Sh::kRowBytes, w);
-          if (E4M3) {  // two chunks of 16 dims
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const uint32_t f[4] = {e4m3_to_h2(w[2 * h], false), e4m3_to_h2(w[2 * h + 1], false),
-                                     e4m3_to_h2(w[2 * h], true), e4m3_to_h2(w[2 * h + 1], true)};
-#pragma unroll
-              for (int t = 0; t < NT; ++t)
-                mma_16816<false>(x[g][t], f, qf[t][2 * j + h][0], qf[t][2 * j + h][1]);
-            }
-          } else {
-#pragma unroll
-            for (int t = 0; t < NT; ++t) mma_16816<true>(x[g][t], w, qf[t][j][0], qf[t][j][1]);
-          }
-        }
-      }
+          for (int e = 0; e < 4; ++e)
+            x[g][t][e] = kChains == 1 ? xs[0][g][t][e] : xs[0][g][t][e] + xs[kChains - 1][g][t][e];
       // Scores, rounded before the maximum is taken off them (a difference of the unrounded
       // product would be off by half a unit of the maximum), into the running state
       const bool hides = key0 + Sh::kKeys > all_see;
@@ -404,11 +438,11 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             if (E4M3) {
-              ph[g][t][h] = transpose_8x8(pack_f16(x[g][t][2 * h], x[g][t][2 * h + 1]));
+              ph[g][t][h] = transposed(pack_f16(x[g][t][2 * h], x[g][t][2 * h + 1]));
             } else {
               uint32_t low;
-              ph[g][t][h] = transpose_8x8(split_weights(x[g][t][2 * h], x[g][t][2 * h + 1], low));
-              pl[g][t][h] = transpose_8x8(low);
+              ph[g][t][h] = transposed(split_weights(x[g][t][2 * h], x[g][t][2 * h + 1], low));
+              pl[g][t][h] = transposed(low);
             }
           }
       }
@@ -416,27 +450,32 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
       // order (bf16), or dims 2 r for row r and 2 r + 1 for row r + 8
       auto values = [&](int g, auto&& use) {
 #pragma unroll
-        for (int j = 0; j < (E4M3 ? M : 2 * M); ++j) {
-          uint32_t w[4];
-          ldmatrix4_trans(Sw::step(tile_v + v_lane, 2 * j) + 16 * g * Sh::kRowBytes, w);
-          if (E4M3) {
+        for (int j0 = 0; j0 < kLoads; j0 += kBatch) {
+          uint32_t w[kBatch][4];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              // a word: dims 2 r, 2 r + 1 of slot 2 c, then of slot 2 c + 1
-              const uint32_t lo = __byte_perm(w[2 * h], 0, 0x3120),
-                             hi = __byte_perm(w[2 * h + 1], 0, 0x3120);
-              const uint32_t f[4] = {e4m3_to_h2(lo, false), e4m3_to_h2(lo, true),
-                                     e4m3_to_h2(hi, false), e4m3_to_h2(hi, true)};
-              use(2 * j + h, f);
+          for (int j = 0; j < kBatch; ++j)
+            ldmatrix4_trans(Sw::step(tile_v + v_lane, 2 * (j0 + j)) + 16 * g * Sh::kRowBytes, w[j]);
+#pragma unroll
+          for (int j = 0; j < kBatch; ++j) {
+            if (E4M3) {
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                // a word: dims 2 r, 2 r + 1 of slot 2 c, then of slot 2 c + 1
+                const uint32_t lo = __byte_perm(w[j][2 * h], 0, 0x3120),
+                               hi = __byte_perm(w[j][2 * h + 1], 0, 0x3120);
+                const uint32_t f[4] = {e4m3_to_h2(lo, false), e4m3_to_h2(lo, true),
+                                       e4m3_to_h2(hi, false), e4m3_to_h2(hi, true)};
+                use(2 * (j0 + j) + h, f);
+              }
+            } else {
+              use(j0 + j, w[j]);
             }
-          } else {
-            use(j, w);
           }
         }
       };
       auto product = [&](float (&y)[4], const uint32_t (&f)[4], int g, int t) {
-        mma_16816<!E4M3>(y, f, ph[g][t][0], ph[g][t][1]);
-        if (!E4M3) mma_16816<true>(y, f, pl[g][t][0], pl[g][t][1]);
+        product16<!E4M3>(y, f, ph[g][t][0], ph[g][t][1]);
+        if (!E4M3) product16<true>(y, f, pl[g][t][0], pl[g][t][1]);
       };
       // A value that is not finite must not reach the tokens that do not see its slot, whose
       // weight for it is 0: then the slots go one by one, to those that do.
