@@ -21,12 +21,12 @@ struct Pages {
   unsigned* status;
   long long page_stride, head_stride, slot_stride;
   int page_size, n_page, max_pages;
-  uint32_t per_page;  // 2^page_shift / page_size, rounded up
+  uint32_t per_page;  // 2^(30 + page_shift) / page_size, rounded up
   int page_shift;
 
-  // Exact for slots below 2^30.
+  // The place of a slot's page in the table, slot / page_size: exact for slots below 2^30.
   __device__ __forceinline__ int place_of(int slot) const {
-    return (int)(((uint64_t)(uint32_t)slot * per_page) >> page_shift);
+    return (int)(__umulhi((uint32_t)slot << 2, per_page) >> page_shift);
   }
   __device__ __forceinline__ int capacity() const { return page_size * max_pages; }
   // The page that holds a slot, -1 (recorded) if the table names none.
@@ -60,11 +60,11 @@ inline Pages pages_of(const vd_paged_cache* c, int layer, unsigned* status) {
   p.page_size = c->page_size;
   p.n_page = c->n_page;
   p.max_pages = c->max_pages;
-  // for slots n < 2^30: n / page_size = n per_page >> page_shift, as per_page page_size exceeds
-  // 2^page_shift by less than page_size <= 2^(page_shift - 30)
-  p.page_shift = 30;
-  while ((1LL << (p.page_shift - 30)) < c->page_size) ++p.page_shift;
-  p.per_page = (uint32_t)(((1ull << p.page_shift) + c->page_size - 1) / c->page_size);
+  // for slots n < 2^30: n / page_size = n per_page >> 30 + page_shift, as per_page page_size
+  // exceeds 2^(30 + page_shift) by less than page_size <= 2^page_shift
+  p.page_shift = 0;
+  while ((1LL << p.page_shift) < c->page_size) ++p.page_shift;
+  p.per_page = (uint32_t)(((1ull << (30 + p.page_shift)) + c->page_size - 1) / c->page_size);
   return p;
 }
 

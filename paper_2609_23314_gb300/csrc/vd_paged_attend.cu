@@ -230,6 +230,9 @@ vd_status vd_paged_attend(const vd_paged_cache* c, int32_t layer, const void* q,
     while (1 << e < x) ++e;
     return e;
   };
+  a.page16 = (uint32_t)(a.pages.page_stride >> 4);
+  a.slot16 = (uint32_t)(a.pages.slot_stride >> 4);
+  a.wait_limit = wait_limit();
   a.row_shift = log2(p.rows);
   a.stage_shift = log2(p.kernel->stage_keys);
   a.cluster_shift = log2(p.cluster);

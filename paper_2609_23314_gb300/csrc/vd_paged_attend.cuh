@@ -41,25 +41,33 @@ struct PagedAttendArgs {
   int row_shift, stage_shift, cluster_shift;  // log2 of rows, of a stage's slots, of cluster
   int causal;
   float scale;
+  uint32_t page16, slot16;  // strides of the pages in 16 bytes (where a layer's rows lie fits 32 bits)
+  uint32_t wait_limit;
 };
 
 constexpr float kLn2 = 0.69314718055994531f;
 
 // What a sequence has to do.
 struct SeqWork {
-  int len, add, total, tiles;  // slots, new tokens, slots that the last of them sees
-  int stages;                  // of a unit
-  __device__ __forceinline__ long long all(int heads) const {
-    return (long long)stages * tiles * heads;
-  }
+  int total, tiles;  // slots that its last token sees, tiles of its tokens
+  int stages;        // of a unit
 };
 
-__device__ __forceinline__ SeqWork seq_work(const PagedAttendArgs& a, int len, int add) {
-  SeqWork w = {len, add, 0, 0, 0};
-  w.total = add == 0 ? 0 : len + (a.causal ? add : 0);
-  w.tiles = (add * a.group + a.rows - 1) >> a.row_shift;
+// What a unit costs beside its stages, in stages of a CTA: its queries, the meeting of the warps.
+constexpr int kUnitCost = 8;
+
+__device__ __forceinline__ SeqWork seq_work(const PagedAttendArgs& a, int2 size) {
+  SeqWork w;
+  w.total = size.y == 0 ? 0 : size.x + (a.causal ? size.y : 0);
+  w.tiles = (size.y * a.group + a.rows - 1) >> a.row_shift;
   w.stages = (w.total + (1 << a.stage_shift) - 1) >> a.stage_shift;
   return w;
+}
+
+// The sequence's length on the line.
+__device__ __forceinline__ long long line_length(const PagedAttendArgs& a, int2 size) {
+  const SeqWork w = seq_work(a, size);
+  return w.stages == 0 ? 0 : (long long)(w.stages + kUnitCost) * w.tiles * a.heads;
 }
 
 // Length and new tokens of a sequence, none of which where they are out of range.
@@ -77,7 +85,7 @@ __device__ __forceinline__ long long divide(long long n, long long d) {
   return (unsigned long long)(n | d) >> 32 ? n / d : (long long)((uint32_t)n / (uint32_t)d);
 }
 
-// The line cut into `ctas` pieces: the first `more` have one stage more.
+// The line cut into `ctas` pieces: the first `more` are longer by one.
 struct Cut {
   long long per;
   int ctas, more;
@@ -94,130 +102,168 @@ struct Cut {
 constexpr int kWhole = -1, kOfCluster = -2;
 
 struct Share {
-  int seq, head, tile, s0, s1;
-  int len, add, total;  // of the sequence, as in SeqWork
+  int seq, head, tile, s0, s1;  // seq -1: no more
+  int len, add;                 // of the sequence
   int slot;  // of the part; kWhole: the whole unit, kOfCluster: a part of the cluster's unit
 };
 
-constexpr int kChunk = 64;  // sequences that are looked at together
+__device__ __forceinline__ long long warp_scan_i64(long long x) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const long long y = __shfl_up_sync(kFull, x, off);
+    if (lane >= off) x += y;
+  }
+  return x;
+}
 
+// Sequences that a warp looks at together, one a lane.
 struct WalkMem {
-  Cut cut;
-  long long end[kChunk];  // where each ends on the line
-  int2 size[kChunk];
-  long long sum[32];
+  int first;
+  long long end[32];  // where each ends on the line
+  int2 size[32];
+  // many sequences: of each warp of the CTA, and what they found
+  long long sum[16];
+  int found_seq;
+  long long found_at;
 };
 
-// Walks over a CTA's piece of the line.  All threads of the CTA construct it together; then each
-// warp may go its own way.
+// Walks over a CTA's piece of the line.  One warp constructs it, all of it; its first lane goes on.
 struct Walk {
-  long long at, end;  // line positions: the next stage, the piece's end
-  int chunk, seq, head, tile, stage;
-  SeqWork w;          // of seq
+  Cut cut;
+  long long at, end;  // line positions: the next one, the piece's end
+  int seq, head, tile, in;  // in: the next position in the unit
+  int2 size;                // of seq
 
-  __device__ Walk() : at(0), end(0) {}
-  // Pieces of `least` stages at least.
-  __device__ Walk(const PagedAttendArgs& a, WalkMem& m, int least)
-      : at(0), end(0), chunk(0), seq(0), head(0), tile(0), stage(0), w() {
-    load(a, m, 0, blockIdx.x == 0);
-    long long all = m.end[kChunk - 1];
-    if (a.n_seq > kChunk) {
-      long long mine = 0;
-      for (int s = kChunk + threadIdx.x; s < a.n_seq; s += blockDim.x) {
-        const int2 n = seq_size(a, s, blockIdx.x == 0);
-        mine += seq_work(a, n.x, n.y).all(a.heads);
-      }
-#pragma unroll
-      for (int off = 16; off > 0; off >>= 1) mine += __shfl_xor_sync(kFull, mine, off);
-      if ((threadIdx.x & 31) == 0) m.sum[threadIdx.x >> 5] = mine;
-      __syncthreads();
-      for (int i = 0; i < (int)blockDim.x / 32; ++i) all += m.sum[i];
+  // Where there are more than 32 sequences, all threads of the CTA come here first: the length
+  // of the line, and a sequence near the piece's first one.
+  static __device__ long long survey(const PagedAttendArgs& a, WalkMem& m) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int per = (a.n_seq + blockDim.x - 1) / blockDim.x, s0 = threadIdx.x * per,
+              s1 = min(a.n_seq, s0 + per);
+    long long mine = 0;
+    for (int s = s0; s < s1; ++s) mine += line_length(a, seq_size(a, s, blockIdx.x == 0));
+    const long long upto = warp_scan_i64(mine);
+    if (lane == 31) m.sum[warp] = upto;
+    __syncthreads();
+    long long before = upto - mine, all = 0;
+    for (int w = 0; w < warps; ++w) {
+      if (w < warp) before += m.sum[w];
+      all += m.sum[w];
     }
+    const Cut cut = cut_of(all);
+    const long long at = cut.begin(blockIdx.x);
+    if ((int)blockIdx.x < cut.ctas && before <= at && at < before + mine) {
+      m.found_seq = s0;
+      m.found_at = before;
+    }
+    __syncthreads();
+    return all;
+  }
+  // Pieces long enough that each has a stage wherever it begins.
+  static __device__ __forceinline__ Cut cut_of(long long all) {
     Cut cut;
-    const long long most = divide(all, least);
+    const long long most = all / (2 * kUnitCost);
     cut.ctas = most >= (long long)gridDim.x ? (int)gridDim.x : most > 1 ? (int)most : 1;
     cut.per = divide(all, cut.ctas);
     cut.more = (int)(all - cut.per * cut.ctas);
-    if (threadIdx.x == 0) m.cut = cut;
+    return cut;
+  }
+
+  __device__ Walk() : at(0), end(0) {}
+  __device__ Walk(const PagedAttendArgs& a, WalkMem& m, long long all)
+      : cut(), at(0), end(0), seq(0), head(0), tile(0), in(0), size() {
+    int first = 0;
+    long long begin = 0;
+    if (a.n_seq <= 32) {
+      load(a, m, 0, 0, blockIdx.x == 0);
+      all = m.end[31];
+    }
+    cut = cut_of(all);
     if ((int)blockIdx.x >= cut.ctas) return;
     at = cut.begin(blockIdx.x);
     end = cut.begin(blockIdx.x + 1);
     if (at >= end) return;
-    // the first sequence and the place in it
-    long long begin = 0, stop;
-    while ((stop = m.end[kChunk - 1]) <= at) {
-      begin = stop;
-      chunk += kChunk;
-      load(a, m, stop, false);
+    if (a.n_seq > 32) {
+      first = m.found_seq;
+      begin = m.found_at;
+      load(a, m, first, begin, false);
+      while (m.end[31] <= at) {
+        begin = m.end[31];
+        first += 32;
+        load(a, m, first, begin, false);
+      }
     }
-    const int lane = threadIdx.x & 31;
-    int done = 0;
-#pragma unroll
-    for (int i = 0; i < kChunk; i += 32)
-      done += __popc(__ballot_sync(kFull, m.end[i + lane] <= at));
+    const int done = __popc(__ballot_sync(kFull, m.end[threadIdx.x & 31] <= at));
     if (done > 0) begin = m.end[done - 1];
-    seq = chunk + done;
-    w = seq_work(a, m.size[done].x, m.size[done].y);
-    const int unit = (int)divide(at - begin, w.stages);
-    stage = (int)(at - begin - (long long)unit * w.stages);
+    seq = first + done;
+    size = m.size[done];
+    const SeqWork w = seq_work(a, size);
+    const int unit = (int)divide(at - begin, w.stages + kUnitCost);
+    in = (int)(at - begin - (long long)unit * (w.stages + kUnitCost));
     head = unit / w.tiles;
     tile = unit - head * w.tiles;
   }
-  // The ends of the chunk's sequences, the first of which begins at `begin`; by the first warp.
-  __device__ void load(const PagedAttendArgs& a, WalkMem& m, long long begin, bool report) {
-    __syncthreads();  // the last chunk's readers
-    if (threadIdx.x < 32) {
-      static_assert(kChunk == 64, "two sequences a lane");
-      const int i = 2 * threadIdx.x, s = chunk + i;
-      const int2 none = make_int2(0, 0), n0 = s < a.n_seq ? seq_size(a, s, report) : none,
-                 n1 = s + 1 < a.n_seq ? seq_size(a, s + 1, report) : none;
-      const long long x0 = seq_work(a, n0.x, n0.y).all(a.heads),
-                      x1 = seq_work(a, n1.x, n1.y).all(a.heads);
-      long long x = x0 + x1;
-#pragma unroll
-      for (int off = 1; off < 32; off <<= 1) {
-        const long long y = __shfl_up_sync(kFull, x, off);
-        if ((int)threadIdx.x >= off) x += y;
-      }
-      m.end[i] = begin + x - x1;
-      m.end[i + 1] = begin + x;
-      m.size[i] = n0;
-      m.size[i + 1] = n1;
-    }
-    __syncthreads();
+  // The warp's next 32 sequences, the first of which begins at `begin`.
+  static __device__ void load(const PagedAttendArgs& a, WalkMem& m, int first, long long begin,
+                              bool report) {
+    const int lane = threadIdx.x & 31, s = first + lane;
+    const int2 n = s < a.n_seq ? seq_size(a, s, report) : make_int2(0, 0);
+    const long long x = warp_scan_i64(line_length(a, n));
+    __syncwarp();
+    m.first = first;
+    m.end[lane] = begin + x;
+    m.size[lane] = n;
+    __syncwarp();
   }
-  // The next share, if there is one.
+  // The next share, if there is one; by one thread.
   __device__ bool next(const PagedAttendArgs& a, const WalkMem& m, Share& s) {
-    if (at >= end) return false;
-    s.seq = seq;
-    s.head = head;
-    s.tile = tile;
-    s.len = w.len;
-    s.add = w.add;
-    s.total = w.total;
-    const int n = end - at < w.stages - stage ? (int)(end - at) : w.stages - stage;
-    s.s0 = stage;
-    s.s1 = stage += n;
-    at += n;
-    // a CTA's first share may begin inside a unit, its last one may end there
-    s.slot = n == w.stages ? kWhole : 2 * (int)blockIdx.x + (s.s0 == 0 ? 1 : 0);
-    if (stage == w.stages) {
-      stage = 0;
-      if (++tile == w.tiles) {
-        tile = 0;
-        if (++head == a.heads) {
-          head = 0;
-          if (at < end) do {
-              ++seq;
-              const int2 n = seq - chunk < kChunk ? m.size[seq - chunk] : seq_size(a, seq, false);
-              w = seq_work(a, n.x, n.y);
-            } while (w.all(a.heads) == 0);
+    while (at < end) {
+      SeqWork w = seq_work(a, size);
+      const int length = w.stages + kUnitCost;
+      const int n = end - at < length - in ? (int)(end - at) : length - in;
+      s.seq = seq;
+      s.head = head;
+      s.tile = tile;
+      s.len = size.x;
+      s.add = size.y;
+      s.s0 = max(0, in - kUnitCost);
+      s.s1 = max(0, in + n - kUnitCost);
+      // a CTA's first share may begin inside a unit, its last one may end there
+      s.slot = s.s1 - s.s0 == w.stages ? kWhole : 2 * (int)blockIdx.x + (s.s0 == 0 ? 1 : 0);
+      in += n;
+      at += n;
+      if (in == length) {
+        in = 0;
+        if (++tile == w.tiles) {
+          tile = 0;
+          if (++head == a.heads) {
+            head = 0;
+            if (at < end) do {
+                ++seq;
+                size = seq - m.first < 32 ? m.size[seq - m.first] : seq_size(a, seq, false);
+                w = seq_work(a, size);
+              } while (w.stages == 0);
+          }
         }
       }
+      if (s.s1 > s.s0) return true;
     }
-    return true;
+    return false;
+  }
+  // What the join has to know of a unit that the last share began and did not end.
+  __device__ int4 split_of(const PagedAttendArgs& a, const Share& s) const {
+    const int row0 = s.tile * a.rows;
+    const int left = seq_work(a, make_int2(s.len, s.add)).stages - s.s1;
+    return make_int4((s.seq * a.B * a.heads + s.head) * a.group, row0,
+                     min(a.rows, s.add * a.group - row0), cut.holder(at + left - 1));
   }
 };
+
+// The slots that the sequence's last token sees.
+__device__ __forceinline__ int seen_slots(const PagedAttendArgs& a, const Share& s) {
+  return s.len + (a.causal ? s.add : 0);
+}
 
 // The share of a CTA of a cluster, with no stage where there are fewer than CTAs; false: the unit
 // has nothing to do.
@@ -228,23 +274,13 @@ __device__ __forceinline__ bool cluster_share(const PagedAttendArgs& a, Share& s
   s.seq = head / a.heads;
   s.head = head - s.seq * a.heads;
   const int2 n = seq_size(a, s.seq, rank == 0 && s.tile == 0 && s.head == 0);
-  const SeqWork w = seq_work(a, n.x, n.y);
-  s.len = w.len;
-  s.add = w.add;
-  s.total = w.total;
+  const SeqWork w = seq_work(a, n);
+  s.len = n.x;
+  s.add = n.y;
   s.s0 = (int)((uint32_t)(w.stages * rank) >> a.cluster_shift);  // below 2^26 stages, 17 ranks
   s.s1 = (int)((uint32_t)(w.stages * (rank + 1)) >> a.cluster_shift);
   s.slot = kOfCluster;
   return s.tile < w.tiles && w.total > 0;
-}
-
-// What the join has to know of such a unit; `at`: the line's position behind the share.
-__device__ __forceinline__ int4 split_of(const PagedAttendArgs& a, const Cut& cut, const Share& s,
-                                         long long at) {
-  const int row0 = s.tile * a.rows;
-  const int left = seq_work(a, s.len, s.add).stages - s.s1;
-  return make_int4((s.seq * a.B * a.heads + s.head) * a.group, row0,
-                   min(a.rows, s.add * a.group - row0), cut.holder(at + left - 1));
 }
 
 // Where a tile's row lies: out and q at row * d, lse at row.  -1: no such row.
@@ -258,10 +294,9 @@ __device__ __forceinline__ long long out_row(const PagedAttendArgs& a, const Sha
 __device__ __forceinline__ void write_empty(const PagedAttendArgs& a) {
   for (int s = blockIdx.x; s < a.n_seq; s += gridDim.x) {
     const int2 n = seq_size(a, s, false);
-    const SeqWork w = seq_work(a, n.x, n.y);
-    if (w.add == 0 || w.total > 0) continue;
+    if (n.y == 0 || seq_work(a, n).total > 0) continue;
     const long long row0 = (long long)s * a.B * a.heads * a.group;
-    const long long rows = (long long)w.add * a.heads * a.group;
+    const long long rows = (long long)n.y * a.heads * a.group;
     const int chunks = a.d / 8;
     for (long long i = threadIdx.x; i < rows * chunks; i += blockDim.x)
       st16(a.out + row0 * a.d + i * 8, make_uint4(0, 0, 0, 0));

@@ -4,9 +4,12 @@
 //   s_ij = scale * q_i . k_j,  o_i = sum_j exp(s_ij - m_i) v_j / sum_j exp(s_ij - m_i)
 //
 // in one pass over the slots with a running maximum and sum.  A CTA takes its piece of the line
-// (vd_paged_attend.cuh); its warps take a share's stages in turn, each with its own
-// ring of asynchronous copies and its own running state, so that warps wait for nothing but their
-// copies, and meet at the end of the share.  The copies run ahead into the next shares.
+// (vd_paged_attend.cuh), a share of a unit at a time, in stages of 16 or 32 slots that go around a
+// ring in shared memory.  Four warps copy: each looks up the pages of its stages, four of them
+// ahead, and issues single asynchronous copies of 16 bytes, so that pages may be of any size and
+// stride; one of the four also finds the shares.  The other warps compute, a stage each in turn
+// with a running state of its own, meet in shared memory at the end of a share, and wait for
+// nothing but their stages there: a warp that is done goes on to the next share.
 //
 // Per 16 slots a warp computes  S^T = K Q^T  and  O^T += V^T P^T  with slots and head dims on the
 // 16-row side of m16n8k16, so that 8 query rows fill a tile.  bf16 pages are multiplied as
@@ -24,14 +27,6 @@
 #include "vd_paged_attend.cuh"
 
 namespace vd {
-
-// Where the CTA's warps are: they take a share together, while each one's copies run ahead.
-struct StreamMem {
-  WalkMem walk;
-  Walk at;
-  Share share[2];
-  int more[2];
-};
 
 // 16 bytes to shared memory, or zeros.
 __device__ __forceinline__ void cp_async16_or_zero(uint32_t smem, const void* p, bool real) {
@@ -76,6 +71,52 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   return r;
 }
 
+// Arrives on the barrier once this thread's copies so far have landed.
+__device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ bool bar_done(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; "
+      "selp.u32 %0, 1, 0, p; }"
+      : "=r"(done)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return done != 0;
+}
+
+// Waits for a phase; gives up after `limit` polls, and once another warp has.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* dead,
+                                         const PagedAttendArgs& a) {
+  if (bar_done(bar, parity)) return true;
+#pragma unroll 1
+  for (uint32_t i = 0; i < a.wait_limit; ++i) {
+    if (bar_done(bar, parity)) return true;
+    if (*dead) return false;
+  }
+  *dead = 1;
+  record_status(a.pages.status, kStTimeout);
+  return false;
+}
+
+constexpr int kShares = 4;     // shares in shared memory: the copies run ahead
+
+template <int NB>
+struct StreamMem {
+  uint64_t full[NB], empty[NB];      // the ring's places
+  uint64_t share_full[kShares], share_free[kShares];
+  uint64_t parts_full, parts_free;   // partial rows
+  Share share[kShares];
+  WalkMem walk;
+  int dead;  // a wait has run out
+};
+
 template <int M, int NT, bool E4M3>
 struct StreamShape {
   static constexpr int kD = 32 * M;  // head_dim, rounded up
@@ -86,17 +127,21 @@ struct StreamShape {
   static constexpr int kKeys = 16 * kGroups;
   static constexpr int kTileBytes = kKeys * kRowBytes;  // of K or V
   static constexpr int kStageBytes = 2 * kTileBytes;
-  static constexpr int kStreamWarps = M <= 4 ? 8 : 4;
-  static constexpr int kStreamThreads = 32 * kStreamWarps;
-  static constexpr int kStages =
-      E4M3 ? (M == 2 ? 5 : M == 3 || M == 8 ? 4 : M == 4 ? 3 : 6) : (M == 3 || M == 6 ? 4 : 3);
-  static constexpr int kRing = kStreamWarps * kStages * kStageBytes;
+  // Warps that compute and that copy: 12, of 168 registers each, or 8 where the sums take more
+  static constexpr bool kWide = M > 4 || M * NT > 6;
+  static constexpr int kWarpsUsed = !kWide ? 8 : M == 4 ? 6 : 4;
+  static constexpr int kProducers = kWide && M == 4 ? 2 : 4;
+  static constexpr int kStreamThreads = 32 * (kWarpsUsed + kProducers);
+  static constexpr int kMost = 192 * 1024 / kStageBytes;
+  static constexpr int kPlaces = (kMost > 32 ? 32 : kMost) / kWarpsUsed * kWarpsUsed;  // of the ring
+  static constexpr int kRing = kPlaces * kStageBytes;
   static constexpr int kPart = kD + 4;  // floats of a partial row
   static constexpr int kParts = kRing;  // [warp][8 rows]
-  static constexpr int kStats = kParts + kStreamWarps * 8 * kPart * 4;  // [warp][8 rows] max, sum
-  static constexpr int kMem = kStats + kStreamWarps * 8 * 8;
-  static constexpr int kTotal = kMem + (int)sizeof(StreamMem);
+  static constexpr int kStats = kParts + kWarpsUsed * 8 * kPart * 4;  // [warp][8 rows] max, sum
+  static constexpr int kMem = kStats + kWarpsUsed * 8 * 8;
+  static constexpr int kTotal = kMem + (int)sizeof(StreamMem<kPlaces>);
   static_assert(kTotal <= 232448, "shared memory");
+  static_assert(kPlaces % kProducers == 0, "a place has one producer and one consumer");
 };
 
 // Chunk c (16 bytes) of a row lies at c ^ turn(row), so that the same chunk of 8 rows falls on
@@ -137,146 +182,190 @@ __device__ __forceinline__ uint32_t split_weights(float x, float y, uint32_t& lo
 
 template <int M, int NT, bool E4M3>
 __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
-    paged_stream_kernel(PagedAttendArgs a) {
+    paged_stream_kernel(const __grid_constant__ PagedAttendArgs a) {
   using Sh = StreamShape<M, NT, E4M3>;
   using Sw = Swizzle<Sh::kChunks>;
-  constexpr int kW = Sh::kStreamWarps, kS = Sh::kStages, kG = Sh::kGroups;
+  constexpr int kW = Sh::kWarpsUsed, kN = Sh::kPlaces, kG = Sh::kGroups;
+  constexpr int kProducers = Sh::kProducers;
   extern __shared__ __align__(128) unsigned char smem[];
   const uint32_t base = smem_addr(smem);
-  float* parts = reinterpret_cast<float*>(smem + Sh::kParts);
-  float2* stats = reinterpret_cast<float2*>(smem + Sh::kStats);
+  auto& mem = *reinterpret_cast<StreamMem<kN>*>(smem + Sh::kMem);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int r = lane >> 2, c = lane & 3;
   const int chunks = a.d * (E4M3 ? 1 : 2) / 16;  // of a row in the pages
-  const uint32_t ring = base + warp * kS * Sh::kStageBytes;
+  if (threadIdx.x < kN) {
+    mbar_init(smem_addr(&mem.full[threadIdx.x]), 32);
+    mbar_init(smem_addr(&mem.empty[threadIdx.x]), 1);
+  } else if (threadIdx.x < kN + kShares) {
+    mbar_init(smem_addr(&mem.share_full[threadIdx.x - kN]), 1);
+    mbar_init(smem_addr(&mem.share_free[threadIdx.x - kN]), kW + kProducers - 1);
+  } else if (threadIdx.x == kN + kShares) {
+    mbar_init(smem_addr(&mem.parts_full), kW);
+    mbar_init(smem_addr(&mem.parts_free), kW);
+    mem.dead = 0;
+    mem.share[0].seq = -1;
+  }
+  fence_mbar_init();
   // what copies do not write: the chunks behind head_dim
   if (chunks < Sh::kChunks)
-    for (int i = lane; i < kS * Sh::kStageBytes / 16; i += 32)
-      st_shared16(ring + 16 * i, make_uint4(0, 0, 0, 0));
+    for (int i = threadIdx.x; i < Sh::kRing / 16; i += Sh::kStreamThreads)
+      st_shared16(base + 16 * i, make_uint4(0, 0, 0, 0));
   grid_dependency_wait();
   grid_launch_dependents();
-  StreamMem& mem = *reinterpret_cast<StreamMem*>(smem + Sh::kMem);
-  Walk ahead;
-  Share fs;  // the share whose stages are being fetched
-  bool any;
-  if (a.cluster > 1) {
-    any = cluster_share(a, fs);
-  } else {
-    ahead = Walk(a, mem.walk, kW);
-    any = ahead.next(a, mem.walk, fs);
-  }
-  if (threadIdx.x == 0) {
-    if (a.cluster == 1) a.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
-    mem.at = ahead;
-    mem.more[0] = any;
-    mem.share[0] = fs;
-  }
-  int fetched = fs.s0 + warp;  // the next stage of fs to look up
-
-  // Q: lane (r, c) holds row r of each n-tile
-  uint32_t qf[NT][2 * M][2];
-  auto load_queries = [&](const Share& s) {
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const long long row = out_row(a, s, 8 * t + r);
-      const uint32_t* src = reinterpret_cast<const uint32_t*>(a.q + (row < 0 ? 0 : row) * a.d);
-#pragma unroll
-      for (int j = 0; j < 2 * M; ++j) {
-        // e4m3: chunk j's dims 4 c .. 4 c + 3; bf16: chunks 2 j and 2 j + 1, dims 2 c, 2 c + 1
-        const int d0 = 16 * j + (E4M3 ? 4 : 2) * c, d1 = E4M3 ? d0 + 2 : d0 + 8;
-        qf[t][j][0] = row >= 0 && d0 < a.d ? __ldcg(src + d0 / 2) : 0u;
-        qf[t][j][1] = row >= 0 && d1 < a.d ? __ldcg(src + d1 / 2) : 0u;
-      }
-    }
-  };
-  if (any) load_queries(fs);  // ahead of the copies, behind which they would wait
+  long long all = 0;
+  if (a.cluster == 1 && a.n_seq > 32) all = Walk::survey(a, mem.walk);
   __syncthreads();
+  bool ok = true;
 
-  // Copies.  A stage's slots, one for each lane, and their pages are looked up one stage before
-  // its copies are issued
-  constexpr int kNone = -2;
-  struct Fetch {
-    int page;   // of the lane's slot; kNone: nothing there
-    int stage;  // kNone: no more
-    int head;
-  };
-  auto lookup = [&](Fetch& f) {
-    while (any && fetched >= fs.s1) {
-      any = ahead.next(a, mem.walk, fs);
-      fetched = fs.s0 + warp;
+  if (warp >= kW) {
+    // ------------------------------------------------------------------ copies
+    const int p = warp - kW;
+    Walk walk;
+    if (p == 0 && a.cluster == 1) {
+      walk = Walk(a, mem.walk, all);
+      if (lane == 0) a.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
     }
-    f.stage = kNone;
-    if (!any) return;
-    f.stage = fetched;
-    f.head = fs.head;
-    const int slot = fetched * Sh::kKeys + (lane & (Sh::kKeys - 1));
-    f.page = kNone;
-    if (slot < fs.total)
-      f.page = __ldcg(a.pages.table + (size_t)fs.seq * a.pages.max_pages + a.pages.place_of(slot));
-    fetched += kW;
-  };
-  constexpr uint32_t kNoRow = 0xffffffffu;
-  auto copy = [&](uint32_t dst, uint32_t row, int t, int ch) {
-    const bool real = row != kNoRow;
-    const size_t from = (size_t)(real ? row + ch : 0u) * 16;
-    const uint32_t to = dst + t * Sh::kRowBytes + ((ch ^ Sw::turn(t)) << 4);
-    cp_async16_or_zero(to, a.pages.k + from, real);
-    cp_async16_or_zero(to + Sh::kTileBytes, a.pages.v + from, real);
-  };
-  auto fetch = [&](const Fetch& f, int at) {
-    if (f.stage != kNone) {
-      bool real = f.page != kNone;
-      if (real && (unsigned)f.page >= (unsigned)a.pages.n_page) {
-        record_status(a.pages.status, kStDevicePage);
-        real = false;
-      }
-      const int slot = f.stage * Sh::kKeys + (lane & (Sh::kKeys - 1));
-      // where the lane's row lies, in 16 bytes
-      const uint32_t mine =
-          real ? (uint32_t)((a.pages.row(f.page, slot) + f.head * a.pages.head_stride) >> 4) : kNoRow;
-      const uint32_t dst = ring + at * Sh::kStageBytes;
-      if (chunks == Sh::kChunks) {
-        constexpr int kCopies = Sh::kKeys * Sh::kChunks / 32;  // of K, and of V
-        uint32_t row[kCopies];
-#pragma unroll
-        for (int i = 0; i < kCopies; ++i)
-          row[i] = __shfl_sync(kFull, mine, (32 * i + lane) / Sh::kChunks);
-#pragma unroll
-        for (int i = 0; i < kCopies; ++i) {
-          const int at = 32 * i + lane;
-          copy(dst, row[i], at / Sh::kChunks, at % Sh::kChunks);
+    int next = p;         // this warp's next stage, from the share's first one
+    int place = p;        // of the ring
+    uint32_t round = 0;   // how often the ring has gone around
+    constexpr bool kFixed = 32 % Sh::kChunks == 0;  // a lane has the same chunk of every row
+    for (int k = 0; ok; ++k) {
+      Share& s = mem.share[k % kShares];
+      const uint32_t turn = (uint32_t)(k / kShares);
+      if (p == 0) {
+        if (turn > 0) ok = bar_wait(smem_addr(&mem.share_free[k % kShares]), (turn - 1) & 1, &mem.dead, a);
+        if (lane == 0) {
+          const bool more = a.cluster > 1 ? k == 0 && cluster_share(a, s) : walk.next(a, mem.walk, s);
+          if (!more) s.seq = -1;
+          else if (s.slot >= 0 && s.s0 == 0) a.split[blockIdx.x] = walk.split_of(a, s);
+          bar_arrive(smem_addr(&mem.share_full[k % kShares]));
         }
-      } else {
-        // whole rows: a warp takes 32 / chunks of them at a time
-        const int rows = 32 / chunks, t0 = lane / chunks, ch = lane - t0 * chunks;
-        for (int t = t0; t - t0 < Sh::kKeys; t += rows) {
-          const uint32_t row = __shfl_sync(kFull, mine, t & (Sh::kKeys - 1));
-          if (t0 < rows && t < Sh::kKeys) copy(dst, row, t, ch);
-        }
+        __syncwarp();
       }
+      ok = ok && bar_wait(smem_addr(&mem.share_full[k % kShares]), turn & 1, &mem.dead, a);
+      if (!ok || s.seq < 0) break;
+      const int s0 = s.s0, count = s.s1 - s.s0, total = seen_slots(a, s);
+      const int32_t* table = a.pages.table + (size_t)s.seq * a.pages.max_pages;
+      const long long in = s.head * a.pages.head_stride + (kFixed ? lane % Sh::kChunks * 16 : 0);
+      const char *k_head = a.pages.k + in, *v_head = a.pages.v + in;
+      if (p > 0) {
+        __syncwarp();
+        if (lane == 0) bar_arrive(smem_addr(&mem.share_free[k % kShares]));
+      }
+      // Pages of the lane's slots: kNone behind the last slot
+      constexpr int kAhead = 4, kNone = -2;
+      auto lookup = [&](int i) {
+        const int slot = (s0 + i) * Sh::kKeys + (lane & (Sh::kKeys - 1));
+        return i < count && slot < total ? __ldcg(table + a.pages.place_of(slot)) : kNone;
+      };
+      int page[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) page[u] = lookup(next + u * kProducers);
+      while (ok && next < count) {
+        int later[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) later[u] = lookup(next + (kAhead + u) * kProducers);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          if (next >= count || !ok) break;
+          if (round > 0) {
+            ok = bar_wait(smem_addr(&mem.empty[place]), (round - 1) & 1, &mem.dead, a);
+            if (!ok) break;
+          }
+          bool real = page[u] != kNone;
+          if (real && (unsigned)page[u] >= (unsigned)a.pages.n_page) {
+            record_status(a.pages.status, kStDevicePage);
+            real = false;
+          }
+          // where the lane's row lies, in 16 bytes
+          const int slot = (s0 + next) * Sh::kKeys + (lane & (Sh::kKeys - 1));
+          const uint32_t mine = (uint32_t)page[u] * a.page16 +
+                                (uint32_t)(slot - a.pages.place_of(slot) * a.pages.page_size) * a.slot16;
+          const uint32_t dst = base + place * Sh::kStageBytes;
+          if (chunks == Sh::kChunks && __all_sync(kFull, real)) {
+            constexpr int kCopies = Sh::kKeys * Sh::kChunks / 32;  // of K, and of V
+            uint32_t row[kCopies];
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i)
+              row[i] = __shfl_sync(kFull, mine, (32 * i + lane) / Sh::kChunks);
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) {
+              const int t = (32 * i + lane) / Sh::kChunks, ch = (32 * i + lane) % Sh::kChunks;
+              const uint32_t to = dst + t * Sh::kRowBytes + ((ch ^ Sw::turn(t)) << 4);
+              const size_t from = (size_t)(row[i] + (kFixed ? 0 : ch)) * 16;
+              cp_async16(to, k_head + from);
+              cp_async16(to + Sh::kTileBytes, v_head + from);
+            }
+          } else {
+            // whole rows: a warp takes 32 / chunks of them at a time
+            const int rows = 32 / chunks, t0 = lane / chunks, ch = lane - t0 * chunks;
+            const int skip = kFixed ? ch - lane % Sh::kChunks : ch;
+            const unsigned reals = __ballot_sync(kFull, real);
+            for (int t = t0; t - t0 < Sh::kKeys; t += rows) {
+              const uint32_t row = __shfl_sync(kFull, mine, t & (Sh::kKeys - 1));
+              if (t0 < rows && t < Sh::kKeys) {
+                const bool there = reals >> t & 1;
+                const uint32_t to = dst + t * Sh::kRowBytes + ((ch ^ Sw::turn(t)) << 4);
+                const long long from = there ? ((long long)row + skip) * 16 : 0;
+                cp_async16_or_zero(to, k_head + from, there);
+                cp_async16_or_zero(to + Sh::kTileBytes, v_head + from, there);
+              }
+            }
+          }
+          cp_async_arrive(smem_addr(&mem.full[place]));
+          next += kProducers;
+          place += kProducers;
+          if (place >= kN) {
+            place -= kN;
+            ++round;
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) page[u] = later[u];
+      }
+      next -= count;
     }
     cp_async_commit();
-  };
-  Fetch pending;
-  {
-    Fetch f[kS - 1];
+    cp_async_wait<0>();
+  } else {
+    // ------------------------------------------------------------------ products
+    float* parts = reinterpret_cast<float*>(smem + Sh::kParts);
+    float2* stats = reinterpret_cast<float2*>(smem + Sh::kStats);
+    const int r = lane >> 2, c = lane & 3;
+    // Q: lane (r, c) holds row r of each n-tile
+    uint32_t qf[NT][2 * M][2];
+    auto load_queries = [&](const Share& s) {
 #pragma unroll
-    for (int i = 0; i < kS - 1; ++i) lookup(f[i]);
-    lookup(pending);
+      for (int t = 0; t < NT; ++t) {
+        const long long row = out_row(a, s, 8 * t + r);
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(a.q + (row < 0 ? 0 : row) * a.d);
 #pragma unroll
-    for (int i = 0; i < kS - 1; ++i) fetch(f[i], i);
-  }
-
+        for (int j = 0; j < 2 * M; ++j) {
+          // e4m3: chunk j's dims 4 c .. 4 c + 3; bf16: chunks 2 j and 2 j + 1, dims 2 c, 2 c + 1
+          const int d0 = 16 * j + (E4M3 ? 4 : 2) * c, d1 = E4M3 ? d0 + 2 : d0 + 8;
+          qf[t][j][0] = row >= 0 && d0 < a.d ? __ldcg(src + d0 / 2) : 0u;
+          qf[t][j][1] = row >= 0 && d1 < a.d ? __ldcg(src + d1 / 2) : 0u;
+        }
+      }
+    };
+    auto share_known = [&](int k) {
+      ok = ok && bar_wait(smem_addr(&mem.share_full[k % kShares]), k / kShares & 1, &mem.dead, a);
+      return ok && mem.share[k % kShares].seq >= 0;
+    };
   // Where a lane's row of the four 8 x 8 blocks of a matrix load lies in a tile: blocks of K are
   // slots 0-7, 8-15 of a chunk, then of the next one; of V in bf16, chunks go first
   const int slots8 = lane & 7, b3 = (lane >> 3) & 1, b4 = lane >> 4;
   const int k_slot = slots8 + 8 * b3, v_slot = slots8 + 8 * (E4M3 ? b3 : b4);
   const uint32_t k_lane = k_slot * Sh::kRowBytes + ((b4 ^ Sw::turn(k_slot)) << 4);
   const uint32_t v_lane = v_slot * Sh::kRowBytes + (((E4M3 ? b4 : b3) ^ Sw::turn(v_slot)) << 4);
-  int at = 0;  // the ring's place of the next stage
-  for (int turn = 0; mem.more[turn & 1]; ++turn) {
-    const Share& s = mem.share[turn & 1];
-    const int s1 = s.s1, len = s.len;
+  int next = warp;     // this warp's next stage, from the share's first one
+  int place = warp;    // of the ring
+  uint32_t phase = 0;  // of its barriers
+  uint32_t met = 0;    // times that the warps have met
+  bool more = share_known(0);
+  if (more) load_queries(mem.share[0]);
+  for (int k = 0; more; ++k) {
+    const Share& s = mem.share[k % kShares];
+    const int s0 = s.s0, count = s.s1 - s.s0, len = s.len;
     int sees[NT][2];  // slots that columns 2 c and 2 c + 1 see
     float qs[NT][2];  // what their scores are multiplied by for log2 units
     const int all_see = a.causal ? len + (s.tile * Sh::kRows) / a.group + 1 : len;
@@ -329,17 +418,12 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
         for (int e = 0; e < 4; ++e) o[t][i][e] = 0.f;
     }
 
-    for (int stage = s.s0 + warp; stage < s1; stage += kW) {
-      cp_async_wait<kS - 2>();
-      __syncwarp();
-      {
-        const Fetch f = pending;
-        lookup(pending);
-        fetch(f, at == 0 ? kS - 1 : at - 1);
-      }
-      const uint32_t tile_k = ring + at * Sh::kStageBytes, tile_v = tile_k + Sh::kTileBytes;
-      at = at + 1 == kS ? 0 : at + 1;
-      const int key0 = stage * Sh::kKeys;
+    const bool idle = next >= count;
+    for (; next < count; next += kW) {
+      ok = ok && bar_wait(smem_addr(&mem.full[place]), phase, &mem.dead, a);
+      if (!ok) break;
+      const uint32_t tile_k = base + place * Sh::kStageBytes, tile_v = tile_k + Sh::kTileBytes;
+      const int key0 = (s0 + next) * Sh::kKeys;
       // Matrix loads go kBatch at a time ahead of their products; a query tile alone has two chains
       // of sums, so that products wait less for one another
       constexpr int kLoads = E4M3 ? M : 2 * M, kBatch = kLoads % 4 == 0 ? 4 : kLoads % 3 == 0 ? 3 : 2;
@@ -517,15 +601,19 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
         }
       }
       __syncwarp();
+      if (lane == 0) bar_arrive(smem_addr(&mem.empty[place]));
+      place += kW;
+      if (place >= kN) {
+        place -= kN;
+        phase ^= 1;
+      }
     }
+    next -= count;
+    if (!ok) break;
+    // the next share's queries come while the warps meet
+    more = share_known(k + 1);
+    if (more) load_queries(mem.share[(k + 1) % kShares]);
 
-    // The warps meet
-    if (threadIdx.x == 32 * (kW - 1)) {
-      const int i = (turn + 1) & 1;
-      if (s.slot >= 0 && s.s0 == 0)
-        a.split[blockIdx.x] = split_of(a, mem.walk.cut, s, mem.at.at);
-      mem.more[i] = mem.at.next(a, mem.walk, mem.share[i]);
-    }
     const bool whole = s.slot == kWhole;
     float* joint = reinterpret_cast<float*>(smem);  // of a cluster: [row][kD], [row] max, sum
     float2* joint_stats = reinterpret_cast<float2*>(joint + Sh::kRows * Sh::kD);
@@ -538,10 +626,13 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
         // all scores NaN: so is the result
         if (sum[t][e] != sum[t][e] && mx[t][e] == -INFINITY) mx[t][e] = 0.f;
       }
+      // where the rows of the last meeting have been read
+      if (met > 0) ok = ok && bar_wait(smem_addr(&mem.parts_free), (met - 1) & 1, &mem.dead, a);
       float* mine = parts + warp * 8 * Sh::kPart;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         float* row = mine + (2 * c + e) * Sh::kPart;
+        if (!idle)
 #pragma unroll
         for (int i = 0; i < 2 * M; ++i) {
           if (E4M3) {
@@ -553,12 +644,13 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
         }
         if (r == 0) stats[warp * 8 + 2 * c + e] = make_float2(mx[t][e], sum[t][e]);
       }
-      __syncthreads();
-      if (t == 0 && mem.more[(turn + 1) & 1]) load_queries(mem.share[(turn + 1) & 1]);
+      __syncwarp();
+      if (lane == 0) bar_arrive(smem_addr(&mem.parts_full));
 #pragma unroll 1
       for (int q = warp; q < 8; q += kW) {
         const long long row = out_row(a, s, 8 * t + q);
         if (row < 0) continue;
+        ok = ok && bar_wait(smem_addr(&mem.parts_full), met & 1, &mem.dead, a);
         float top = -INFINITY, total = 0.f, f[kW];
 #pragma unroll
         for (int w = 0; w < kW; ++w) top = fmaxf(top, stats[w * 8 + q].x);
@@ -597,10 +689,21 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
             a.lse[row] = (top + log2f(total)) * kLn2;
         }
       }
-      __syncthreads();
+      __syncwarp();
+      if (lane == 0) bar_arrive(smem_addr(&mem.parts_free));
+      ++met;
     }
-    if (s.slot == kOfCluster) {
-      cluster_sync();
+    __syncwarp();
+    if (lane == 0) bar_arrive(smem_addr(&mem.share_free[k % kShares]));
+  }
+  }
+  // A cluster's CTAs join their parts; all of its threads come here
+  if (a.cluster > 1) {
+    Share& s = mem.share[0];
+    cluster_sync();
+    if (s.seq >= 0 && warp < kW) {
+      float* joint = reinterpret_cast<float*>(smem);
+      float2* joint_stats = reinterpret_cast<float2*>(joint + Sh::kRows * Sh::kD);
       for (int q = blockIdx.x % a.cluster + a.cluster * warp; q < Sh::kRows; q += a.cluster * kW) {
         const long long row = out_row(a, s, q);
         if (row < 0) continue;
@@ -645,8 +748,10 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
         }
         if (lane == 0 && a.lse) a.lse[row] = (top + log2f(total)) * kLn2;
       }
-      cluster_sync();  // no CTA leaves while its results are read
     }
+    // no CTA leaves while its results are read
+    cluster_arrive_relaxed();
+    cluster_wait();
   }
   write_empty(a);
 }
