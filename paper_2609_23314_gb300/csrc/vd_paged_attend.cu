@@ -102,7 +102,7 @@ struct Slots {
   int at[5];
 };
 std::mutex g_slots_mu;
-Slots g_slots[64][2][8][2];
+Slots g_slots[64][2][8][kKinds];
 
 vd_status slots_of(const DeviceInfo& dev, const PagedKernel& k, Slots& s) {
   std::lock_guard<std::mutex> lk(g_slots_mu);
@@ -140,6 +140,7 @@ vd_status slots_of(const DeviceInfo& dev, const PagedKernel& k, Slots& s) {
 struct Plan {
   const PagedKernel* kernel;
   int rows, tiles, cluster, ctas;
+  bool one_launch;             // no parts to join
   size_t split, stats, parts;  // bytes of the workspace's three parts
   unsigned* status;
 };
@@ -156,9 +157,11 @@ vd_status plan_of(const vd_paged_cache* c, int n_q_head, int B, Plan* plan) {
   r = device_info(&dev);
   if (r != VD_OK) return r;
   const bool e4m3 = c->type == VD_PAGED_E4M3;
-  const int m = (c->head_dim + 31) / 32 - 1, nt = rows > 8;
-  const PagedKernel& k = (e4m3 ? kPagedE4m3 : kPagedBf16)[m][nt];
-  Slots& slots = g_slots[dev.id][e4m3][m][nt];
+  const int m = (c->head_dim + 31) / 32 - 1;
+  const int want_kind = env_int("VD_PAGED_KERNEL", -1);
+  const int kind = want_kind >= 0 && want_kind < kKinds ? want_kind : rows <= 8 ? 0 : rows <= 16 ? 1 : 2;
+  const PagedKernel& k = (e4m3 ? kPagedE4m3 : kPagedBf16)[m][kind];
+  Slots& slots = g_slots[dev.id][e4m3][m][kind];
   r = slots_of(dev, k, slots);
   if (r != VD_OK) return r;
   plan->kernel = &k;
@@ -170,13 +173,15 @@ vd_status plan_of(const vd_paged_cache* c, int n_q_head, int B, Plan* plan) {
   const long long capacity = (long long)c->page_size * c->max_pages;
   int e = 4;
   while (e > 0 && (units << e > slots.at[e] || capacity < 128 << e)) --e;
-  if (capacity > 1024 << e) e = 0;
+  if (kind < 2 && capacity > 1024 << e) e = 0;
   const int want = env_int("VD_PAGED_CLUSTER", -1);
   if (want == 1) e = 0;
   plan->cluster = 1 << e;
-  plan->ctas = e > 0 ? (int)(units << e) : slots.at[0];
-  const size_t parts = e > 0 ? 0 : 2 * (size_t)plan->ctas * plan->rows;
-  plan->split = e > 0 ? 0 : (size_t)plan->ctas * sizeof(int4);
+  plan->one_launch = e > 0 || kind == 2;
+  if (units << e > INT_MAX) return VD_ERR_UNSUPPORTED;
+  plan->ctas = plan->one_launch ? (int)(units << e) : slots.at[0];
+  const size_t parts = plan->one_launch ? 0 : 2 * (size_t)plan->ctas * plan->rows;
+  plan->split = plan->one_launch ? 0 : (size_t)plan->ctas * sizeof(int4);
   plan->stats = parts * sizeof(float2);
   plan->parts = parts * c->head_dim * sizeof(float);
   return VD_OK;
@@ -244,7 +249,7 @@ vd_status vd_paged_attend(const vd_paged_cache* c, int32_t layer, const void* q,
   const PagedKernel& k = *p.kernel;
   r = launch_clusters((unsigned)p.ctas, (unsigned)k.threads, (unsigned)p.cluster, k.smem, s, k.kern,
                       a);
-  if (r != VD_OK || p.cluster > 1) return r;
+  if (r != VD_OK || p.one_launch) return r;
   return launch_dependent((unsigned)(p.ctas * p.rows), s, paged_join_kernel, a);
 }
 

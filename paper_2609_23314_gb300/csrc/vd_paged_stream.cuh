@@ -768,7 +768,9 @@ constexpr PagedKernel paged_stream() {
           Sh::kKeys};
 }
 
-// [(head_dim + 31) / 32 - 1][tiles of 8 or 16 rows]
-extern const PagedKernel kPagedBf16[8][2], kPagedE4m3[8][2];
+// [(head_dim + 31) / 32 - 1][kind]: the streaming kernel with tiles of 8 and of 16 rows (where their
+// sums fit the registers), the block kernel
+constexpr int kKinds = 3;
+extern const PagedKernel kPagedBf16[8][kKinds], kPagedE4m3[8][kKinds];
 
 }  // namespace vd

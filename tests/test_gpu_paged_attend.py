@@ -26,12 +26,18 @@ def _lib():
     assert vd.vd_get_device_status() == 0
 
 
-@pytest.fixture(params=["automatic", "pieces"])
+ROUTES = {"automatic": {}, "pieces": dict(VD_PAGED_CLUSTER="1"),
+          "tiles_of_16": dict(VD_PAGED_KERNEL="1", VD_PAGED_CLUSTER="1"),
+          "block": dict(VD_PAGED_KERNEL="2"),
+          "block_alone": dict(VD_PAGED_KERNEL="2", VD_PAGED_CLUSTER="1")}
+
+
+@pytest.fixture(params=ROUTES)
 def route(request, monkeypatch):
-    """The plan that the library takes, which for few units is a cluster for each, and again with
-    pieces of the line and the join."""
-    if request.param == "pieces":
-        monkeypatch.setenv("VD_PAGED_CLUSTER", "1")
+    """The kernel and plan that the library takes by the sizes, which for few units is a cluster for
+    each; pieces of the line and the join; the other kernels for all sizes."""
+    for name, value in ROUTES[request.param].items():
+        monkeypatch.setenv(name, value)
 
 
 def queries(n, B, n_q, d, seed=0, size=1.0):
