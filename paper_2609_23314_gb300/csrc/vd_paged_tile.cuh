@@ -340,15 +340,39 @@ __global__ void __launch_bounds__(kTileThreads, 1)
         lookup(i + 1, next);
         ok = await_buffer(i);
         if (!ok) break;
-        const uint32_t dst = buffer(i), first = row_of(now, 0), second = row_of(now, 1);
+        constexpr int kRowChunks = kD / 8;
+        const uint32_t dst = buffer(i);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          if (32 * u >= slice.count) break;
+          const uint32_t mine = row_of(now, u);
+          const int here = min(32, slice.count - 32 * u);  // slots, a multiple of 8
+          constexpr bool kFixed = 32 % kRowChunks == 0;    // a lane has the same chunk of every row
+          if (kFixed && chunks == kRowChunks &&
+              __all_sync(kFull, mine != kNoRow || lane >= here)) {
+            constexpr int kStep = 32 / kRowChunks, kBatch = 8 / kStep;  // rows, and copies of 8 rows
+            const int chunk = lane % kRowChunks, key = lane / kRowChunks;
+            const char* from = pool + chunk * 16;
+            uint32_t to = tile_at<M>(dst, slice.first + 32 * u + key, chunk);
 #pragma unroll 1
-        for (int j = lane; j < slice.count * (kD / 8); j += 32) {
-          const int key = j / (kD / 8), chunk = j % (kD / 8);
-          const uint32_t r0 = __shfl_sync(kFull, first, key & 31),
-                         r1 = __shfl_sync(kFull, second, key & 31), r = key < 32 ? r0 : r1;
-          const bool real = r != kNoRow && chunk < chunks;
-          cp_async16_or_zero(tile_at<M>(dst, slice.first + key, chunk),
-                             pool + (real ? (size_t)(r + chunk) * 16 : 0), real);
+            for (int k0 = 0; k0 < here; k0 += 8, to += 8 * 128) {
+              uint32_t row[kBatch];
+#pragma unroll
+              for (int j = 0; j < kBatch; ++j) row[j] = __shfl_sync(kFull, mine, k0 + kStep * j + key);
+#pragma unroll
+              for (int j = 0; j < kBatch; ++j)
+                cp_async16((to ^ (kStep * j << 4)) + kStep * j * 128, from + (size_t)row[j] * 16);
+            }
+          } else {
+#pragma unroll 1
+            for (int j = lane; j < here * kRowChunks; j += 32) {
+              const int key = j / kRowChunks, chunk = j % kRowChunks;
+              const uint32_t row = __shfl_sync(kFull, mine, key);
+              const bool real = row != kNoRow && chunk < chunks;
+              cp_async16_or_zero(tile_at<M>(dst, slice.first + 32 * u + key, chunk),
+                                 pool + (size_t)(real ? row + chunk : 0u) * 16, real);
+            }
+          }
         }
         cp_async_commit();
         if (i > 0) {
