@@ -71,6 +71,10 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   return r;
 }
 
+__device__ __forceinline__ void prefetch_l2(const void* p) {
+  asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
+}
+
 // Arrives on the barrier once this thread's copies so far have landed.
 __device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
@@ -171,12 +175,16 @@ __device__ __forceinline__ bool not_finite(uint32_t w) {
 }
 
 // Two weights in bf16, and in `low` what that leaves of them: together within 2^-16 of a weight.
-// Both parts of a weight above 0 are above 0, so that an infinite value stays one.
+// Both parts of a weight whose upper one is not 0 are above 0 (low ones at least 2^-133), so that
+// an infinite value stays one.
 __device__ __forceinline__ uint32_t split_weights(float x, float y, uint32_t& low) {
   uint32_t high;
   asm("cvt.rz.bf16x2.f32 %0, %1, %2;" : "=r"(high) : "f"(y), "f"(x));
-  low = pack_bf16(fmaxf(x - __uint_as_float(high << 16), x * 0x1p-30f),
-                  fmaxf(y - __uint_as_float(high & 0xffff0000u), y * 0x1p-30f));
+  float lx, ly;
+  f2_unpack(f2_add(f2_pack(x, y), f2_pack(__uint_as_float(high << 16 ^ 0x80000000u),
+                                          __uint_as_float((high & 0xffff0000u) ^ 0x80000000u))),
+            lx, ly);
+  low = pack_bf16(lx, ly) | __vminu2(high, 0x00010001u);
   return high;
 }
 
@@ -211,6 +219,19 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
       st_shared16(base + 16 * i, make_uint4(0, 0, 0, 0));
   grid_dependency_wait();
   grid_launch_dependents();
+  if (a.cluster > 1) {
+    // queries and the table, which a wait for the length need not delay, into L2
+    const int unit = blockIdx.x >> a.cluster_shift, head = unit / a.tiles, seq = head / a.heads;
+    const int line = threadIdx.x - 32, row = (unit - head * a.tiles) * Sh::kRows + (lane & (Sh::kRows - 1));
+    if (warp == 0 && row < a.B * a.group) {
+      const int tok = row / a.group;
+      const uint16_t* q = a.q + ((((size_t)seq * a.B + tok) * a.heads + head - seq * a.heads) * a.group +
+                                 row - tok * a.group) * a.d;
+      prefetch_l2(q + (lane >= Sh::kRows ? a.d / 2 : 0));
+    } else if (line >= 0 && 32 * line < a.pages.max_pages) {
+      prefetch_l2(a.pages.table + (size_t)seq * a.pages.max_pages + 32 * line);
+    }
+  }
   long long all = 0;
   if (a.cluster == 1 && a.n_seq > 32) all = Walk::survey(a, mem.walk);
   __syncthreads();
@@ -368,6 +389,8 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
     const int s0 = s.s0, count = s.s1 - s.s0, len = s.len;
     int sees[NT][2];  // slots that columns 2 c and 2 c + 1 see
     float qs[NT][2];  // what their scores are multiplied by for log2 units
+    // some token does not see a slot that others see (what lies behind them all reads as zero)
+    const bool unseen = a.causal && (s.tile * Sh::kRows) / a.group + 1 < s.add;
     const int all_see = a.causal ? len + (s.tile * Sh::kRows) / a.group + 1 : len;
     const float ks = E4M3 && a.pages.k_scale ? __ldcg(a.pages.k_scale + s.head) : 1.f;
     const float vs = E4M3 && a.pages.v_scale ? __ldcg(a.pages.v_scale + s.head) : 1.f;
@@ -564,7 +587,7 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
       // A value that is not finite must not reach the tokens that do not see its slot, whose
       // weight for it is 0: then the slots go one by one, to those that do.
       bool odd = false;
-      if (hides) {
+      if (hides && unseen) {
         for (int i = lane; i < Sh::kTileBytes / 16; i += 32) {
           const uint4 w = ld_shared16(tile_v + 16 * i);
           odd |= not_finite<E4M3>(w.x) || not_finite<E4M3>(w.y) || not_finite<E4M3>(w.z) ||

@@ -90,6 +90,19 @@ __global__ void __launch_bounds__(kTileThreads, 1)
   grid_dependency_wait();
   grid_launch_dependents();
 
+  // Queries and the table, which a wait for the length need not delay, into L2
+  {
+    const int r = tile * kTileRows + (threadIdx.x & 127);
+    if (threadIdx.x < 256 && r < a.B * a.group) {
+      const int tok = r / a.group;
+      const char* q = reinterpret_cast<const char*>(
+          a.q + ((((size_t)seq * a.B + tok) * a.heads + head) * a.group + r - tok * a.group) * a.d);
+      prefetch_l2(q + (threadIdx.x >= 128 ? a.d : 0));
+    }
+    const int line = threadIdx.x - 256;  // of 32 entries
+    if (line >= 0 && 32 * line < a.pages.max_pages)
+      prefetch_l2(a.pages.table + (size_t)seq * a.pages.max_pages + 32 * line);
+  }
   // kept where the loops need no registers for it
   volatile int* kept = reinterpret_cast<volatile int*>(smem + Sh::kFactors);
   const int2 size = seq_size(a, seq, rank == 0 && tile == 0 && head == 0 && threadIdx.x == 0);
@@ -237,9 +250,13 @@ __global__ void __launch_bounds__(kTileThreads, 1)
           uint32_t low[8];
 #pragma unroll
           for (int j = j0; j < j0 + 16; j += 2) {
-            const float lo = exp2_approx(__fadd_rn(__fmul_rn(__uint_as_float(s[j]), factor), shift));
-            const float hi =
-                exp2_approx(__fadd_rn(__fmul_rn(__uint_as_float(s[j + 1]), factor), shift));
+            float lo, hi;
+            f2_unpack(f2_add(f2_mul(f2_pack(__uint_as_float(s[j]), __uint_as_float(s[j + 1])),
+                                    f2_pack(factor, factor)),
+                             f2_pack(shift, shift)),
+                      lo, hi);
+            lo = exp2_approx(lo);
+            hi = exp2_approx(hi);
             sum2 = f2_add(sum2, f2_pack(lo, hi));
             s[j / 2] = E4M3 ? pack_f16(lo, hi) : split_weights(lo, hi, low[(j - j0) / 2]);
           }
