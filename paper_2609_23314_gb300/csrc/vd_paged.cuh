@@ -81,6 +81,34 @@ __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d
   return r;
 }
 
+// y / s for the rounding to e4m3 that follows: the fp32 quotient, correctly rounded, wherever it is
+// between 2^-11 and 2^9 (smaller ones become 0, larger ones 448, whatever their last bits).
+// From y times the rounded inverse, which is off by 1.5 units in the last place, by two steps
+// q + (y - q s) inverse with one rounding each: the first leaves one unit, and the second rounds
+// correctly (Markstein's theorem on quotients from a correctly rounded inverse, which excepts a
+// divisor whose significand is all ones).  Divisors that the steps do not suit are divided by.
+struct Divisor {
+  float s, inverse;
+  bool plain;
+  __device__ __forceinline__ explicit Divisor(float scale) : s(scale), inverse(1.f / scale) {
+    plain = !(scale >= 0x1p-60f && scale <= 0x1p60f) ||
+            (__float_as_uint(scale) & 0x7fffffu) == 0x7fffffu;
+  }
+  __device__ __forceinline__ float operator()(float y) const {
+    if (plain) return y / s;  // the same for the threads of a head
+    float q = y * inverse;
+    if (fabsf(q) < 0x1p10f && fabsf(q) > 0x1p-12f) {
+      q = fmaf(fmaf(-q, s, y), inverse, q);
+      q = fmaf(fmaf(-q, s, y), inverse, q);
+    }
+    return q;
+  }
+};
+
+__device__ __forceinline__ uint32_t pack_quotients(const Divisor& by, const float* x) {
+  return pack_e4m3(by(x[0]), by(x[1]), by(x[2]), by(x[3]));
+}
+
 // Two e4m3 values (the low or the high half of w) to two fp16 ones, exactly.
 __device__ __forceinline__ uint32_t e4m3_to_h2(uint32_t w, bool high) {
   uint32_t r;

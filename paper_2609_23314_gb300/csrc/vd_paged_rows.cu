@@ -85,10 +85,8 @@ struct PagedRows {
     if (rows[t] == kNoRow) return;
     char* dst = base + rows[t] + kh * p.pages.head_stride + c * (E4M3 ? 8 : 16);
     if (E4M3) {
-      const float s = scale ? scale[kh] : 1.f;
-      *reinterpret_cast<uint2*>(dst) =
-          make_uint2(pack_e4m3(x[0] / s, x[1] / s, x[2] / s, x[3] / s),
-                     pack_e4m3(x[4] / s, x[5] / s, x[6] / s, x[7] / s));
+      const Divisor by(scale ? __ldcg(scale + kh) : 1.f);
+      *reinterpret_cast<uint2*>(dst) = make_uint2(pack_quotients(by, x), pack_quotients(by, x + 4));
     } else {
       st16(dst, pack8(x));
     }
@@ -137,27 +135,23 @@ struct CopyArgs {
   uint16_t *k, *v;       // the contiguous side
   const int32_t* len_in; // lengths that say which rows
   int32_t* len_out;      // where they are copied to (nullable)
-  int layers, heads, cap, d;
-  unsigned blocks;       // CTAs of a unit
+  int units, heads, cap, d;  // units: layers x heads
+  unsigned blocks, groups;   // of a sequence's rows, of its units
 };
 
-constexpr int kRowsInFlight = 4;  // of K and of V, a thread
+constexpr int kRowsInFlight = 2;  // of K and of V, a thread, twice
 
-struct Values16 {  // 8 bf16 values, or 16 that are e4m3 in the pages
-  uint4 w[2];
-};
-
-// A thread takes 16 bytes of a page's row of K and of V, or what becomes them; the threads of a
-// CTA take whole rows, one after the other, kRowsInFlight of them at a time.
+// A thread takes 16 bytes of kRowsInFlight rows of K and of V in the pages, or what becomes them.
+// Their pages are looked up once for a group of units (layers and heads, for which they are
+// the same), which the CTA goes through with the loads of the next one under way.
 template <bool PACK, bool E4M3>
 __global__ void __launch_bounds__(kThreads) paged_copy_kernel(CopyArgs a) {
   grid_dependency_wait();
   grid_launch_dependents();
-  const unsigned unit = blockIdx.x / a.blocks, block = blockIdx.x % a.blocks;
-  const unsigned per = a.layers * a.heads;
-  const int seq = unit / per, inner = unit % per, layer = inner / a.heads, head = inner % a.heads;
+  const unsigned group = blockIdx.x % a.groups, at_seq = blockIdx.x / a.groups;
+  const int seq = at_seq / a.blocks, block = at_seq % a.blocks;
   const int n = __ldcg(a.len_in + seq);
-  const bool leader = threadIdx.x == 0 && block == 0 && inner == 0;
+  const bool leader = threadIdx.x == 0 && block == 0 && group == 0;
   if (n < 0 || n > a.cap || n > a.pages.capacity()) {
     if (leader) record_status(a.pages.status, kStDeviceLen);
     return;
@@ -165,79 +159,102 @@ __global__ void __launch_bounds__(kThreads) paged_copy_kernel(CopyArgs a) {
   if (leader && a.len_out) a.len_out[seq] = n;
   constexpr int kValues = E4M3 ? 16 : 8;
   const int chunks = a.d / kValues, rows = kThreads / chunks;
-  const int r = threadIdx.x / chunks, c = threadIdx.x % chunks;
+  const int r = threadIdx.x / chunks, c = threadIdx.x - r * chunks;
   if (r >= rows) return;
-  const long long in_page = layer * a.layer_stride + head * a.pages.head_stride + c * 16;
-  const size_t in_rows = (size_t)unit * a.cap * a.d + c * kValues;
-  float ks = 1.f, vs = 1.f;
-  if (E4M3) {
-    if (a.pages.k_scale) ks = a.pages.k_scale[inner];
-    if (a.pages.v_scale) vs = a.pages.v_scale[inner];
-  }
+  const int u0 = (int)((long long)a.units * group / a.groups),
+            u1 = (int)((long long)a.units * (group + 1) / a.groups);
+  struct Data {
+    uint4 w[kRowsInFlight][2][PACK && E4M3 ? 2 : 1];
+    float scale[2];
+  };
   const long long step = (long long)a.blocks * rows * kRowsInFlight;
   for (long long t0 = (long long)block * rows * kRowsInFlight + r; t0 < n; t0 += step) {
-    long long at[kRowsInFlight];
+    long long in_pages[kRowsInFlight];
 #pragma unroll
     for (int i = 0; i < kRowsInFlight; ++i) {
       const long long t = t0 + i * rows;
-      at[i] = -1;
-      if (t < n) {
-        const int page = a.pages.page_of(seq, (int)t);
-        if (page >= 0) at[i] = in_page + a.pages.row(page, (int)t);
-      }
+      const int page = t < n ? a.pages.page_of(seq, (int)t) : -1;
+      in_pages[i] = page < 0 ? -1 : a.pages.row(page, (int)t) + c * 16;
     }
-    Values16 x[kRowsInFlight][2];
-#pragma unroll
-    for (int i = 0; i < kRowsInFlight; ++i) {
-      if (at[i] < 0) continue;
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const uint16_t* row = (t ? a.v : a.k) + in_rows + (t0 + i * rows) * a.d;
-        if (PACK) {
-          x[i][t].w[0] = ld_cg16(row);
-          if (E4M3) x[i][t].w[1] = ld_cg16(row + 8);
-        } else {
-          x[i][t].w[0] = ld_cg16((t ? a.pages.v : a.pages.k) + at[i]);
-        }
+    auto place = [&](int u) {  // of a unit in the pages
+      const int layer = u / a.heads;
+      return layer * a.layer_stride + (u - layer * a.heads) * a.pages.head_stride;
+    };
+    auto flat = [&](int u) {  // and in the rows
+      return (((size_t)seq * a.units + u) * a.cap + t0) * a.d + c * kValues;
+    };
+    auto load = [&](int u, Data& x) {
+      const long long unit = place(u);
+      const size_t rows_at = flat(u);
+      if (E4M3) {
+        x.scale[0] = a.pages.k_scale ? __ldcg(a.pages.k_scale + u) : 1.f;
+        x.scale[1] = a.pages.v_scale ? __ldcg(a.pages.v_scale + u) : 1.f;
       }
-    }
 #pragma unroll
-    for (int i = 0; i < kRowsInFlight; ++i) {
-      if (at[i] < 0) continue;
+      for (int i = 0; i < kRowsInFlight; ++i) {
+        if (in_pages[i] < 0) continue;
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        uint16_t* row = (t ? a.v : a.k) + in_rows + (t0 + i * rows) * a.d;
-        char* page = (t ? a.pages.v : a.pages.k) + at[i];
-        const float s = t ? vs : ks;
-        if (PACK) {
-          if (E4M3) {
-            float y[8], z[8];
-            unpack8(x[i][t].w[0], y);
-            unpack8(x[i][t].w[1], z);
-            st16(page, make_uint4(pack_e4m3(y[0] / s, y[1] / s, y[2] / s, y[3] / s),
-                                  pack_e4m3(y[4] / s, y[5] / s, y[6] / s, y[7] / s),
-                                  pack_e4m3(z[0] / s, z[1] / s, z[2] / s, z[3] / s),
-                                  pack_e4m3(z[4] / s, z[5] / s, z[6] / s, z[7] / s)));
+        for (int t = 0; t < 2; ++t) {
+          if (PACK) {
+            const uint16_t* row = (t ? a.v : a.k) + rows_at + (size_t)(i * rows) * a.d;
+            x.w[i][t][0] = ld_cg16(row);
+            if (E4M3) x.w[i][t][PACK && E4M3] = ld_cg16(row + 8);
           } else {
-            st16(page, x[i][t].w[0]);
+            x.w[i][t][0] = ld_cg16((t ? a.pages.v : a.pages.k) + in_pages[i] + unit);
           }
-        } else if (E4M3) {
-          const uint32_t w[4] = {x[i][t].w[0].x, x[i][t].w[0].y, x[i][t].w[0].z, x[i][t].w[0].w};
-          uint32_t o[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            float lo, hi;
-            asm("{ .reg .b16 a, b; mov.b32 {a, b}, %2; cvt.f32.f16 %0, a; cvt.f32.f16 %1, b; }"
-                : "=f"(lo), "=f"(hi)
-                : "r"(e4m3_to_h2(w[e >> 1], e & 1)));
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[e]) : "f"(hi * s), "f"(lo * s));
-          }
-          st16(row, make_uint4(o[0], o[1], o[2], o[3]));
-          st16(row + 8, make_uint4(o[4], o[5], o[6], o[7]));
-        } else {
-          st16(row, x[i][t].w[0]);
         }
       }
+    };
+    auto store = [&](int u, const Data& x) {
+      const long long unit = place(u);
+      const size_t rows_at = flat(u);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const Divisor by(PACK && E4M3 ? x.scale[t] : 1.f);
+#pragma unroll
+        for (int i = 0; i < kRowsInFlight; ++i) {
+          if (in_pages[i] < 0) continue;
+          uint16_t* row = (t ? a.v : a.k) + rows_at + (size_t)(i * rows) * a.d;
+          char* page = (t ? a.pages.v : a.pages.k) + in_pages[i] + unit;
+          const uint4& w = x.w[i][t][0];
+          if (PACK) {
+            if (E4M3) {
+              float y[8], z[8];
+              unpack8(w, y);
+              unpack8(x.w[i][t][PACK && E4M3], z);
+              st16(page, make_uint4(pack_quotients(by, y), pack_quotients(by, y + 4),
+                                    pack_quotients(by, z), pack_quotients(by, z + 4)));
+            } else {
+              st16(page, w);
+            }
+          } else if (E4M3) {
+            const uint32_t in[4] = {w.x, w.y, w.z, w.w};
+            uint32_t o[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              float lo, hi;
+              asm("{ .reg .b16 a, b; mov.b32 {a, b}, %2; cvt.f32.f16 %0, a; cvt.f32.f16 %1, b; }"
+                  : "=f"(lo), "=f"(hi)
+                  : "r"(e4m3_to_h2(in[e >> 1], e & 1)));
+              asm("cvt.rn.bf16x2.f32 %0, %1, %2;"
+                  : "=r"(o[e])
+                  : "f"(hi * x.scale[t]), "f"(lo * x.scale[t]));
+            }
+            st16(row, make_uint4(o[0], o[1], o[2], o[3]));
+            st16(row + 8, make_uint4(o[4], o[5], o[6], o[7]));
+          } else {
+            st16(row, w);
+          }
+        }
+      }
+    };
+    Data x, y;
+    load(u0, x);
+    for (int u = u0; u < u1; u += 2) {
+      if (u + 1 < u1) load(u + 1, y);
+      store(u, x);
+      if (u + 2 < u1) load(u + 2, x);
+      if (u + 1 < u1) store(u + 1, y);
     }
   }
 }
@@ -260,26 +277,29 @@ vd_status run_paged_copy(bool pack, const vd_paged_cache* c, int32_t layer0, con
   a.layer_stride = c->layer_stride * (e4m3 ? 1 : 2);
   a.k = static_cast<uint16_t*>(b->k);
   a.v = static_cast<uint16_t*>(b->v);
-  a.layers = b->n_layer;
+  a.units = b->n_layer * b->n_kv_head;
   a.heads = b->n_kv_head;
   a.cap = b->capacity;
   a.d = b->head_dim;
   a.len_in = pack ? b->len : c->len;
   a.len_out = !pack ? b->len : layer0 + b->n_layer == c->n_layer ? c->len : nullptr;
-  // CTAs for a few waves at most, each going on over its unit's rows: the lengths are on the
-  // device, and a large capacity costs nothing beyond them
-  const long long units = (long long)b->n_seq * b->n_layer * b->n_kv_head;
+  // CTAs for a few waves, each going on over its rows: the lengths are on the device, and a large
+  // capacity costs nothing beyond them.  A row block's units are shared out as far as that takes.
   const long long most = (long long)c->page_size * c->max_pages < b->capacity
                              ? (long long)c->page_size * c->max_pages
                              : b->capacity;
   const int rows = kThreads / (b->head_dim / (e4m3 ? 16 : 8)) * kRowsInFlight;
-  long long blocks = (most + rows - 1) / rows, want = (32LL * dev.sms + units - 1) / units;
-  if (blocks > want) blocks = want;
+  const long long want = 32LL * dev.sms;
+  long long blocks = (most + rows - 1) / rows, room = (want + b->n_seq - 1) / b->n_seq;
+  if (blocks > room) blocks = room;
+  long long groups = (room + blocks - 1) / blocks;
+  if (groups > a.units) groups = a.units;
   a.blocks = (unsigned)blocks;
-  if (units * blocks > INT_MAX) return VD_ERR_UNSUPPORTED;
+  a.groups = (unsigned)groups;
+  const long long ctas = b->n_seq * blocks * groups;
   void (*kern)(CopyArgs) = pack ? (e4m3 ? paged_copy_kernel<true, true> : paged_copy_kernel<true, false>)
                                 : (e4m3 ? paged_copy_kernel<false, true> : paged_copy_kernel<false, false>);
-  return launch_clusters((unsigned)(units * blocks), kThreads, 1, 0, s, kern, a);
+  return launch_clusters((unsigned)ctas, kThreads, 1, 0, s, kern, a);
 }
 
 }  // namespace

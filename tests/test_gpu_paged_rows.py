@@ -126,6 +126,37 @@ def test_values_that_8_bits_do_not_hold(value, stored):
         assert raw(pool)[0, int(c.page_table[0, 0]), 0, 0].tolist() == [stored] * 16
 
 
+def test_every_bf16_value_by_many_scales():
+    """What is stored is the fp32 quotient rounded to e4m3, for every value and odd divisors."""
+    g = torch.Generator().manual_seed(3)
+    scales = torch.cat((2.0 ** (torch.rand(52, generator=g) * 40 - 20),
+                        torch.tensor([1.0, 0.3, 3.0, 2.0 - 2.0 ** -23, 1.0 + 2.0 ** -23, 1e-30, 1e30,
+                                      2.0 ** -126, 7.0 / 8, 2.0 ** -61, 2.0 ** 61, 1.0 / 448])))
+    h = scales.numel()
+    c = vd.PagedCache.empty(1, 1, h, 256, n_page=16, page_size=16, max_pages=16, dtype=FP8)
+    c.page_table.copy_(torch.arange(16))
+    c = vd.PagedCache(c.k, c.v, c.page_table, c.len, scales[None].cuda(), scales[None].cuda())
+    rows = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(BF).view(256, 1, 256).cuda()
+    qkv = rows.expand(256, 1 + 2 * h, 256).contiguous()[None]
+    flat = vd.Cache.empty(1, 1, h, 256, 256)
+    for pack in (False, True):
+        if pack:  # the same by way of the contiguous layout
+            flat.k.copy_(rows.transpose(0, 1).expand(h, 256, 256)[None, None])
+            flat.v.copy_(flat.k)
+            flat.len.fill_(256)
+            raw(c.k).zero_(), raw(c.v).zero_()
+            vd.vd_paged_pack(c, flat)
+        else:
+            vd.vd_paged_append(c, qkv, torch.empty((1, 256, 1, 256), dtype=BF, device="cuda"))
+        want = rows[:, 0].float()[None] / scales.cuda()[:, None, None]
+        want = raw(want.clamp(-448, 448).to(FP8))
+        for pool in (c.k, c.v):
+            got = raw(pool)[0].transpose(0, 1).reshape(h, 256, 256)
+            nan = torch.isnan(rows[:, 0].float())[None].expand_as(got)
+            assert torch.equal(got[~nan], want[~nan])
+            assert bool(((got[nan] & 0x7f) == 0x7f).all())
+
+
 @pytest.mark.parametrize("dtype", [BF, FP8])
 @pytest.mark.parametrize("by_token,d,page", [(False, 128, 16), (True, 96, 24), (False, 16, 1),
                                              (True, 256, 7), (False, 64, 128)])
