@@ -42,6 +42,17 @@ struct Pages {
   }
 };
 
+// Sums over the lanes up to this one.
+__device__ __forceinline__ long long warp_scan_i64(long long x) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const long long y = __shfl_up_sync(kFull, x, off);
+    if (lane >= off) x += y;
+  }
+  return x;
+}
+
 vd_status validate_paged(const vd_paged_cache* c);
 
 inline Pages pages_of(const vd_paged_cache* c, int layer, unsigned* status) {
@@ -94,19 +105,34 @@ struct Divisor {
     plain = !(scale >= 0x1p-60f && scale <= 0x1p60f) ||
             (__float_as_uint(scale) & 0x7fffffu) == 0x7fffffu;
   }
-  __device__ __forceinline__ float operator()(float y) const {
-    if (plain) return y / s;  // the same for the threads of a head
-    float q = y * inverse;
-    if (fabsf(q) < 0x1p10f && fabsf(q) > 0x1p-12f) {
-      q = fmaf(fmaf(-q, s, y), inverse, q);
-      q = fmaf(fmaf(-q, s, y), inverse, q);
-    }
-    return q;
+  __device__ __forceinline__ void operator()(float& x, float& y) const {
+    const unsigned long long xy = f2_pack(x, y), inv = f2_pack(inverse, inverse),
+                             minus = f2_pack(-s, -s), first = f2_mul(xy, inv);
+    const unsigned long long second = f2_fma(f2_fma(first, minus, xy), inv, first);
+    const unsigned long long third = f2_fma(f2_fma(second, minus, xy), inv, second);
+    float x0, y0, x1, y1;
+    f2_unpack(first, x0, y0);
+    f2_unpack(third, x1, y1);
+    x = fabsf(x0) < 0x1p10f && fabsf(x0) > 0x1p-12f ? x1 : x0;
+    y = fabsf(y0) < 0x1p10f && fabsf(y0) > 0x1p-12f ? y1 : y0;
   }
 };
 
-__device__ __forceinline__ uint32_t pack_quotients(const Divisor& by, const float* x) {
-  return pack_e4m3(by(x[0]), by(x[1]), by(x[2]), by(x[3]));
+// Eight values to e4m3.
+__device__ __forceinline__ uint2 pack_quotients(const Divisor& by, const float (&v)[8]) {
+  float x[8];
+  if (by.plain) {  // the same for the threads of a head
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = v[i] / by.s;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      x[i] = v[i];
+      x[i + 1] = v[i + 1];
+      by(x[i], x[i + 1]);
+    }
+  }
+  return make_uint2(pack_e4m3(x[0], x[1], x[2], x[3]), pack_e4m3(x[4], x[5], x[6], x[7]));
 }
 
 // Two e4m3 values (the low or the high half of w) to two fp16 ones, exactly.

@@ -107,16 +107,6 @@ struct Share {
   int slot;  // of the part; kWhole: the whole unit, kOfCluster: a part of the cluster's unit
 };
 
-__device__ __forceinline__ long long warp_scan_i64(long long x) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int off = 1; off < 32; off <<= 1) {
-    const long long y = __shfl_up_sync(kFull, x, off);
-    if (lane >= off) x += y;
-  }
-  return x;
-}
-
 // Sequences that a warp looks at together, one a lane.
 struct WalkMem {
   int first;

@@ -86,7 +86,7 @@ struct PagedRows {
     char* dst = base + rows[t] + kh * p.pages.head_stride + c * (E4M3 ? 8 : 16);
     if (E4M3) {
       const Divisor by(scale ? __ldcg(scale + kh) : 1.f);
-      *reinterpret_cast<uint2*>(dst) = make_uint2(pack_quotients(by, x), pack_quotients(by, x + 4));
+      *reinterpret_cast<uint2*>(dst) = pack_quotients(by, x);
     } else {
       st16(dst, pack8(x));
     }
@@ -105,11 +105,11 @@ struct PagedRows {
   }
 };
 
-template <bool INTERLEAVED, bool E4M3>
-__global__ void __launch_bounds__(kThreads) paged_append_kernel(QkvArgs a, PagedRowsArgs p) {
+template <bool INTERLEAVED, bool E4M3, bool FEW>
+__global__ void __launch_bounds__(kThreads, FEW ? 2 : 4) paged_append_kernel(QkvArgs a, PagedRowsArgs p) {
   extern __shared__ __align__(16) float table[];
   __shared__ long long rows[kMaxTokens];
-  norm_rope_tokens<INTERLEAVED>(a, table, PagedRows<E4M3>{a, p, rows});
+  norm_rope_tokens<INTERLEAVED, FEW>(a, table, PagedRows<E4M3>{a, p, rows});
 }
 
 __global__ void __launch_bounds__(kThreads)
@@ -130,108 +130,184 @@ __global__ void __launch_bounds__(kThreads)
 // whole caches: pages to contiguous rows and back
 // ---------------------------------------------------------------------------
 struct CopyArgs {
-  Pages pages;           // layer layer0; its len is not used
+  Pages pages;             // layer layer0; its len is not used
   long long layer_stride;  // bytes
-  uint16_t *k, *v;       // the contiguous side
-  const int32_t* len_in; // lengths that say which rows
-  int32_t* len_out;      // where they are copied to (nullable)
-  int units, heads, cap, d;  // units: layers x heads
-  unsigned blocks, groups;   // of a sequence's rows, of its units
+  uint16_t *k, *v;         // the contiguous side
+  const int32_t* len_in;   // lengths that say which rows
+  int32_t* len_out;        // where they are copied to (nullable)
+  int n_seq, units, heads, cap, d;  // units: layers x heads
 };
 
 constexpr int kRowsInFlight = 2;  // of K and of V, a thread, twice
 
-// A thread takes 16 bytes of kRowsInFlight rows of K and of V in the pages, or what becomes them.
-// Their pages are looked up once for a group of units (layers and heads, for which they are
-// the same), which the CTA goes through with the loads of the next one under way.
+// The copies of all sequences make a line: a block of rows of the first one in unit (layer and
+// head) after unit, the next block, and so on.  Each CTA takes an equal piece of it, whatever the
+// lengths are.  A thread takes 8 values of some rows of K and of V.  A block's pages are looked up once for its units, for which they are the same, and the
+// loads of the next unit are under way while one is stored.
 template <bool PACK, bool E4M3>
-__global__ void __launch_bounds__(kThreads) paged_copy_kernel(CopyArgs a) {
+__global__ void __launch_bounds__(kThreads, PACK && E4M3 ? 2 : 3) paged_copy_kernel(CopyArgs a) {
+  __shared__ long long sums[kWarps];
+  __shared__ long long found[2];
   grid_dependency_wait();
   grid_launch_dependents();
-  const unsigned group = blockIdx.x % a.groups, at_seq = blockIdx.x / a.groups;
-  const int seq = at_seq / a.blocks, block = at_seq % a.blocks;
-  const int n = __ldcg(a.len_in + seq);
-  const bool leader = threadIdx.x == 0 && block == 0 && group == 0;
-  if (n < 0 || n > a.cap || n > a.pages.capacity()) {
-    if (leader) record_status(a.pages.status, kStDeviceLen);
-    return;
+  const int chunks = a.d / 8, rows = kThreads / chunks, per_block = rows * kRowsInFlight;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  // blocks of a sequence, none where its length is out of range
+  auto blocks_of = [&](int s, bool report) {
+    if (s >= a.n_seq) return 0;
+    const int n = __ldcg(a.len_in + s);
+    if (n >= 0 && n <= a.cap && n <= a.pages.capacity()) return (n + per_block - 1) / per_block;
+    if (report) record_status(a.pages.status, kStDeviceLen);
+    return 0;
+  };
+  // sum over the CTA's threads up to this one, and over all
+  auto scan = [&](long long x, long long& all) {
+    const long long upto = warp_scan_i64(x);
+    __syncthreads();
+    if (lane == 31) sums[warp] = upto;
+    __syncthreads();
+    long long before = 0;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      if (w < warp) before += sums[w];
+      all += sums[w];
+    }
+    return before + upto;
+  };
+  long long all = 0, upto = 0, mine = 0;
+  if (a.n_seq > kThreads) {
+    long long x = 0;
+    for (int s = threadIdx.x; s < a.n_seq; s += kThreads) x += blocks_of(s, blockIdx.x == 0);
+    scan(x, all);
+  } else {
+    mine = blocks_of(threadIdx.x, blockIdx.x == 0);
+    upto = scan(mine, all);
   }
-  if (leader && a.len_out) a.len_out[seq] = n;
-  constexpr int kValues = E4M3 ? 16 : 8;
-  const int chunks = a.d / kValues, rows = kThreads / chunks;
+  if (a.len_out)
+    for (int s = blockIdx.x * kThreads + threadIdx.x; s < a.n_seq; s += gridDim.x * kThreads) {
+      const int n = __ldcg(a.len_in + s);
+      if (n >= 0 && n <= a.cap && n <= a.pages.capacity()) a.len_out[s] = n;
+    }
+  // this CTA's piece, the block and the sequence of its first position
+  const long long line = all * a.units;
+  const long long per = line / gridDim.x, more = line - per * gridDim.x;
+  long long at = per * blockIdx.x + min((long long)blockIdx.x, more);
+  const long long end = at + per + (blockIdx.x < more ? 1 : 0);
+  if (at >= end) return;
+  long long block = at / a.units;
+  int u = (int)(at - block * a.units);
+  long long base = 0;  // of a chunk of sequences
+  for (int chunk = 0;; chunk += kThreads) {
+    if (a.n_seq > kThreads) {
+      mine = blocks_of(chunk + threadIdx.x, false);
+      long long here;
+      upto = base + scan(mine, here);
+      all = base + here;
+    }
+    if (block < upto && block >= upto - mine) {
+      found[0] = chunk + threadIdx.x;
+      found[1] = block - (upto - mine);
+    }
+    __syncthreads();
+    if (block < all) break;
+    base = all;
+  }
+  int seq = (int)found[0];
+  block = found[1];
   const int r = threadIdx.x / chunks, c = threadIdx.x - r * chunks;
-  if (r >= rows) return;
-  const int u0 = (int)((long long)a.units * group / a.groups),
-            u1 = (int)((long long)a.units * (group + 1) / a.groups);
+
   struct Data {
-    uint4 w[kRowsInFlight][2][PACK && E4M3 ? 2 : 1];
+    uint4 w[kRowsInFlight][2];  // of an e4m3 row the first two words
     float scale[2];
   };
-  const long long step = (long long)a.blocks * rows * kRowsInFlight;
-  for (long long t0 = (long long)block * rows * kRowsInFlight + r; t0 < n; t0 += step) {
-    long long in_pages[kRowsInFlight];
+  // Where a unit lies on both sides
+  struct Place {
+    long long page, row;  // bytes, values
+    int u, head;
+  };
+  auto place = [&](int unit) {
+    const int layer = unit / a.heads, head = unit - layer * a.heads;
+    return Place{layer * a.layer_stride + head * a.pages.head_stride,
+                 ((long long)seq * a.units + unit) * a.cap * a.d, unit, head};
+  };
+  const long long to_layer = a.layer_stride - (a.heads - 1) * a.pages.head_stride,
+                  to_unit = (long long)a.cap * a.d;
+  auto step = [&](Place& p) {
+    p.row += to_unit;
+    ++p.u;
+    if (++p.head == a.heads) {
+      p.head = 0;
+      p.page += to_layer;
+    } else {
+      p.page += a.pages.head_stride;
+    }
+  };
+  while (at < end) {
+    const int n = __ldcg(a.len_in + seq);  // in range where the line has a block of it
+    const int blocks = n < 0 || n > a.cap ? 0 : (n + per_block - 1) / per_block;
+    if (block >= blocks) {
+      ++seq;
+      block = 0;
+      continue;
+    }
+    const int u1 = (int)min((long long)a.units, u + (end - at));
+    const long long t0 = block * per_block + r;
+    constexpr uint32_t kNoRow = 0xffffffffu;
+    uint32_t in_pages[kRowsInFlight];  // rows, in 16 bytes
 #pragma unroll
     for (int i = 0; i < kRowsInFlight; ++i) {
       const long long t = t0 + i * rows;
-      const int page = t < n ? a.pages.page_of(seq, (int)t) : -1;
-      in_pages[i] = page < 0 ? -1 : a.pages.row(page, (int)t) + c * 16;
+      const int page = r < rows && t < n ? a.pages.page_of(seq, (int)t) : -1;
+      in_pages[i] = page < 0 ? kNoRow : (uint32_t)(a.pages.row(page, (int)t) >> 4);
     }
-    auto place = [&](int u) {  // of a unit in the pages
-      const int layer = u / a.heads;
-      return layer * a.layer_stride + (u - layer * a.heads) * a.pages.head_stride;
-    };
-    auto flat = [&](int u) {  // and in the rows
-      return (((size_t)seq * a.units + u) * a.cap + t0) * a.d + c * kValues;
-    };
-    auto load = [&](int u, Data& x) {
-      const long long unit = place(u);
-      const size_t rows_at = flat(u);
+    const long long in_rows = t0 * a.d + c * 8, in_page = c * (E4M3 ? 8 : 16);
+    auto load = [&](const Place& p, Data& x) {
       if (E4M3) {
-        x.scale[0] = a.pages.k_scale ? __ldcg(a.pages.k_scale + u) : 1.f;
-        x.scale[1] = a.pages.v_scale ? __ldcg(a.pages.v_scale + u) : 1.f;
+        x.scale[0] = a.pages.k_scale ? __ldcg(a.pages.k_scale + p.u) : 1.f;
+        x.scale[1] = a.pages.v_scale ? __ldcg(a.pages.v_scale + p.u) : 1.f;
       }
 #pragma unroll
       for (int i = 0; i < kRowsInFlight; ++i) {
-        if (in_pages[i] < 0) continue;
+        if (in_pages[i] == kNoRow) continue;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
+          const char* page =
+              (t ? a.pages.v : a.pages.k) + (p.page + in_page) + (size_t)in_pages[i] * 16;
           if (PACK) {
-            const uint16_t* row = (t ? a.v : a.k) + rows_at + (size_t)(i * rows) * a.d;
-            x.w[i][t][0] = ld_cg16(row);
-            if (E4M3) x.w[i][t][PACK && E4M3] = ld_cg16(row + 8);
+            x.w[i][t] = ld_cg16((t ? a.v : a.k) + (p.row + in_rows) + i * rows * a.d);
+          } else if (E4M3) {
+            const uint2 w = __ldcg(reinterpret_cast<const uint2*>(page));
+            x.w[i][t].x = w.x;
+            x.w[i][t].y = w.y;
           } else {
-            x.w[i][t][0] = ld_cg16((t ? a.pages.v : a.pages.k) + in_pages[i] + unit);
+            x.w[i][t] = ld_cg16(page);
           }
         }
       }
     };
-    auto store = [&](int u, const Data& x) {
-      const long long unit = place(u);
-      const size_t rows_at = flat(u);
+    auto store = [&](const Place& p, const Data& x) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const Divisor by(PACK && E4M3 ? x.scale[t] : 1.f);
 #pragma unroll
         for (int i = 0; i < kRowsInFlight; ++i) {
-          if (in_pages[i] < 0) continue;
-          uint16_t* row = (t ? a.v : a.k) + rows_at + (size_t)(i * rows) * a.d;
-          char* page = (t ? a.pages.v : a.pages.k) + in_pages[i] + unit;
-          const uint4& w = x.w[i][t][0];
-          if (PACK) {
-            if (E4M3) {
-              float y[8], z[8];
-              unpack8(w, y);
-              unpack8(x.w[i][t][PACK && E4M3], z);
-              st16(page, make_uint4(pack_quotients(by, y), pack_quotients(by, y + 4),
-                                    pack_quotients(by, z), pack_quotients(by, z + 4)));
-            } else {
-              st16(page, w);
-            }
+          if (in_pages[i] == kNoRow) continue;
+          uint16_t* row = (t ? a.v : a.k) + (p.row + in_rows) + i * rows * a.d;
+          char* page =
+              (t ? a.pages.v : a.pages.k) + (p.page + in_page) + (size_t)in_pages[i] * 16;
+          const uint4& w = x.w[i][t];
+          if (PACK && E4M3) {
+            float y[8];
+            unpack8(w, y);
+            *reinterpret_cast<uint2*>(page) = pack_quotients(by, y);
+          } else if (PACK) {
+            st16(page, w);
           } else if (E4M3) {
-            const uint32_t in[4] = {w.x, w.y, w.z, w.w};
-            uint32_t o[8];
+            const uint32_t in[2] = {w.x, w.y};
+            uint32_t o[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < 4; ++e) {
               float lo, hi;
               asm("{ .reg .b16 a, b; mov.b32 {a, b}, %2; cvt.f32.f16 %0, a; cvt.f32.f16 %1, b; }"
                   : "=f"(lo), "=f"(hi)
@@ -241,7 +317,6 @@ __global__ void __launch_bounds__(kThreads) paged_copy_kernel(CopyArgs a) {
                   : "f"(hi * x.scale[t]), "f"(lo * x.scale[t]));
             }
             st16(row, make_uint4(o[0], o[1], o[2], o[3]));
-            st16(row + 8, make_uint4(o[4], o[5], o[6], o[7]));
           } else {
             st16(row, w);
           }
@@ -249,13 +324,27 @@ __global__ void __launch_bounds__(kThreads) paged_copy_kernel(CopyArgs a) {
       }
     };
     Data x, y;
-    load(u0, x);
-    for (int u = u0; u < u1; u += 2) {
-      if (u + 1 < u1) load(u + 1, y);
-      store(u, x);
-      if (u + 2 < u1) load(u + 2, x);
-      if (u + 1 < u1) store(u + 1, y);
+    Place from = place(u), to = from;
+    load(from, x);
+    for (int i = u; i < u1; i += 2) {
+      if (i + 1 < u1) {
+        step(from);
+        load(from, y);
+      }
+      store(to, x);
+      step(to);
+      if (i + 2 < u1) {
+        step(from);
+        load(from, x);
+      }
+      if (i + 1 < u1) {
+        store(to, y);
+        step(to);
+      }
     }
+    at += u1 - u;
+    u = 0;
+    ++block;
   }
 }
 
@@ -277,26 +366,22 @@ vd_status run_paged_copy(bool pack, const vd_paged_cache* c, int32_t layer0, con
   a.layer_stride = c->layer_stride * (e4m3 ? 1 : 2);
   a.k = static_cast<uint16_t*>(b->k);
   a.v = static_cast<uint16_t*>(b->v);
+  a.n_seq = b->n_seq;
   a.units = b->n_layer * b->n_kv_head;
   a.heads = b->n_kv_head;
   a.cap = b->capacity;
   a.d = b->head_dim;
   a.len_in = pack ? b->len : c->len;
   a.len_out = !pack ? b->len : layer0 + b->n_layer == c->n_layer ? c->len : nullptr;
-  // CTAs for a few waves, each going on over its rows: the lengths are on the device, and a large
-  // capacity costs nothing beyond them.  A row block's units are shared out as far as that takes.
   const long long most = (long long)c->page_size * c->max_pages < b->capacity
                              ? (long long)c->page_size * c->max_pages
                              : b->capacity;
-  const int rows = kThreads / (b->head_dim / (e4m3 ? 16 : 8)) * kRowsInFlight;
-  const long long want = 32LL * dev.sms;
-  long long blocks = (most + rows - 1) / rows, room = (want + b->n_seq - 1) / b->n_seq;
-  if (blocks > room) blocks = room;
-  long long groups = (room + blocks - 1) / blocks;
-  if (groups > a.units) groups = a.units;
-  a.blocks = (unsigned)blocks;
-  a.groups = (unsigned)groups;
-  const long long ctas = b->n_seq * blocks * groups;
+  // Pieces for many waves, so that none lasts long, of 16 units at least (the length's look-up and
+  // the pages' have to pay)
+  const int per_block = kThreads / (b->head_dim / 8) * kRowsInFlight;
+  const long long line = (most + per_block - 1) / per_block * b->n_seq * a.units;
+  const long long pieces = (line + 15) / 16, some = 32LL * dev.sms;
+  const long long ctas = pieces < some ? pieces : some;
   void (*kern)(CopyArgs) = pack ? (e4m3 ? paged_copy_kernel<true, true> : paged_copy_kernel<true, false>)
                                 : (e4m3 ? paged_copy_kernel<false, true> : paged_copy_kernel<false, false>);
   return launch_clusters((unsigned)ctas, kThreads, 1, 0, s, kern, a);
@@ -327,9 +412,13 @@ vd_status vd_paged_append(const vd_paged_cache* c, int32_t layer, const void* qk
                              k_weight, eps, inv_freq, rotary_dim, q_out, dev.sms);
   const PagedRowsArgs p = {pages_of(c, layer, dev.status), n_new, pos_first_new};
   const bool e4m3 = c->type == VD_PAGED_E4M3;
-  void (*kern)(QkvArgs, PagedRowsArgs) =
-      interleaved ? (e4m3 ? paged_append_kernel<true, true> : paged_append_kernel<true, false>)
-                  : (e4m3 ? paged_append_kernel<false, true> : paged_append_kernel<false, false>);
+  using Kernel = void (*)(QkvArgs, PagedRowsArgs);
+  static const Kernel kernels[2][2][2] = {  // [interleaved][e4m3][few tokens]
+      {{paged_append_kernel<false, false, false>, paged_append_kernel<false, false, true>},
+       {paged_append_kernel<false, true, false>, paged_append_kernel<false, true, true>}},
+      {{paged_append_kernel<true, false, false>, paged_append_kernel<true, false, true>},
+       {paged_append_kernel<true, true, false>, paged_append_kernel<true, true, true>}}};
+  const Kernel kern = kernels[interleaved != 0][e4m3][a.tokens_per_cta == 1];
   return launch_clusters(qkv_grid(a), kThreads, 1, qkv_smem(a),
                          reinterpret_cast<cudaStream_t>(stream), kern, a, p);
 }

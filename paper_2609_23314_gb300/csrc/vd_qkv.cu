@@ -41,11 +41,11 @@ struct NewRows {  // rows of [n_seq][n_layer][n_kv_head][B][head_dim]
   }
 };
 
-template <bool INTERLEAVED>
+template <bool INTERLEAVED, bool FEW>
 __global__ void __launch_bounds__(kThreads) qkv_norm_rope_kernel(QkvArgs a, NewRowsArgs n) {
   extern __shared__ __align__(16) float table[];
   __shared__ size_t new_row[kMaxTokens];
-  norm_rope_tokens<INTERLEAVED>(a, table, NewRows{a, n, new_row});
+  norm_rope_tokens<INTERLEAVED, FEW>(a, table, NewRows{a, n, new_row});
 }
 
 }  // namespace
@@ -75,6 +75,9 @@ extern "C" vd_status vd_qkv_norm_rope(const void* qkv, int32_t n_seq, int32_t B,
                          static_cast<uint16_t*>(v_new), layer, n_layer};
   return launch_clusters(qkv_grid(a), kThreads, 1, qkv_smem(a),
                          reinterpret_cast<cudaStream_t>(stream),
-                         interleaved ? qkv_norm_rope_kernel<true> : qkv_norm_rope_kernel<false>, a,
-                         n);
+                         a.tokens_per_cta > 1 ? (interleaved ? qkv_norm_rope_kernel<true, false>
+                                                             : qkv_norm_rope_kernel<false, false>)
+                                              : (interleaved ? qkv_norm_rope_kernel<true, true>
+                                                             : qkv_norm_rope_kernel<false, true>),
+                         a, n);
 }

@@ -45,7 +45,10 @@ __device__ __forceinline__ float half_turns(double pos, float inv_freq) {
 //   position(tok)  of a token (any thread)
 //   on(t)          whether the token's heads are written at all
 //   key(t, kh, c, x), value(t, kh, c, w)  chunk c of a KV head, in fp32 and as it came
-template <bool INTERLEAVED, class Sink>
+// FEW (a token a CTA): the norm weights are loaded with the first values, not where they are
+// wanted: one token 5.3 us in a graph for 7.1; with many tokens their registers cost a CTA of the
+// SM (16384 tokens 91 us for 81).
+template <bool INTERLEAVED, bool FEW, class Sink>
 __device__ __forceinline__ void norm_rope_tokens(const QkvArgs& a, float* table, const Sink& sink) {
   const int half = a.rd >> 1;
   const int tok0 = (int)blockIdx.x * a.tokens_per_cta;
@@ -73,6 +76,16 @@ __device__ __forceinline__ void norm_rope_tokens(const QkvArgs& a, float* table,
     if (second && it < items) n1 = ld_cg16(p + c1 * 8);
   };
   fetch(threadIdx.x / a.lanes);
+  uint4 early[2][2];  // FEW: of queries, of keys
+  if (FEW) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint16_t* w = k ? a.k_weight : a.q_weight;
+      early[k][0] = early[k][1] = make_uint4(0, 0, 0, 0);
+      if (w && active) early[k][0] = *reinterpret_cast<const uint4*>(w + c0 * 8);
+      if (w && second) early[k][1] = *reinterpret_cast<const uint4*>(w + c1 * 8);
+    }
+  }
   if (threadIdx.x < n_tok) sink.place(threadIdx.x, tok0 + threadIdx.x);
   for (int i = threadIdx.x; i < n_tok * half; i += kThreads) {
     const int t = i / half, f = i % half, tok = tok0 + t;
@@ -103,12 +116,12 @@ __device__ __forceinline__ void norm_rope_tokens(const QkvArgs& a, float* table,
         const float r = 1.f / sqrtf(ss / (float)a.d + a.eps);
         float g[8];
         if (active) {
-          unpack8(*reinterpret_cast<const uint4*>(wt + c0 * 8), g);
+          unpack8(FEW ? (h < a.n_q ? early[0][0] : early[1][0]) : *reinterpret_cast<const uint4*>(wt + c0 * 8), g);
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] = x[e] * r * g[e];
         }
         if (second) {
-          unpack8(*reinterpret_cast<const uint4*>(wt + c1 * 8), g);
+          unpack8(FEW ? (h < a.n_q ? early[0][1] : early[1][1]) : *reinterpret_cast<const uint4*>(wt + c1 * 8), g);
 #pragma unroll
           for (int e = 0; e < 8; ++e) y[e] = y[e] * r * g[e];
         }
