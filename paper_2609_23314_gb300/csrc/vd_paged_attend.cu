@@ -137,6 +137,26 @@ vd_status slots_of(const DeviceInfo& dev, const PagedKernel& k, Slots& s) {
   return VD_OK;
 }
 
+// 0, 1: the streaming kernel with tiles of 8 or of 16 query rows, 2: the block kernel.  By the
+// capacity, which the host knows, not by the lengths.  Up to 8 rows stream.  More: tiles of 8, which
+// go over the slots once each (from L2 mostly), while they are few; us with tiles of 8 / tiles of
+// 16 / block at 8 KV heads, head_dim 128, bf16:
+//   one sequence of 4000 tokens, 32 rows 16.1 / 23.6 / 18.8, 48 rows 22.9 / 24.3 / 19.5; of 500, 48
+//   rows 11.3 / 15.1 / 14.0; 4 of 1000, 16 rows 13.4 / 16.8 / 15.4, 24 rows 20.2 / 18.8 / 15.4; 8 of
+//   500, 16 rows 19.1 / 17.4 / 14.7.
+// Long sequences in a batch are bound by reading the slots: bf16 ones take tiles of 16 up to 16 rows
+// (32 of 2000, 12 rows 90.5 / 62.5 / 68.7), e4m3 ones tiles of 8 up to 24, as the block kernel turns
+// them to fp16 on the way (32 of 2000, 24 rows 70.0 / 83.7 / 80.9, 32 rows 88.4 / 88.5 / 81.3).
+int choose_kernel(long long rows, long long units, long long capacity, bool e4m3, int sms) {
+  const long long tiles8 = units * ((rows + 7) / 8);
+  if (rows <= 8 || tiles8 <= (rows <= 16 || e4m3 ? 64 : 47)) return 0;
+  if (capacity >= 1500) {
+    if (e4m3 && rows <= 24) return 0;
+    if (!e4m3 && rows <= 16 && units > sms) return 1;
+  }
+  return 2;
+}
+
 struct Plan {
   const PagedKernel* kernel;
   int rows, tiles, cluster, ctas;
@@ -159,7 +179,10 @@ vd_status plan_of(const vd_paged_cache* c, int n_q_head, int B, Plan* plan) {
   const bool e4m3 = c->type == VD_PAGED_E4M3;
   const int m = (c->head_dim + 31) / 32 - 1;
   const int want_kind = env_int("VD_PAGED_KERNEL", -1);
-  const int kind = want_kind >= 0 && want_kind < kKinds ? want_kind : rows <= 8 ? 0 : rows <= 16 ? 1 : 2;
+  const long long capacity = (long long)c->page_size * c->max_pages;
+  const int kind = want_kind >= 0 && want_kind < kKinds
+                       ? want_kind
+                       : choose_kernel(rows, (long long)c->n_seq * c->n_kv_head, capacity, e4m3, dev.sms);
   const PagedKernel& k = (e4m3 ? kPagedE4m3 : kPagedBf16)[m][kind];
   Slots& slots = g_slots[dev.id][e4m3][m][kind];
   r = slots_of(dev, k, slots);
@@ -170,7 +193,6 @@ vd_status plan_of(const vd_paged_cache* c, int n_q_head, int B, Plan* plan) {
   plan->tiles = (int)((rows + k.rows - 1) / k.rows);
   // A cluster for each unit: the largest with which they run at once
   const long long units = (long long)c->n_seq * c->n_kv_head * plan->tiles;
-  const long long capacity = (long long)c->page_size * c->max_pages;
   int e = 4;
   while (e > 0 && (units << e > slots.at[e] || capacity < 128 << e)) --e;
   if (kind < 2 && capacity > 1024 << e) e = 0;

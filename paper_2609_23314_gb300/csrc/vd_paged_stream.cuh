@@ -791,8 +791,8 @@ constexpr PagedKernel paged_stream() {
           Sh::kKeys};
 }
 
-// [(head_dim + 31) / 32 - 1][kind]: the streaming kernel with tiles of 8 and of 16 rows (where their
-// sums fit the registers), the block kernel
+// [(head_dim + 31) / 32 - 1][kind]: the streaming kernel with tiles of 8 and of 16 rows (bf16 pages,
+// where their sums fit the registers; else the first again), the block kernel
 constexpr int kKinds = 3;
 extern const PagedKernel kPagedBf16[8][kKinds], kPagedE4m3[8][kKinds];
 
