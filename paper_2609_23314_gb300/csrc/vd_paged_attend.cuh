@@ -54,7 +54,7 @@ struct SeqWork {
 };
 
 // What a unit costs beside its stages, in stages of a CTA: its queries, the meeting of the warps.
-constexpr int kUnitCost = 8;
+constexpr int kUnitCost = 16;
 
 __device__ __forceinline__ SeqWork seq_work(const PagedAttendArgs& a, int2 size) {
   SeqWork w;
@@ -107,6 +107,8 @@ struct Share {
   int slot;  // of the part; kWhole: the whole unit, kOfCluster: a part of the cluster's unit
 };
 
+constexpr int kFewSeqs = 128;  // so many a warp takes in at once
+
 // Sequences that a warp looks at together, one a lane.
 struct WalkMem {
   int first;
@@ -125,7 +127,7 @@ struct Walk {
   int seq, head, tile, in;  // in: the next position in the unit
   int2 size;                // of seq
 
-  // Where there are more than 32 sequences, all threads of the CTA come here first: the length
+  // Where there are more than kFewSeqs sequences, all threads of the CTA come here first: the length
   // of the line, and a sequence near the piece's first one.
   static __device__ long long survey(const PagedAttendArgs& a, WalkMem& m) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
@@ -165,16 +167,45 @@ struct Walk {
       : cut(), at(0), end(0), seq(0), head(0), tile(0), in(0), size() {
     int first = 0;
     long long begin = 0;
-    if (a.n_seq <= 32) {
-      load(a, m, 0, 0, blockIdx.x == 0);
-      all = m.end[31];
+    if (a.n_seq <= kFewSeqs) {
+      // all sequences, the lane's one of each 32, and where they end on the line
+      const int lane = threadIdx.x & 31;
+      int2 n[kFewSeqs / 32];
+      long long end_of[kFewSeqs / 32], before[kFewSeqs / 32];
+#pragma unroll
+      for (int i = 0; i < kFewSeqs / 32; ++i) {
+        const int s = 32 * i + lane;
+        n[i] = s < a.n_seq ? seq_size(a, s, blockIdx.x == 0) : make_int2(0, 0);
+      }
+      all = 0;
+#pragma unroll
+      for (int i = 0; i < kFewSeqs / 32; ++i) {
+        before[i] = all;
+        end_of[i] = 0;
+        if (32 * i < a.n_seq) {
+          end_of[i] = all + warp_scan_i64(line_length(a, n[i]));
+          all = __shfl_sync(kFull, end_of[i], 31);
+        }
+      }
+      cut = cut_of(all);
+      at = (int)blockIdx.x < cut.ctas ? cut.begin(blockIdx.x) : all;
+#pragma unroll
+      for (int i = 0; i < kFewSeqs / 32; ++i)
+        if (32 * i < a.n_seq && at >= before[i]) {  // the last that holds
+          first = 32 * i;
+          begin = before[i];
+          m.end[lane] = end_of[i];
+          m.size[lane] = n[i];
+        }
+      m.first = first;
+      __syncwarp();
+    } else {
+      cut = cut_of(all);
+      at = (int)blockIdx.x < cut.ctas ? cut.begin(blockIdx.x) : all;
     }
-    cut = cut_of(all);
-    if ((int)blockIdx.x >= cut.ctas) return;
-    at = cut.begin(blockIdx.x);
-    end = cut.begin(blockIdx.x + 1);
+    end = (int)blockIdx.x < cut.ctas ? cut.begin(blockIdx.x + 1) : at;
     if (at >= end) return;
-    if (a.n_seq > 32) {
+    if (a.n_seq > kFewSeqs) {
       first = m.found_seq;
       begin = m.found_at;
       load(a, m, first, begin, false);

@@ -233,7 +233,7 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
     }
   }
   long long all = 0;
-  if (a.cluster == 1 && a.n_seq > 32) all = Walk::survey(a, mem.walk);
+  if (a.cluster == 1 && a.n_seq > kFewSeqs) all = Walk::survey(a, mem.walk);
   __syncthreads();
   bool ok = true;
 
@@ -268,6 +268,10 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
       const int32_t* table = a.pages.table + (size_t)s.seq * a.pages.max_pages;
       const long long in = s.head * a.pages.head_stride + (kFixed ? lane % Sh::kChunks * 16 : 0);
       const char *k_head = a.pages.k + in, *v_head = a.pages.v + in;
+      if (p == 1 && lane < 2 * Sh::kRows) {  // its queries, which the other warps will want, into L2
+        const long long row = out_row(a, s, lane & (Sh::kRows - 1));
+        if (row >= 0) prefetch_l2(a.q + row * a.d + (lane < Sh::kRows ? 0 : a.d / 2));
+      }
       if (p > 0) {
         __syncwarp();
         if (lane == 0) bar_arrive(smem_addr(&mem.share_free[k % kShares]));
@@ -667,34 +671,34 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
         }
         if (r == 0) stats[warp * 8 + 2 * c + e] = make_float2(mx[t][e], sum[t][e]);
       }
-      __syncwarp();
-      if (lane == 0) bar_arrive(smem_addr(&mem.parts_full));
-#pragma unroll 1
-      for (int q = warp; q < 8; q += kW) {
-        const long long row = out_row(a, s, 8 * t + q);
-        if (row < 0) continue;
-        ok = ok && bar_wait(smem_addr(&mem.parts_full), met & 1, &mem.dead, a);
+      // Row q of the tile from all warps' parts, in their order
+      auto combine = [&](int q, long long row) {
+        float2 st[kW];
         float top = -INFINITY, total = 0.f, f[kW];
 #pragma unroll
-        for (int w = 0; w < kW; ++w) top = fmaxf(top, stats[w * 8 + q].x);
+        for (int w = 0; w < kW; ++w) st[w] = stats[w * 8 + q];
+#pragma unroll
+        for (int w = 0; w < kW; ++w) top = fmaxf(top, st[w].x);
 #pragma unroll
         for (int w = 0; w < kW; ++w) {
-          const float2 st = stats[w * 8 + q];
-          f[w] = st.x == -INFINITY ? 0.f : exp2_approx(st.x - top);
-          total += st.x == -INFINITY ? 0.f : f[w] * st.y;
+          // a warp that has seen nothing may have left nothing
+          f[w] = st[w].x == -INFINITY ? 0.f : exp2_approx(st[w].x - top);
+          total += st[w].x == -INFINITY ? 0.f : f[w] * st[w].y;
         }
         const float scale = whole ? (top == -INFINITY ? 0.f : vs / total) : vs;
         const size_t part = (size_t)s.slot * Sh::kRows + 8 * t + q;
         for (int d = 4 * lane; d < a.d; d += 128) {
-          float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+          float4 z[kW], y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int w = 0; w < kW; ++w)
+            z[w] = *reinterpret_cast<const float4*>(parts + (w * 8 + q) * Sh::kPart + d);
 #pragma unroll
           for (int w = 0; w < kW; ++w) {
-            const float4 z = *reinterpret_cast<const float4*>(parts + (w * 8 + q) * Sh::kPart + d);
-            if (stats[w * 8 + q].x == -INFINITY) continue;
-            y.x += f[w] * z.x;
-            y.y += f[w] * z.y;
-            y.z += f[w] * z.z;
-            y.w += f[w] * z.w;
+            const bool none = st[w].x == -INFINITY;
+            y.x += none ? 0.f : f[w] * z[w].x;
+            y.y += none ? 0.f : f[w] * z[w].y;
+            y.z += none ? 0.f : f[w] * z[w].z;
+            y.w += none ? 0.f : f[w] * z[w].w;
           }
           y = make_float4(y.x * scale, y.y * scale, y.z * scale, y.w * scale);
           if (whole)
@@ -711,6 +715,15 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
           else if (a.lse)
             a.lse[row] = (top + log2f(total)) * kLn2;
         }
+      };
+      __syncwarp();
+      if (lane == 0) bar_arrive(smem_addr(&mem.parts_full));
+#pragma unroll 1
+      for (int q = warp; q < 8; q += kW) {
+        const long long row = out_row(a, s, 8 * t + q);
+        if (row < 0) continue;
+        ok = ok && bar_wait(smem_addr(&mem.parts_full), met & 1, &mem.dead, a);
+        combine(q, row);
       }
       __syncwarp();
       if (lane == 0) bar_arrive(smem_addr(&mem.parts_free));
