@@ -195,7 +195,10 @@ vd_status plan_of(const vd_paged_cache* c, int n_q_head, int B, Plan* plan) {
   const long long units = (long long)c->n_seq * c->n_kv_head * plan->tiles;
   int e = 4;
   while (e > 0 && (units << e > slots.at[e] || capacity < 128 << e)) --e;
-  if (kind < 2 && capacity > 1024 << e) e = 0;
+  // Streaming: unless equal pieces are ahead, whose look at all lengths and whose join cost what 600
+  // slots of a CTA do.  us, clusters / pieces, one sequence, head_dim 128: 8 KV heads of 1024 slots
+  // 11.3 / 15.4, 8000 16.1 / 18.1, 16000 24.9 / 24.3; one KV head of 16000 17.4 / 15.4.
+  if (kind < 2 && capacity >> e > units * capacity / dev.sms + 600) e = 0;
   const int want = env_int("VD_PAGED_CLUSTER", -1);
   if (want == 1) e = 0;
   plan->cluster = 1 << e;
