@@ -456,8 +456,9 @@ vd_status vd_qkv_norm_rope(const void* qkv, int32_t n_seq, int32_t B, int32_t n_
  * Every call checks the cache: a null pointer, an extent below 1, a scale with bf16 pages, or a
  * stride that is smaller than a row (of an extent above 1) is VD_ERR_INVALID_ARG; rows that
  * are not 16-byte aligned (addresses, strides, head_dim) VD_ERR_ALIGNMENT; head_dim above 256,
- * more than 2^30 slots a sequence, 2^20 sequences, 65536 KV heads or 2^31 - 1 units (n_seq *
- * n_layer * n_kv_head) VD_ERR_UNSUPPORTED.
+ * more than 2^30 slots a sequence, 2^20 sequences, 65536 KV heads, 2^31 - 1 units (n_seq *
+ * n_layer * n_kv_head), or a layer whose K or V reaches over 2^36 - 4096 bytes or more,
+ * VD_ERR_UNSUPPORTED.
  * On the device, a sequence whose len, or len and new tokens, lie out of
  * [0, max_pages * page_size], or whose n_new lies out of [0, B], gets no row and no output
  * (VD_ERR_DEVICE_LEN).  A page out of [0, n_page) is neither read nor written
@@ -520,14 +521,15 @@ vd_status vd_paged_append(const vd_paged_cache* c, int32_t layer, const void* qk
  *                 sequence are joined there.  Its content means nothing between calls; calls
  *                 that may run at the same time (on two streams, in two graphs) need one each.
  * A token that sees no slot, or whose scores are all -infinity, gets out = 0 and lse = -inf.
- * Values that a token does not see do not reach it, NaN and infinities among them.  Scores,
- * softmax statistics and sums are fp32; weights are rounded to two bf16 parts (2^-16 of
- * themselves) for bf16 pages and to fp16 for e4m3 ones, where those below 2^-36 of the largest
- * count for nothing.
- * Range: products q . k and sums of values times weights of up to 2^8 have to be finite in fp32;
- * with e4m3 pages, scale times the scales and a query row's largest magnitude has to lie in
- * [2^-60, 2^60].
- * The same inputs give the same bits on the same GPU.  out must not overlap the inputs. */
+ * Values that a token does not see do not reach it, NaN and infinities among them; one that it
+ * sees gives NaN (a NaN, or an infinity whose weight is 0) or an infinity.  Scores, softmax
+ * statistics and sums are fp32; weights are rounded to two bf16 parts (2^-16 of themselves) for
+ * bf16 pages and to fp16 for e4m3 ones, where those below 2^-36 of the largest count for nothing.
+ * Range: scores, products of a query's and a key's values, and sums of values times weights of up
+ * to 2^15 have to be finite in fp32; scale times a query row's largest magnitude (times the keys'
+ * scale, with e4m3 pages) has to lie in [2^-60, 2^60].
+ * VD_ERR_TIMEOUT: the outputs are unspecified.  The same inputs and lengths give the same bits on
+ * the same GPU.  out must not overlap the inputs. */
 vd_status vd_paged_attend(const vd_paged_cache* c, int32_t layer, const void* q, int32_t B,
                           int32_t n_q_head, const int32_t* n_new, int32_t causal, float scale,
                           void* out, float* lse_out, void* workspace, size_t workspace_bytes,

@@ -51,14 +51,6 @@ __device__ __forceinline__ void unpack8(const uint4& q, float (&x)[8]) {
   x[7] = __uint_as_float(q.w & 0xffff0000u);
 }
 
-__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
-  uint32_t o[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[i]) : "f"(x[2 * i + 1]), "f"(x[2 * i]));
-  return make_uint4(o[0], o[1], o[2], o[3]);
-}
-
 // ---------------------------------------------------------------------------
 // Packed fp32 pairs: the sm_100-family f32x2 add/fma instructions do two
 // fp32 operations (each rounded as the scalar one) per issue slot.  A pair

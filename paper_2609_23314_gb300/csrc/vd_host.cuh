@@ -26,8 +26,6 @@ vd_status validate_q4(const vd_q4_cache* c);
 // Polls after which a device wait gives up (VD_WAIT_LIMIT lowers it, for tests).
 uint32_t wait_limit();
 
-inline bool misaligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
-
 // The environment variable's number, or `unset`.
 int env_int(const char* name, int unset);
 

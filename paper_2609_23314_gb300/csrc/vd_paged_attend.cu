@@ -14,6 +14,7 @@
 #include "vd_paged.cuh"
 #include "vd_paged_attend.cuh"
 #include "vd_paged_stream.cuh"
+#include "vd_qkv.cuh"
 
 namespace vd {
 

@@ -36,6 +36,14 @@ __device__ __forceinline__ float half_turns(double pos, float inv_freq) {
   return (float)(t - 2.0 * rint(0.5 * t));
 }
 
+__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
+  uint32_t o[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[i]) : "f"(x[2 * i + 1]), "f"(x[2 * i]));
+  return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
 // A thread holds two 8-value chunks of a head that turn together: chunks j and
 // j + rotary_dim / 16 (pairs (i, i + rotary_dim / 2)), or, interleaved, 2 j and 2 j + 1;
 // behind rotary_dim, neighbours.  `lanes` threads hold a head and share the sum of its
@@ -159,6 +167,8 @@ __device__ __forceinline__ void norm_rope_tokens(const QkvArgs& a, float* table,
     }
   }
 }
+
+inline bool misaligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
 // What both calls check of the arguments that they share, before any launch.
 inline vd_status validate_qkv(const void* qkv, int n_seq, int B, int n_q, int n_kv, int d,
