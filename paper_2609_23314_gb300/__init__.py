@@ -338,6 +338,7 @@ class PagedCache:
                                 self.n_page, self.max_pages)
         self._ref = ctypes.byref(self._s)
         self._gpu = self.device.type == "cuda"
+        self._vector = (self.n_seq,)
 
     @classmethod
     def empty(cls, n_seq, n_layer, n_kv_head, head_dim, n_page, page_size, max_pages, dtype=None,
@@ -704,6 +705,18 @@ def vd_qkv_norm_rope(qkv, q_out, k_new, v_new, layer: int = 0, q_weight=None, k_
            "vd_qkv_norm_rope")
 
 
+def _paged_stream(cache: PagedCache, stream):
+    """_launch_stream for a cache that is on a GPU, where CUDA is up."""
+    if not cache._gpu:
+        return None
+    C = _torch()._C
+    index = C._cuda_getDevice()
+    if cache.device.index != index:
+        raise ValueError(f"the tensors live on {cache.device}, the current device is cuda:{index}")
+    raw = getattr(C, "_cuda_getCurrentRawStream", None)
+    return raw(index) if stream is None and raw is not None else _stream(stream)
+
+
 def vd_paged_append(cache: PagedCache, qkv, q_out, layer: int = 0, q_weight=None, k_weight=None,
                     eps: float = 1e-6, inv_freq=None, pos_first_new=None,
                     interleaved: bool = False, n_new=None, stream=None) -> None:
@@ -711,26 +724,29 @@ def vd_paged_append(cache: PagedCache, qkv, q_out, layer: int = 0, q_weight=None
     paged cache (n_new int32 [n_seq], or None: all B); without pos_first_new a token's
     position is its slot.  len stays until vd_paged_advance."""
     torch = _torch()
-    if qkv.dim() != 4 or q_out.dim() != 4:
+    shape = qkv.shape
+    if len(shape) != 4 or q_out.dim() != 4:
         raise ValueError("qkv and q_out must have 4 dimensions")
-    dev, n_seq, d = cache.device, cache.n_seq, cache.head_dim
-    s = _launch_stream(dev, stream)
-    _, B, heads, _ = qkv.shape
+    dev, n_seq, d, bf16 = cache.device, cache.n_seq, cache.head_dim, torch.bfloat16
+    s = _paged_stream(cache, stream)
+    B, heads = shape[1], shape[2]
     n_q = heads - 2 * cache.n_kv_head
     pairs = 0 if inv_freq is None else inv_freq.numel()
     args = (
-        _ptr(qkv, torch.bfloat16, (n_seq, B, heads, d), "qkv", dev),
-        _ptr(n_new, torch.int32, (n_seq,), "n_new", dev),
-        _ptr(q_weight, torch.bfloat16, (d,), "q_weight", dev),
-        _ptr(k_weight, torch.bfloat16, (d,), "k_weight", dev),
-        _ptr(inv_freq, torch.float32, (pairs,), "inv_freq", dev),
-        _ptr(pos_first_new, torch.int32, (n_seq,), "pos_first_new", dev),
-        _ptr(q_out, torch.bfloat16, (n_seq, B, n_q, d), "q_out", dev),
+        _ptr(qkv, bf16, (n_seq, B, heads, d), "qkv", dev),
+        None if n_new is None else _ptr(n_new, torch.int32, cache._vector, "n_new", dev),
+        None if q_weight is None else _ptr(q_weight, bf16, (d,), "q_weight", dev),
+        None if k_weight is None else _ptr(k_weight, bf16, (d,), "k_weight", dev),
+        None if inv_freq is None else _ptr(inv_freq, torch.float32, (pairs,), "inv_freq", dev),
+        None if pos_first_new is None else _ptr(pos_first_new, torch.int32, cache._vector,
+                                                "pos_first_new", dev),
+        _ptr(q_out, bf16, (n_seq, B, n_q, d), "q_out", dev),
     )
-    _check(load_library().vd_paged_append(cache.ref(), int(layer), args[0], B, n_q, args[1],
-                                          args[2], args[3], float(eps), args[4], 2 * pairs,
-                                          int(bool(interleaved)), args[5], args[6], s),
-           "vd_paged_append")
+    code = load_library().vd_paged_append(cache.ref(), int(layer), args[0], B, n_q, args[1], args[2],
+                                          args[3], float(eps), args[4], 2 * pairs, bool(interleaved),
+                                          args[5], args[6], s)
+    if code:
+        raise VdError(code, "vd_paged_append")
 
 
 def vd_paged_attend_workspace(cache: PagedCache, n_q_head: int, B: int) -> int:
@@ -748,23 +764,23 @@ def vd_paged_attend(cache: PagedCache, q, out, workspace, layer: int = 0, causal
     fp32 [n_seq, B, n_q_head]."""
     torch = _torch()
     dev = cache.device
-    s = _launch_stream(dev, stream)
+    s = _paged_stream(cache, stream)
     if q.dim() != 4:
         raise ValueError("q must be [n_seq, B, n_q_head, head_dim]")
     _, B, n_q, _ = q.shape
-    shape = (cache.n_seq, B, n_q, cache.head_dim)
+    shape, size = (cache.n_seq, B, n_q, cache.head_dim), workspace.numel()
     args = (
         _ptr(q, torch.bfloat16, shape, "q", dev),
-        _ptr(n_new, torch.int32, (cache.n_seq,), "n_new", dev),
+        None if n_new is None else _ptr(n_new, torch.int32, cache._vector, "n_new", dev),
         _ptr(out, torch.bfloat16, shape, "out", dev),
-        _ptr(lse_out, torch.float32, shape[:3], "lse_out", dev),
-        _ptr(workspace, torch.uint8, (workspace.numel(),), "workspace", dev),
+        None if lse_out is None else _ptr(lse_out, torch.float32, shape[:3], "lse_out", dev),
+        _ptr(workspace, torch.uint8, (size,), "workspace", dev),
     )
     scale = cache.head_dim ** -0.5 if scale is None else float(scale)
-    _check(load_library().vd_paged_attend(cache.ref(), int(layer), args[0], B, n_q, args[1],
-                                          int(bool(causal)), scale, args[2], args[3], args[4],
-                                          workspace.numel(), s),
-           "vd_paged_attend")
+    code = load_library().vd_paged_attend(cache.ref(), int(layer), args[0], B, n_q, args[1],
+                                          bool(causal), scale, args[2], args[3], args[4], size, s)
+    if code:
+        raise VdError(code, "vd_paged_attend")
 
 
 def vd_paged_advance(cache: PagedCache, B: int = 1, n_new=None, stream=None) -> None:

@@ -175,17 +175,14 @@ __device__ __forceinline__ bool not_finite(uint32_t w) {
 }
 
 // Two weights in bf16, and in `low` what that leaves of them: together within 2^-16 of a weight.
-// Both parts of a weight whose upper one is not 0 are above 0 (low ones at least 2^-133), so that
-// an infinite value stays one.
+// The upper part is rounded towards zero and the lower one is of 2^-20 of the weight more, so that
+// both are above 0 where the weight is (but for weights below 2^-113): an infinite value stays one.
 __device__ __forceinline__ uint32_t split_weights(float x, float y, uint32_t& low) {
-  uint32_t high;
-  asm("cvt.rz.bf16x2.f32 %0, %1, %2;" : "=r"(high) : "f"(y), "f"(x));
-  float lx, ly;
-  f2_unpack(f2_add(f2_pack(x, y), f2_pack(__uint_as_float(high << 16 ^ 0x80000000u),
-                                          __uint_as_float((high & 0xffff0000u) ^ 0x80000000u))),
-            lx, ly);
-  low = pack_bf16(lx, ly) | __vminu2(high, 0x00010001u);
-  return high;
+  uint32_t minus;
+  asm("cvt.rz.bf16x2.f32 %0, %1, %2;" : "=r"(minus) : "f"(-y), "f"(-x));
+  low = pack_bf16(fmaf(x, 1.f + 0x1p-20f, __uint_as_float(minus << 16)),
+                  fmaf(y, 1.f + 0x1p-20f, __uint_as_float(minus & 0xffff0000u)));
+  return minus ^ 0x80008000u;
 }
 
 template <int M, int NT, bool E4M3>
