@@ -106,7 +106,7 @@ struct PagedRows {
 };
 
 template <bool INTERLEAVED, bool E4M3, bool FEW>
-__global__ void __launch_bounds__(kThreads, FEW ? 2 : E4M3 ? 4 : 5) paged_append_kernel(QkvArgs a, PagedRowsArgs p) {
+__global__ void __launch_bounds__(kThreads, FEW ? 2 : E4M3 ? 3 : 5) paged_append_kernel(QkvArgs a, PagedRowsArgs p) {
   extern __shared__ __align__(16) float table[];
   __shared__ long long rows[kMaxTokens];
   norm_rope_tokens<INTERLEAVED, FEW>(a, table, PagedRows<E4M3>{a, p, rows});

@@ -44,6 +44,15 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
   return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
+// x times r times w, rounded after each.
+__device__ __forceinline__ void scale8(float (&x)[8], float r, const uint4& w) {
+  const uint32_t in[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    f2_unpack(f2_mul(f2_mul(f2_pack(x[2 * e], x[2 * e + 1]), f2_pack(r, r)), bf16x2_to_f2(in[e])),
+              x[2 * e], x[2 * e + 1]);
+}
+
 // A thread holds two 8-value chunks of a head that turn together: chunks j and
 // j + rotary_dim / 16 (pairs (i, i + rotary_dim / 2)), or, interleaved, 2 j and 2 j + 1;
 // behind rotary_dim, neighbours.  `lanes` threads hold a head and share the sum of its
@@ -104,8 +113,17 @@ __device__ __forceinline__ void norm_rope_tokens(const QkvArgs& a, float* table,
     table[t * a.rd + half + f] = sn;
   }
   __syncthreads();
-  for (int it = threadIdx.x / a.lanes; it < items; it += slots) {
-    const int t = it / heads, h = it % heads;
+  const int dt = slots / heads, dh = slots - dt * heads;  // of a round
+  int t = (int)(threadIdx.x / a.lanes) / heads, h = (int)(threadIdx.x / a.lanes) - t * heads;
+  auto advance = [&] {
+    t += dt;
+    h += dh;
+    if (h >= heads) {
+      h -= heads;
+      ++t;
+    }
+  };
+  for (int it = threadIdx.x / a.lanes; it < items; it += slots, advance()) {
     const uint4 w0 = n0, w1 = n1;
     fetch(it + slots);
     if (!sink.on(t)) continue;
@@ -122,16 +140,13 @@ __device__ __forceinline__ void norm_rope_tokens(const QkvArgs& a, float* table,
         const unsigned mask = ((1u << a.lanes) - 1u) << (lane & ~(a.lanes - 1u));  // <= 16 lanes
         for (int off = a.lanes >> 1; off > 0; off >>= 1) ss += __shfl_xor_sync(mask, ss, off);
         const float r = 1.f / sqrtf(ss / (float)a.d + a.eps);
-        float g[8];
         if (active) {
-          unpack8(FEW ? (h < a.n_q ? early[0][0] : early[1][0]) : *reinterpret_cast<const uint4*>(wt + c0 * 8), g);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = x[e] * r * g[e];
+          scale8(x, r, FEW ? (h < a.n_q ? early[0][0] : early[1][0])
+                           : *reinterpret_cast<const uint4*>(wt + c0 * 8));
         }
         if (second) {
-          unpack8(FEW ? (h < a.n_q ? early[0][1] : early[1][1]) : *reinterpret_cast<const uint4*>(wt + c1 * 8), g);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = y[e] * r * g[e];
+          scale8(y, r, FEW ? (h < a.n_q ? early[0][1] : early[1][1])
+                           : *reinterpret_cast<const uint4*>(wt + c1 * 8));
         }
       }
       if (j < rot8 / 2) {
