@@ -96,11 +96,13 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(PagedAttendArgs a)
   if (threadIdx.x == 0 && a.lse) a.lse[row] = (top + log2f(sum)) * kLn2;
 }
 
-// CTAs of a kernel that run at once on a device, in clusters of 1, 2, 4, 8, 16 (0: such a
-// cluster does not fit); asked for once per device and kernel.
+// Clusters of 1 to 16 CTAs of a kernel that run at once on a device; asked for once per device and
+// kernel.  They do not go by powers of two: 152 SMs hold 15 of 8 or of 9, 8 of 12, 7 of 16.
+constexpr int kMaxCluster = 16;
+
 struct Slots {
   bool ready;
-  int at[5];
+  int at[kMaxCluster + 1];
 };
 std::mutex g_slots_mu;
 Slots g_slots[64][2][8][kKinds];
@@ -115,25 +117,25 @@ vd_status slots_of(const DeviceInfo& dev, const PagedKernel& k, Slots& s) {
     cudaGetLastError();
     return VD_ERR_CUDA;
   }
-  for (int e = 0; e < 5; ++e) {
+  for (int n = 1; n <= kMaxCluster; ++n) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(16 * dev.sms);
+    cfg.gridDim = dim3(n * dev.sms);
     cfg.blockDim = dim3(k.threads);
     cfg.dynamicSmemBytes = k.smem;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = 1u << e;
+    attr.val.clusterDim.x = (unsigned)n;
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, k.kern, &cfg) != cudaSuccess) {
+    int active = 0;
+    if (cudaOccupancyMaxActiveClusters(&active, k.kern, &cfg) != cudaSuccess) {
       cudaGetLastError();
-      n = 0;
+      active = 0;
     }
-    s.at[e] = n << e;
+    s.at[n] = active;
   }
-  if (s.at[0] < 1) return VD_ERR_CUDA;
+  if (s.at[1] < 1) return VD_ERR_CUDA;
   s.ready = true;
   return VD_OK;
 }
@@ -192,20 +194,22 @@ vd_status plan_of(const vd_paged_cache* c, int n_q_head, int B, Plan* plan) {
   plan->status = dev.status;
   plan->rows = k.rows;
   plan->tiles = (int)((rows + k.rows - 1) / k.rows);
-  // A cluster for each unit: the largest with which they run at once
+  // A cluster for each unit: the largest with which they run at once and whose CTAs have slots enough
+  // to pay for the join, large clusters more of them.  us, 8 KV heads, clusters of 8 / 12: 4096 slots
+  // 11.2 / 11.7, 16000 25.0 / 20.2.
   const long long units = (long long)c->n_seq * c->n_kv_head * plan->tiles;
-  int e = 4;
-  while (e > 0 && (units << e > slots.at[e] || capacity < 128 << e)) --e;
+  int n = kMaxCluster;
+  while (n > 1 && (units > slots.at[n] || capacity < (n > 8 ? 512 : 128) * n)) --n;
   // Streaming: unless equal pieces are ahead, whose look at all lengths and whose join cost what 600
   // slots of a CTA do.  us, clusters / pieces, one sequence, head_dim 128: 8 KV heads of 1024 slots
-  // 11.3 / 15.4, 8000 16.1 / 18.1, 16000 24.9 / 24.3; one KV head of 16000 17.4 / 15.4.
-  if (kind < 2 && capacity >> e > units * capacity / dev.sms + 600) e = 0;
+  // 11.3 / 15.1, 8000 16.1 / 18.1, 16000 20.2 / 25.0; one KV head of 16000 17.4 / 15.4.
+  if (kind < 2 && capacity / n > units * capacity / dev.sms + 600) n = 1;
   const int want = env_int("VD_PAGED_CLUSTER", -1);
-  if (want == 1) e = 0;
-  plan->cluster = 1 << e;
-  plan->one_launch = e > 0 || kind == 2;
-  if (units << e > INT_MAX) return VD_ERR_UNSUPPORTED;
-  plan->ctas = plan->one_launch ? (int)(units << e) : slots.at[0];
+  if (want >= 1 && want <= kMaxCluster && slots.at[want] > 0) n = want;
+  plan->cluster = n;
+  plan->one_launch = n > 1 || kind == 2;
+  if (units * n > INT_MAX) return VD_ERR_UNSUPPORTED;
+  plan->ctas = plan->one_launch ? (int)(units * n) : slots.at[1];
   const size_t parts = plan->one_launch ? 0 : 2 * (size_t)plan->ctas * plan->rows;
   plan->split = plan->one_launch ? 0 : (size_t)plan->ctas * sizeof(int4);
   plan->stats = parts * sizeof(float2);
@@ -266,7 +270,6 @@ vd_status vd_paged_attend(const vd_paged_cache* c, int32_t layer, const void* q,
   a.wait_limit = wait_limit();
   a.row_shift = log2(p.rows);
   a.stage_shift = log2(p.kernel->stage_keys);
-  a.cluster_shift = log2(p.cluster);
   a.causal = causal != 0;
   a.scale = scale;
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);

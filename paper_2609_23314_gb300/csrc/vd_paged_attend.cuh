@@ -37,8 +37,8 @@ struct PagedAttendArgs {
   int n_seq, heads, group, B, d;
   int rows;              // of a tile, a power of two
   int tiles;             // of B tokens
-  int cluster;           // CTAs that share a unit, a power of two, or 1: pieces of the line
-  int row_shift, stage_shift, cluster_shift;  // log2 of rows, of a stage's slots, of cluster
+  int cluster;           // CTAs that share a unit, at most 16, or 1: pieces of the line
+  int row_shift, stage_shift;  // log2 of rows, of a stage's slots
   int causal;
   float scale;
   uint32_t page16, slot16;  // strides of the pages in 16 bytes (where a layer's rows lie fits 32 bits)
@@ -289,7 +289,7 @@ __device__ __forceinline__ int seen_slots(const PagedAttendArgs& a, const Share&
 // The share of a CTA of a cluster, with no stage where there are fewer than CTAs; false: the unit
 // has nothing to do.
 __device__ __forceinline__ bool cluster_share(const PagedAttendArgs& a, Share& s) {
-  const int rank = blockIdx.x & (a.cluster - 1), unit = blockIdx.x >> a.cluster_shift;
+  const int unit = blockIdx.x / a.cluster, rank = blockIdx.x - unit * a.cluster;
   const int head = unit / a.tiles;
   s.tile = unit - head * a.tiles;
   s.seq = head / a.heads;
@@ -298,8 +298,8 @@ __device__ __forceinline__ bool cluster_share(const PagedAttendArgs& a, Share& s
   const SeqWork w = seq_work(a, n);
   s.len = n.x;
   s.add = n.y;
-  s.s0 = (int)((uint32_t)(w.stages * rank) >> a.cluster_shift);  // below 2^26 stages, 17 ranks
-  s.s1 = (int)((uint32_t)(w.stages * (rank + 1)) >> a.cluster_shift);
+  s.s0 = (int)((uint32_t)(w.stages * rank) / a.cluster);  // below 2^26 stages, 17 ranks
+  s.s1 = (int)((uint32_t)(w.stages * (rank + 1)) / a.cluster);
   s.slot = kOfCluster;
   return s.tile < w.tiles && w.total > 0;
 }

@@ -218,7 +218,7 @@ __global__ void __launch_bounds__((StreamShape<M, NT, E4M3>::kStreamThreads), 1)
   grid_launch_dependents();
   if (a.cluster > 1) {
     // queries and the table, which a wait for the length need not delay, into L2
-    const int unit = blockIdx.x >> a.cluster_shift, head = unit / a.tiles, seq = head / a.heads;
+    const int unit = blockIdx.x / a.cluster, head = unit / a.tiles, seq = head / a.heads;
     const int line = threadIdx.x - 32, row = (unit - head * a.tiles) * Sh::kRows + (lane & (Sh::kRows - 1));
     if (warp == 0 && row < a.B * a.group) {
       const int tok = row / a.group;

@@ -40,8 +40,8 @@ struct BlockPlace {
     keys = row0 >= rows_all ? 0 : size.x + (a.causal ? last + 1 : 0);
     all_see = size.x + (a.causal ? row0 / a.group + 1 : 0);
     const int tiles = (keys + kKeys - 1) / kKeys;
-    t0 = (int)((uint32_t)(tiles * rank) >> a.cluster_shift);
-    count = (int)((uint32_t)(tiles * (rank + 1)) >> a.cluster_shift) - t0;
+    t0 = (int)((uint32_t)(tiles * rank) / a.cluster);  // below 2^24 tiles, 17 ranks
+    count = (int)((uint32_t)(tiles * (rank + 1)) / a.cluster) - t0;
   }
 };
 
@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
   const uint32_t base = (raw_base + 1023u) & ~1023u;
   unsigned char* smem = smem_raw + (base - raw_base);
   const int warp = threadIdx.x >> 5;
-  const int rank = blockIdx.x & (a.cluster - 1), item = blockIdx.x >> a.cluster_shift;
+  const int item = blockIdx.x / a.cluster, rank = blockIdx.x - item * a.cluster;
   const int unit = item / a.tiles, tile = item - unit * a.tiles;
   const int seq = unit / a.heads, head = unit - seq * a.heads;
 
@@ -598,11 +598,12 @@ __global__ void __launch_bounds__(kTileThreads, 1)
   // Each CTA writes its share of the rows (those that are there), from all CTAs' results in
   // rank order: first every CTA's factor for every row of the share, then the sums.
   const int rows = max(0, min(kTileRows, rows_all - row0));
-  const int share = (rows + a.cluster - 1) >> a.cluster_shift;
+  const int share = (rows + a.cluster - 1) / a.cluster;
   const int r0 = rank * share, mine = max(0, min(share, rows - r0));
   const uint32_t stats = base + Sh::kStats;
-  float* factor = reinterpret_cast<float*>(smem + Sh::kFactors);  // [cluster][share], maxima first
-  float* sums = reinterpret_cast<float*>(smem + Sh::kSwap);       // the same
+  // [cluster][share], at most 128 + 15, maxima first, and the same of sums (kSwap follows kFactors)
+  float* factor = reinterpret_cast<float*>(smem + Sh::kFactors);
+  float* sums = reinterpret_cast<float*>(smem + Sh::kSwap) + 16;
   for (int i = threadIdx.x; i < mine * a.cluster; i += kTileThreads) {
     const int q = i / mine, r = i % mine;
     factor[q * share + r] = ld_cluster_f32(mapa(stats + 4 * (r0 + r), q));

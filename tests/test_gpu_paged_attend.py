@@ -29,6 +29,8 @@ def _lib():
 ROUTES = {"automatic": {}, "pieces": dict(VD_PAGED_CLUSTER="1"),
           "tiles_of_16": dict(VD_PAGED_KERNEL="1", VD_PAGED_CLUSTER="1"),
           "block": dict(VD_PAGED_KERNEL="2"),
+          "clusters_of_3": dict(VD_PAGED_KERNEL="0", VD_PAGED_CLUSTER="3"),
+          "block_clusters_of_7": dict(VD_PAGED_KERNEL="2", VD_PAGED_CLUSTER="7"),
           "block_alone": dict(VD_PAGED_KERNEL="2", VD_PAGED_CLUSTER="1")}
 
 
