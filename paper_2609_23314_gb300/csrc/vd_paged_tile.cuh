@@ -13,6 +13,11 @@
 //   12-14 V's tiles, the same;
 //   15    one thread issues the products.
 // A cluster splits the tiles of a unit and joins the results through distributed shared memory.
+//
+// 128 new tokens over 2048, 8 KV heads of 4 query heads, 21 us: start and queries 4, 5 tiles of 2.2
+// (softmax 2000 cycles a tile of 128 slots, most of it the exponentials; the products 2300, of which
+// the weights' lower parts are 800), the join.  8 sequences of 4000 slots, 16 rows 39 us (3.4 TB/s).
+// Copies by lanes with a fixed chunk of every row: 26 us without.
 #pragma once
 
 #include <cstdint>
