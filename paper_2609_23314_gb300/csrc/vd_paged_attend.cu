@@ -22,43 +22,61 @@ namespace {
 
 constexpr int kMaxDim = 256;
 
-// A CTA puts together one row of the unit that CTA `first` of the kernel before begins and
-// does not end: its warps take parts in turn, a lane 4 values, or 8.  4 us behind the kernel, of which
-// an empty launch is 1.
-__global__ void __launch_bounds__(kThreads) paged_join_kernel(PagedAttendArgs a) {
+// Puts together the rows of units that a CTA of the kernel before begins and another one ends.  A block
+// for every kWarps rows of each of those CTAs.  A unit of up to kWarps parts: the blocks of the CTA that
+// begins it, a warp a row, without a meeting.  Of more: the CTAs after that one are in the unit too and
+// begin none, so that their blocks help: a block a row, its warps take the parts in turn (one unit over
+// all CTAs would be 150 parts for a warp).  A lane has 4 of the row's values, or 8.  Against a block a
+// row everywhere: 32 sequences of 4000 tokens, 8 heads, 131.1 us (132.5), 40 of 300 tokens with one of
+// 100000 35.2 (36.6), 100 of 200 with one of 50000 28.4 (26.9).
+constexpr int kTogether = 4;  // parts that a warp loads at once
+
+__global__ void __launch_bounds__(kThreads)
+    paged_join_kernel(const __grid_constant__ PagedAttendArgs a) {
   __shared__ float4 part[kWarps][kMaxDim / 4];
   __shared__ float2 stat[kWarps];
   grid_dependency_wait();
   grid_launch_dependents();
-  const int first = blockIdx.x / a.rows, i = blockIdx.x % a.rows;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int4 unit = __ldcg(a.split + first);
-  if (unit.x < 0 || i >= unit.z) return;
+  const int at = blockIdx.x * kWarps >> a.row_shift, sub = blockIdx.x * kWarps & (a.rows - 1);
+  // the last unit begun by one of the kWarps CTAs up to `at`
+  int4 unit = make_int4(-1, 0, 0, 0);
+  if (lane < kWarps && lane <= at) unit = __ldcg(a.split + (at - lane));
+  const uint32_t begun = __ballot_sync(0xffffffffu, unit.x >= 0);
+  if (begun == 0) return;
+  const int back = __ffs(begun) - 1, first = at - back;
+  unit = make_int4(__shfl_sync(0xffffffffu, unit.x, back), __shfl_sync(0xffffffffu, unit.y, back),
+                   __shfl_sync(0xffffffffu, unit.z, back), __shfl_sync(0xffffffffu, unit.w, back));
+  const int n = unit.w - first + 1;
+  const bool many = n > kWarps;
+  if (!many && back > 0) return;
+  const int i = many ? ((back << a.row_shift) + sub) / kWarps : sub + warp;
+  if (i >= unit.z) return;
+  const int begin = many ? warp : 0, step = many ? kWarps : 1;
   const int tok = (unit.y + i) / a.group, g = unit.y + i - tok * a.group;
   const long long row = unit.x + (long long)tok * a.heads * a.group + g;
-  const int n = unit.w - first + 1;
   float2 total = make_float2(-INFINITY, 0.f);
   float y[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) y[e] = 0.f;
-  for (int p0 = warp; p0 < n; p0 += 2 * kWarps) {
-    float2 st[2];
-    float4 v[2][2];
+  for (int p0 = begin; p0 < n; p0 += kTogether * step) {
+    float2 st[kTogether];
+    float4 v[kTogether][2];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {  // loads of two parts together
-      const int p = p0 + j * kWarps;
-      const size_t at = (size_t)(2 * (first + p) + (p == 0 ? 1 : 0)) * a.rows + i;
+    for (int j = 0; j < kTogether; ++j) {
+      const int p = p0 + j * step;
+      const size_t from = (size_t)(2 * (first + p) + (p == 0 ? 1 : 0)) * a.rows + i;
       st[j] = make_float2(-INFINITY, 0.f);
       if (p < n) {
-        st[j] = __ldcg(a.stats + at);
+        st[j] = __ldcg(a.stats + from);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
           if (128 * h + 4 * lane < a.d)
-            v[j][h] = __ldcg(reinterpret_cast<const float4*>(a.parts + at * a.d + 128 * h + 4 * lane));
+            v[j][h] = __ldcg(reinterpret_cast<const float4*>(a.parts + from * a.d + 128 * h + 4 * lane));
       }
     }
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < kTogether; ++j) {
       if (st[j].x == -INFINITY) continue;  // nothing seen
       const float m = fmaxf(total.x, st[j].x);
       const float f = total.x == -INFINITY ? 0.f : exp2_approx(total.x - m);
@@ -73,6 +91,17 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(PagedAttendArgs a)
           y[4 * h + 3] = y[4 * h + 3] * f + w * v[j][h].w;
         }
     }
+  }
+  if (!many) {
+    const float inverse = total.x == -INFINITY ? 0.f : 1.f / total.y;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (128 * h + 4 * lane < a.d)
+        *reinterpret_cast<uint2*>(a.out + row * a.d + 128 * h + 4 * lane) =
+            make_uint2(pack_bf16(y[4 * h] * inverse, y[4 * h + 1] * inverse),
+                       pack_bf16(y[4 * h + 2] * inverse, y[4 * h + 3] * inverse));
+    if (lane == 0 && a.lse) a.lse[row] = (total.x + log2f(total.y)) * kLn2;
+    return;
   }
   part[warp][lane] = make_float4(y[0], y[1], y[2], y[3]);
   part[warp][32 + lane] = make_float4(y[4], y[5], y[6], y[7]);
@@ -280,7 +309,8 @@ vd_status vd_paged_attend(const vd_paged_cache* c, int32_t layer, const void* q,
   r = launch_clusters((unsigned)p.ctas, (unsigned)k.threads, (unsigned)p.cluster, k.smem, s, k.kern,
                       a);
   if (r != VD_OK || p.one_launch) return r;
-  return launch_dependent((unsigned)(p.ctas * p.rows), s, paged_join_kernel, a);
+  // rows are 8 or 16, kWarps or twice that
+  return launch_dependent((unsigned)(p.ctas * p.rows / kWarps), s, paged_join_kernel, a);
 }
 
 }  // extern "C"

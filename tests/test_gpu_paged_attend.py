@@ -122,6 +122,17 @@ def test_long_sequences():
     check_attend(c, queries(3, 1, 4, 64))
 
 
+@pytest.mark.parametrize("G", [3, 8, 16])
+def test_one_long_sequence_among_short_ones(G):
+    """Units of few parts and one of many in a call; the long one first, in the middle and last."""
+    for at, length in ((0, 1500), (50, 3100), (50, 6000), (99, 12000), (50, 40000)):
+        lens = [(i * 61) % 300 for i in range(100)]
+        lens[at] = length
+        c = ref.cache([m + 1 for m in lens], 1, 1, 64, 16)
+        c.len -= 1
+        check_attend(c, queries(100, 1, G, 64))
+
+
 def test_more_sequences_than_threads():
     lens = [(i * 37) % 23 for i in range(700)]
     c = ref.cache([m + 2 for m in lens], 1, 2, 32, 8)
