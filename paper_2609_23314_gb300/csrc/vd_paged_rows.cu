@@ -154,14 +154,16 @@ __global__ void __launch_bounds__(kThreads, PACK && E4M3 ? 2 : 3) paged_copy_ker
   grid_launch_dependents();
   const int chunks = a.d / 8, rows = kThreads / chunks, per_block = rows * kRowsInFlight;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  // blocks of a sequence, none where its length is out of range
-  auto blocks_of = [&](int s, bool report) {
+  // Rows of a sequence, none where either side is too short for its length: what the line is cut by,
+  // and what the walk along it goes by, which passes over refused sequences too.
+  auto rows_of = [&](int s, bool report) {
     if (s >= a.n_seq) return 0;
     const int n = __ldcg(a.len_in + s);
-    if (n >= 0 && n <= a.cap && n <= a.pages.capacity()) return (n + per_block - 1) / per_block;
+    if (n >= 0 && n <= a.cap && n <= a.pages.capacity()) return n;
     if (report) record_status(a.pages.status, kStDeviceLen);
     return 0;
   };
+  auto blocks_of = [&](int n) { return (n + per_block - 1) / per_block; };
   // sum over the CTA's threads up to this one, and over all
   auto scan = [&](long long x, long long& all) {
     const long long upto = warp_scan_i64(x);
@@ -180,10 +182,10 @@ __global__ void __launch_bounds__(kThreads, PACK && E4M3 ? 2 : 3) paged_copy_ker
   long long all = 0, upto = 0, mine = 0;
   if (a.n_seq > kThreads) {
     long long x = 0;
-    for (int s = threadIdx.x; s < a.n_seq; s += kThreads) x += blocks_of(s, blockIdx.x == 0);
+    for (int s = threadIdx.x; s < a.n_seq; s += kThreads) x += blocks_of(rows_of(s, blockIdx.x == 0));
     scan(x, all);
   } else {
-    mine = blocks_of(threadIdx.x, blockIdx.x == 0);
+    mine = blocks_of(rows_of(threadIdx.x, blockIdx.x == 0));
     upto = scan(mine, all);
   }
   if (a.len_out)
@@ -202,7 +204,7 @@ __global__ void __launch_bounds__(kThreads, PACK && E4M3 ? 2 : 3) paged_copy_ker
   long long base = 0;  // of a chunk of sequences
   for (int chunk = 0;; chunk += kThreads) {
     if (a.n_seq > kThreads) {
-      mine = blocks_of(chunk + threadIdx.x, false);
+      mine = blocks_of(rows_of(chunk + threadIdx.x, false));
       long long here;
       upto = base + scan(mine, here);
       all = base + here;
@@ -213,6 +215,7 @@ __global__ void __launch_bounds__(kThreads, PACK && E4M3 ? 2 : 3) paged_copy_ker
     }
     __syncthreads();
     if (block < all) break;
+    if (chunk + kThreads >= a.n_seq) return;  // the lengths have changed since the line was cut
     base = all;
   }
   int seq = (int)found[0];
@@ -245,10 +248,9 @@ __global__ void __launch_bounds__(kThreads, PACK && E4M3 ? 2 : 3) paged_copy_ker
       p.page += a.pages.head_stride;
     }
   };
-  while (at < end) {
-    const int n = __ldcg(a.len_in + seq);  // in range where the line has a block of it
-    const int blocks = n < 0 || n > a.cap ? 0 : (n + per_block - 1) / per_block;
-    if (block >= blocks) {
+  while (at < end && seq < a.n_seq) {
+    const int n = rows_of(seq, false);
+    if (block >= blocks_of(n)) {
       ++seq;
       block = 0;
       continue;
