@@ -81,6 +81,7 @@ struct PagedRows {
     const int seq = tok / a.B, b = tok - seq * a.B;
     return (long long)(p.pos_first_new ? p.pos_first_new[seq] : __ldcg(p.pages.len + seq)) + b;
   }
+  static constexpr bool kRows = false;
   __device__ bool on(int t) const { return rows[t] != kNoToken; }
   __device__ void put(char* base, const float* scale, int t, int kh, int c,
                       const float (&x)[8]) const {

@@ -1,9 +1,9 @@
 // vd_qkv.cu -- vd_qkv_norm_rope (include/vd.h): from the projection rows of new
 // tokens to the queries and to the new rows of one layer, in one pass (vd_qkv.cuh).
 //
-// Bound by DRAM for prompts (16384 tokens of 48 heads of 128 values 69.7 us, 85 % of the copy
+// Bound by DRAM for prompts (16384 tokens of 48 heads of 128 values 69.4 us, 86 % of the copy
 // peak; 82.5 without the early load of the next head), by launch and latency for single
-// tokens (4.1 us in a graph).
+// tokens (4.2 us in a graph).
 #include <cuda_runtime.h>
 
 #include <cstdint>
@@ -32,14 +32,15 @@ struct NewRows {  // rows of [n_seq][n_layer][n_kv_head][B][head_dim]
   __device__ long long position(int tok) const {
     return (long long)n.pos_first_new[tok / a.B] + tok % a.B;
   }
-  __device__ bool on(int) const { return true; }
-  __device__ void key(int t, int kh, int c, const float (&x)[8]) const {
-    st16(n.k_new + (new_row[t] + (size_t)kh * a.B) * a.d + c * 8, pack8(x));
-  }
-  __device__ void value(int t, int kh, int c, const uint4& w) const {
-    st16(n.v_new + (new_row[t] + (size_t)kh * a.B) * a.d + c * 8, w);
+  static constexpr bool kRows = true;
+  __device__ uint16_t* row(int t, int kh, bool key) const {
+    return (key ? n.k_new : n.v_new) + (new_row[t] + (size_t)kh * a.B) * a.d;
   }
 };
+
+// Up to 3 tokens an SM take the kernel with registers for the norm weights, whose CTAs all run at once
+// then (us in a graph, 32 + 16 heads: 456 tokens 6.4 / 7.5 without, 608 9.5 / 7.5)
+constexpr int kFewCtas = 3;
 
 template <bool INTERLEAVED, bool FEW>
 __global__ void __launch_bounds__(kThreads) qkv_norm_rope_kernel(QkvArgs a, NewRowsArgs n) {
@@ -75,9 +76,10 @@ extern "C" vd_status vd_qkv_norm_rope(const void* qkv, int32_t n_seq, int32_t B,
                          static_cast<uint16_t*>(v_new), layer, n_layer};
   return launch_clusters(qkv_grid(a), kThreads, 1, qkv_smem(a),
                          reinterpret_cast<cudaStream_t>(stream),
-                         a.tokens_per_cta > 1 ? (interleaved ? qkv_norm_rope_kernel<true, false>
-                                                             : qkv_norm_rope_kernel<false, false>)
-                                              : (interleaved ? qkv_norm_rope_kernel<true, true>
-                                                             : qkv_norm_rope_kernel<false, true>),
+                         a.tokens <= kFewCtas * dev.sms
+                             ? (interleaved ? qkv_norm_rope_kernel<true, true>
+                                            : qkv_norm_rope_kernel<false, true>)
+                             : (interleaved ? qkv_norm_rope_kernel<true, false>
+                                            : qkv_norm_rope_kernel<false, false>),
                          a, n);
 }

@@ -60,11 +60,16 @@ __device__ __forceinline__ void scale8(float (&x)[8], float r, const uint4& w) {
 // table: [token][cos half | sin half].  Sink: where keys and values go,
 //   place(t, tok)  by one thread for each token t of the CTA, before the others are called
 //   position(tok)  of a token (any thread)
-//   on(t)          whether the token's heads are written at all
-//   key(t, kh, c, x), value(t, kh, c, w)  chunk c of a KV head, in fp32 and as it came
-// FEW (a token a CTA): the norm weights are loaded with the first values, not where they are
-// wanted: one token 5.3 us in a graph for 7.1; with many tokens their registers cost a CTA of the
-// SM (16384 tokens 91 us for 81).
+//   kRows          every head goes to a bf16 row, which
+//     row(t, kh, key)  names (of the keys, or of the values); else
+//     on(t)            whether the token's heads are written at all
+//     key(t, kh, c, x), value(t, kh, c, w)  chunk c of a KV head, in fp32 and as it came
+// Rows have one store for all heads and their place by a quotient, the others by steps: 16384 tokens
+// into rows 69.4 us (72.0 the other way), into 8-bit pages 97.1 (101.7), where what is live around the
+// conversions leaves no registers for it.
+// FEW (a token a CTA, and all CTAs run at once or nearly): the norm weights are loaded with the first
+// values, not where they are wanted: one token 4.9 us in a graph for 6.4; with many tokens their
+// registers cost CTAs of the SM (16384 tokens 91 us for 81 into pages; 608 into rows 9.5 for 7.5).
 template <bool INTERLEAVED, bool FEW, class Sink>
 __device__ __forceinline__ void norm_rope_tokens(const QkvArgs& a, float* table, const Sink& sink) {
   const int half = a.rd >> 1;
@@ -114,19 +119,31 @@ __device__ __forceinline__ void norm_rope_tokens(const QkvArgs& a, float* table,
   }
   __syncthreads();
   const int dt = slots / heads, dh = slots - dt * heads;  // of a round
-  int t = (int)(threadIdx.x / a.lanes) / heads, h = (int)(threadIdx.x / a.lanes) - t * heads;
+  int step_t = (int)(threadIdx.x / a.lanes) / heads,
+      step_h = (int)(threadIdx.x / a.lanes) - step_t * heads;
   auto advance = [&] {
-    t += dt;
-    h += dh;
-    if (h >= heads) {
-      h -= heads;
-      ++t;
+    step_t += dt;
+    step_h += dh;
+    if (step_h >= heads) {
+      step_h -= heads;
+      ++step_t;
     }
   };
   for (int it = threadIdx.x / a.lanes; it < items; it += slots, advance()) {
-    const uint4 w0 = n0, w1 = n1;
+    const int t = Sink::kRows ? it / heads : step_t, h = Sink::kRows ? it % heads : step_h;
+    uint4 w0 = n0, w1 = n1;
     fetch(it + slots);
-    if (!sink.on(t)) continue;
+    uint16_t* dst = nullptr;  // kRows: of the head
+    if constexpr (Sink::kRows) {
+      if (h < a.n_q) {
+        dst = a.q_out + ((size_t)(tok0 + t) * a.n_q + h) * a.d;
+      } else {
+        const bool key = h < a.n_q + a.n_kv;
+        dst = sink.row(t, key ? h - a.n_q : h - a.n_q - a.n_kv, key);
+      }
+    } else {
+      if (!sink.on(t)) continue;
+    }
     if (h < a.n_q + a.n_kv) {
       float x[8], y[8];
       unpack8(w0, x);
@@ -168,17 +185,24 @@ __device__ __forceinline__ void norm_rope_tokens(const QkvArgs& a, float* table,
           }
         }
       }
-      if (h >= a.n_q) {
+      if constexpr (Sink::kRows) {
+        w0 = pack8(x);
+        w1 = pack8(y);
+      } else if (h >= a.n_q) {
         if (active) sink.key(t, h - a.n_q, c0, x);
         if (second) sink.key(t, h - a.n_q, c1, y);
       } else {
-        uint16_t* dst = a.q_out + ((size_t)(tok0 + t) * a.n_q + h) * a.d;
+        dst = a.q_out + ((size_t)(tok0 + t) * a.n_q + h) * a.d;
         if (active) st16(dst + c0 * 8, pack8(x));
         if (second) st16(dst + c1 * 8, pack8(y));
       }
-    } else {
+    } else if constexpr (!Sink::kRows) {
       if (active) sink.value(t, h - a.n_q - a.n_kv, c0, w0);
       if (second) sink.value(t, h - a.n_q - a.n_kv, c1, w1);
+    }
+    if constexpr (Sink::kRows) {
+      if (active) st16(dst + c0 * 8, w0);
+      if (second) st16(dst + c1 * 8, w1);
     }
   }
 }
