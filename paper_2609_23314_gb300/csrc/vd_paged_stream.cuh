@@ -101,14 +101,18 @@ __device__ __forceinline__ bool bar_done(uint32_t bar, uint32_t parity) {
   return done != 0;
 }
 
-// Waits for a phase; gives up after `limit` polls, and once another warp has.
+// Waits for a phase; gives up after `limit` polls, and once another warp has.  By a whole warp, whose
+// lanes get the same answer: what follows a wait are products, shuffles and barriers of all of them, and
+// a lane that has seen the phase end beside one that has run out of polls would wait there for ever.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* dead,
                                          const PagedAttendArgs& a) {
-  if (bar_done(bar, parity)) return true;
+  bool done = bar_done(bar, parity);
+  if (__all_sync(kFull, done)) return true;
 #pragma unroll 1
   for (uint32_t i = 0; i < a.wait_limit; ++i) {
-    if (bar_done(bar, parity)) return true;
-    if (*dead) return false;
+    if (!done) done = bar_done(bar, parity);
+    if (__all_sync(kFull, done)) return true;
+    if (__any_sync(kFull, *dead)) break;
   }
   *dead = 1;
   record_status(a.pages.status, kStTimeout);
