@@ -535,8 +535,9 @@ vd_status vd_paged_attend(const vd_paged_cache* c, int32_t layer, const void* q,
                           void* out, float* lse_out, void* workspace, size_t workspace_bytes,
                           vd_stream_t stream);
 
-/* Bytes of workspace that vd_paged_attend takes on the current device for B tokens of
- * n_q_head heads, whatever the lengths (0 where the arguments are refused). */
+/* Bytes of workspace that vd_paged_attend takes on the current device: one size for all calls over
+ * caches of c's type and head_dim, whatever their sequences, tokens, heads and lengths (0 where the
+ * arguments are refused). */
 size_t vd_paged_attend_workspace(const vd_paged_cache* c, int32_t n_q_head, int32_t B);
 
 /* len[s] += n_new[s] (NULL: B), at the end of a step, after its last layer. */

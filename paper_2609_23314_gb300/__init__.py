@@ -750,7 +750,8 @@ def vd_paged_append(cache: PagedCache, qkv, q_out, layer: int = 0, q_weight=None
 
 
 def vd_paged_attend_workspace(cache: PagedCache, n_q_head: int, B: int) -> int:
-    """Bytes of workspace that vd_paged_attend takes on the current device."""
+    """Bytes of workspace that vd_paged_attend takes on the current device: one size for all calls
+    over caches of this type and head_dim, whatever their sequences, tokens, heads and lengths."""
     return int(load_library().vd_paged_attend_workspace(cache._ref, int(n_q_head), int(B)))
 
 

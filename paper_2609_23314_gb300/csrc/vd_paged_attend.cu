@@ -194,9 +194,19 @@ struct Plan {
   const PagedKernel* kernel;
   int rows, tiles, cluster, ctas;
   bool one_launch;             // no parts to join
-  size_t split, stats, parts;  // bytes of the workspace's three parts
+  size_t split, stats;         // bytes of the workspace's first two parts
+  size_t workspace;            // of all that a call may take
   unsigned* status;
 };
+
+// What a call over a cache of this type and head_dim takes at most: pieces of the line on all SMs (the
+// streaming kernel's shared memory leaves room for one CTA on each), in the larger of its tiles.  By
+// neither tokens nor sequences: a single token may go in pieces where a block of tokens takes
+// clusters, and a workspace that fits the one call has to fit the other.
+size_t workspace_of(const PagedKernel* kernels, int sms, int d) {
+  const size_t rows = kernels[0].rows > kernels[1].rows ? kernels[0].rows : kernels[1].rows;
+  return 16 + sms * (sizeof(int4) + 2 * rows * (sizeof(float2) + d * sizeof(float)));
+}
 
 // Refuses what the call refuses of its sizes.
 vd_status plan_of(const vd_paged_cache* c, int n_q_head, int B, Plan* plan) {
@@ -216,7 +226,8 @@ vd_status plan_of(const vd_paged_cache* c, int n_q_head, int B, Plan* plan) {
   const int kind = want_kind >= 0 && want_kind < kKinds
                        ? want_kind
                        : choose_kernel(rows, (long long)c->n_seq * c->n_kv_head, capacity, e4m3, dev.sms);
-  const PagedKernel& k = (e4m3 ? kPagedE4m3 : kPagedBf16)[m][kind];
+  const PagedKernel* kernels = (e4m3 ? kPagedE4m3 : kPagedBf16)[m];
+  const PagedKernel& k = kernels[kind];
   Slots& slots = g_slots[dev.id][e4m3][m][kind];
   r = slots_of(dev, k, slots);
   if (r != VD_OK) return r;
@@ -239,11 +250,10 @@ vd_status plan_of(const vd_paged_cache* c, int n_q_head, int B, Plan* plan) {
   plan->cluster = n;
   plan->one_launch = n > 1 || kind == 2;
   if (units * n > INT_MAX) return VD_ERR_UNSUPPORTED;
-  plan->ctas = plan->one_launch ? (int)(units * n) : slots.at[1];
-  const size_t parts = plan->one_launch ? 0 : 2 * (size_t)plan->ctas * plan->rows;
+  plan->ctas = plan->one_launch ? (int)(units * n) : slots.at[1] < dev.sms ? slots.at[1] : dev.sms;
   plan->split = plan->one_launch ? 0 : (size_t)plan->ctas * sizeof(int4);
-  plan->stats = parts * sizeof(float2);
-  plan->parts = parts * c->head_dim * sizeof(float);
+  plan->stats = plan->one_launch ? 0 : 2 * (size_t)plan->ctas * plan->rows * sizeof(float2);
+  plan->workspace = workspace_of(kernels, dev.sms, c->head_dim);
   return VD_OK;
 }
 
@@ -255,8 +265,7 @@ extern "C" {
 
 size_t vd_paged_attend_workspace(const vd_paged_cache* c, int32_t n_q_head, int32_t B) {
   vd::Plan p;
-  // at least one unit of 16 bytes: a workspace is never empty
-  return vd::plan_of(c, n_q_head, B, &p) == VD_OK ? 16 + p.split + p.stats + p.parts : 0;
+  return vd::plan_of(c, n_q_head, B, &p) == VD_OK ? p.workspace : 0;
 }
 
 vd_status vd_paged_attend(const vd_paged_cache* c, int32_t layer, const void* q, int32_t B,
@@ -273,7 +282,7 @@ vd_status vd_paged_attend(const vd_paged_cache* c, int32_t layer, const void* q,
   Plan p;
   r = plan_of(c, n_q_head, B, &p);
   if (r != VD_OK) return r;
-  if (workspace_bytes < 16 + p.split + p.stats + p.parts) return VD_ERR_INVALID_ARG;
+  if (workspace_bytes < p.workspace) return VD_ERR_INVALID_ARG;
   PagedAttendArgs a;
   a.pages = pages_of(c, layer, p.status);
   a.q = static_cast<const uint16_t*>(q);

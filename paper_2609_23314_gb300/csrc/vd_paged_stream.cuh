@@ -155,6 +155,7 @@ struct StreamShape {
   static constexpr int kMem = kStats + kWarpsUsed * 8 * 8;
   static constexpr int kTotal = kMem + (int)sizeof(StreamMem<kPlaces>);
   static_assert(kTotal <= 232448, "shared memory");
+  static_assert(2 * kTotal > 228 * 1024, "one CTA on an SM, as the workspace has it");
   static_assert(kPlaces % kProducers == 0, "a place has one producer and one consumer");
 };
 
