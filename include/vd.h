@@ -462,7 +462,8 @@ vd_status vd_qkv_norm_rope(const void* qkv, int32_t n_seq, int32_t B, int32_t n_
  * On the device, a sequence whose len, or len and new tokens, lie out of
  * [0, max_pages * page_size], or whose n_new lies out of [0, B], gets no row and no output
  * (VD_ERR_DEVICE_LEN).  A page out of [0, n_page) is neither read nor written
- * (VD_ERR_DEVICE_PAGE); outputs that needed it are unspecified.
+ * (VD_ERR_DEVICE_PAGE); outputs that needed it are unspecified.  len, page_table and n_new are read
+ * while a call runs, more than once: they change in stream order, never beside a call.
  * ------------------------------------------------------------------------ */
 typedef enum { VD_PAGED_BF16 = 0, VD_PAGED_E4M3 = 1 } vd_paged_type;
 
@@ -523,8 +524,8 @@ vd_status vd_paged_append(const vd_paged_cache* c, int32_t layer, const void* qk
  * A token that sees no slot, or whose scores are all -infinity, gets out = 0 and lse = -inf.
  * Values that a token does not see do not reach it, NaN and infinities among them; one that it
  * sees gives NaN (a NaN, or an infinity whose weight is 0) or an infinity.  Scores, softmax
- * statistics and sums are fp32; weights are rounded to two bf16 parts (2^-16 of themselves) for
- * bf16 pages and to fp16 for e4m3 ones, where those below 2^-36 of the largest count for nothing.
+ * statistics and sums are fp32; weights are rounded to two bf16 parts (1.06 * 2^-16 of themselves)
+ * for bf16 pages and to fp16 for e4m3 ones, where those below 2^-36 of the largest count for nothing.
  * Range: scores, products of a query's and a key's values, and sums of values times weights of up
  * to 2^15 have to be finite in fp32; scale times a query row's largest magnitude (times the keys'
  * scale, with e4m3 pages) has to lie in [2^-60, 2^60].

@@ -4,8 +4,10 @@
 //
 // One read and one write of every value.  Whole caches are bound by DRAM (36 layers of 8 heads and
 // 4096 slots out of pages and back 364 us, 98 % of the copy peak); prompts by the issue of the norms'
-// and the rotation's instructions (16384 tokens of 48 heads 78 us, 5.1 TB/s); ragged 8-bit pages by
-// their conversions (183 MB 51 us); single tokens by launch and latency (5.3 us in a graph).
+// and the rotation's instructions (16384 tokens of 48 heads 78 us, 5.1 TB/s); ragged 8-bit pages (183 MB
+// 52 us) by neither, 0.46 instructions a cycle and scheduler: their CTAs are short, each with a chain of
+// latencies before its first row (lengths, scan, page), and come in 1.6 to 2.4 waves, as the grid goes by
+// capacities; single tokens by launch and latency (5.3 us in a graph).
 #include <cuda_runtime.h>
 
 #include <climits>

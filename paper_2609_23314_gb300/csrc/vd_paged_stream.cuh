@@ -13,14 +13,14 @@
 //
 // Per 16 slots a warp computes  S^T = K Q^T  and  O^T += V^T P^T  with slots and head dims on the
 // 16-row side of m16n8k16, so that 8 query rows fill a tile.  bf16 pages are multiplied as
-// they are, weights in two bf16 parts (2^-16 of a weight); e4m3 ones go to fp16 (exact), Q too
+// they are, weights in two bf16 parts (1.06 * 2^-16 of a weight); e4m3 ones go to fp16 (exact), Q too
 // with each row scaled by a power of two (QueryScale), weights are rounded to fp16.  Sums are
 // fp32.
 //
 // Long batches are bound by DRAM: 512 KV heads around 4096 slots 131 us (6.2 TB/s, 92 % of the copy
-// peak), 16 heads of 131000 slots 165 (96 %); in e4m3, where a slot's arithmetic takes 300 cycles of an
-// SM for the 350 of its bytes, 84 (4.9 TB/s).  Small calls by a chain of latencies (length, page,
-// slots, meeting, join): 8 heads of 4096 slots 11.2 us.  Copies in the computing warps took 40 % of
+// peak), 16 heads of 131000 slots 166 (95 %); in e4m3, where a slot's arithmetic takes 300 cycles of an
+// SM for the 350 of its bytes, 77 to 86 from one machine to another (4.8 to 5.3 TB/s).  Small calls by a chain of latencies (length, page,
+// slots, meeting, join): 8 heads of 4096 slots 11.7 us.  Copies in the computing warps took 40 % of
 // their time (93 us for 84), boxes of tensor maps 119.
 #pragma once
 
@@ -173,8 +173,9 @@ struct Swizzle {
   }
 };
 
-// The running maximum less this is the point that weights are relative to: fp16 weights far
-// below the largest keep their bits, and the point moves only where the maximum rises by more.
+// The running maximum less this is the point that weights are relative to: fp16 weights far below the
+// largest keep their bits.  The point moves with every rise of the maximum that one of the warp's rows
+// sees (there is no slack before it does).
 template <bool E4M3>
 constexpr float kPagedLift = E4M3 ? 15.f : 8.f;
 
@@ -185,7 +186,8 @@ __device__ __forceinline__ bool not_finite(uint32_t w) {
   return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
 }
 
-// Two weights in bf16, and in `low` what that leaves of them: together within 2^-16 of a weight.
+// Two weights in bf16, and in `low` what that leaves of them: together within 1.06 * 2^-16 of a weight
+// (half a step of the lower part, and 2^-20).
 // The upper part is rounded towards zero and the lower one is of 2^-20 of the weight more, so that
 // both are above 0 where the weight is (but for weights below 2^-113): an infinite value stays one.
 __device__ __forceinline__ uint32_t split_weights(float x, float y, uint32_t& low) {

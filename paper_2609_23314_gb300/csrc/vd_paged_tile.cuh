@@ -14,9 +14,11 @@
 //   15    one thread issues the products.
 // A cluster splits the tiles of a unit and joins the results through distributed shared memory.
 //
-// 128 new tokens over 2048, 8 KV heads of 4 query heads, 21 us: start and queries 4, 5 tiles of 2.2
-// (softmax 2000 cycles a tile of 128 slots, most of it the exponentials; the products 2300, of which
-// the weights' lower parts are 800), the join.  8 sequences of 4000 slots, 16 rows 39 us (3.4 TB/s).
+// 128 new tokens over 2048, 8 KV heads of 4 query heads, 21 us: start and queries 4, 5 tiles of 2.2,
+// the join.  A tile of 128 slots takes the softmax 2000 cycles, most of it the exponentials, and the
+// products 2300, of which the weights' lower parts are 800; its 2.2 us are about 4500, the sum of the
+// two, although the roles are there to overlap.  What keeps them apart has not been measured: copies
+// that run one tile ahead only, with 5 tiles a CTA, or the chain from scores to weights to product.  8 sequences of 4000 slots, 16 rows 39 us (3.4 TB/s).
 // Copies by lanes with a fixed chunk of every row: 26 us without.
 #pragma once
 
